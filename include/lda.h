@@ -229,8 +229,8 @@ lda_status lda_loglik_noalloc(lda_handle *h, double *llpt);
 /* Release every resource of the handle.  NULL is allowed. */
 void lda_destroy(lda_handle *h);
 
-/* Message for the last failure on h (or on the last failed lda_create when h
- * is NULL).  Never NULL. */
+/* Message for the last failure on h (when h is NULL: of the last failed
+ * lda_create or operator of lda_ops.h on the calling thread).  Never NULL. */
 const char *lda_last_error(const lda_handle *h);
 
 /*
