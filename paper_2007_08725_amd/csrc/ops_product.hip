@@ -54,31 +54,82 @@ __device__ inline f32x4 mma<float>(u32x4 r, u32x4 l, f32x4 c) {
   return c;
 }
 
-// Rows of an operand.  Rows past the end repeat the last one: their products
-// go nowhere, and no read leaves the matrix.
+// Operands.  A step of the product takes 128 bytes of k of every row (kStep
+// elements), in 16-byte chunks (kChunk elements).  An operand lies in memory
+// either with k contiguous ("rows") or with its rows contiguous ("columns":
+// the transposed matrix, element (row, k) at p[k * ld + row]); neither is
+// copied for the other, LDS is read transposed.  `base` gives the address of
+// the chunk that a lane loads in step 0, `in` whether its chunk of a later
+// step lies inside k; steps before `full` need no check.  Rows past the end
+// repeat the last one (or chunk): their products go nowhere, and no read
+// leaves the matrix.
+template <typename T>
+constexpr int kChunk = 16 / int(sizeof(T));
+template <typename T>
+constexpr int kStep = 128 / int(sizeof(T));
+
 template <typename T>
 struct Rows {
+  static constexpr bool kContiguous = true;
   const T *p;
   int64_t ld;
-  int rows;
-  __device__ const char *row(int r) const {
-    return reinterpret_cast<const char *>(p + int64_t(min(r, rows - 1)) * ld);
+  int rows, k;
+  __device__ int full() const { return k / kStep<T>; }
+  __device__ int64_t stride() const { return 128; }
+  __device__ const char *base(int row, int k0) const {
+    return reinterpret_cast<const char *>(p + int64_t(min(row, rows - 1)) * ld + k0);
   }
+  __device__ bool in(int step, int k0) const { return step * kStep<T> + k0 < k; }
 };
 
-// Rows of w_gate and w_value in turns of 16: row n of the pair is row
+template <typename T>
+struct Columns {
+  static constexpr bool kContiguous = false;
+  const T *p;
+  int64_t ld;
+  int rows, k;
+  __device__ int full() const { return k / kStep<T>; }
+  __device__ int64_t stride() const { return 128 * ld; }
+  __device__ const char *base(int row, int k0) const {
+    return reinterpret_cast<const char *>(p + int64_t(k0) * ld + min(row, (rows - 1) / kChunk<T> * kChunk<T>));
+  }
+  __device__ bool in(int step, int k0) const { return step * kStep<T> + k0 < k; }
+};
+
+// The rows of w_gate and w_value in turns of 16: row n of the pair is row
 // (n / 32) * 16 + n % 16 of w_gate where n & 16 is 0, else of w_value.  A lane
 // that holds a fragment of a then holds the same elements of b in the next.
 __device__ inline int pair_row(int n) { return (n >> 5) * 16 + (n & 15); }
+
 template <typename T>
 struct PairRows {
+  static constexpr bool kContiguous = true;
   const T *gate, *value;
   int64_t ld_gate, ld_value;
-  int rows;
-  __device__ const char *row(int n) const {
-    const int64_t f = min(pair_row(n), rows - 1);
-    return reinterpret_cast<const char *>(n & 16 ? value + f * ld_value : gate + f * ld_gate);
+  int hidden, k;
+  __device__ int full() const { return k / kStep<T>; }
+  __device__ int64_t stride() const { return 128; }
+  __device__ const char *base(int n, int k0) const {
+    const int64_t f = min(pair_row(n), hidden - 1);
+    return reinterpret_cast<const char *>((n & 16 ? value + f * ld_value : gate + f * ld_gate) + k0);
   }
+  __device__ bool in(int step, int k0) const { return step * kStep<T> + k0 < k; }
+};
+
+// The pair as an operand of dx, whose k runs over the pair's rows.
+template <typename T>
+struct PairColumns {
+  static constexpr bool kContiguous = false;
+  const T *gate, *value;
+  int64_t ld;  // of both
+  int width, hidden;
+  __device__ int full() const { return 2 * hidden / kStep<T>; }
+  __device__ int64_t stride() const { return 64 * ld; }
+  __device__ const char *base(int row, int k0) const {
+    return reinterpret_cast<const char *>((k0 & 16 ? value : gate) + int64_t(pair_row(k0)) * ld +
+                                          min(row, (width - 1) / kChunk<T> * kChunk<T>));
+  }
+  __device__ bool in(int step, int k0) const { return pair_row(step * kStep<T> + k0) < hidden; }
 };
 
 // What the epilogue of a workgroup's wave needs to know.
@@ -92,15 +143,16 @@ struct Place {
 
 struct Grid {
   int mtiles, ntiles;
-  int chunks;        // 16-byte chunks of k
-  int steps, split;  // 128-byte steps of k in all, and of one split
+  int steps, split;  // steps of k in all, and of one split
 };
 
-// 16 bytes that every lane whose chunk lies past the end of k reads instead
+// what a lane whose chunk lies past the end of k reads instead
 __device__ const u32x4 kZeroChunk = {0, 0, 0, 0};
 
 typedef const __attribute__((address_space(1))) void *global_ptr;
 typedef __attribute__((address_space(3))) void *lds_ptr;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // Tile order: the tiles are cut into eight runs, one for each accelerator die
 // (workgroups go to the dies in turn), and a run walks groups of eight tile
@@ -118,47 +170,108 @@ __device__ inline bool tile_of(const Grid &g, int &mt, int &nt) {
   return true;
 }
 
-// C tile of BM x BN by WM x WN waves.  Each step loads 128 bytes of k of every
-// row straight into LDS (two buffers, the next step's loads in flight while
-// this step's fragments are multiplied).  A row is eight 16-byte chunks; chunk
-// c of row r lies at place c ^ (r & 7), so that the 16 rows that a fragment
-// read touches spread over the banks.
+// An operand's part of a stage in LDS, B rows: B/8 loads of 1 KiB, dealt to the
+// waves in turns.
+//
+// k contiguous: 128 bytes a row; chunk c of row r lies at place c ^ (r & 7), so
+// that the 16 rows that a fragment read touches spread over the banks.
+//
+// Rows contiguous: kStep lines of B elements, in slots of 16 rows.  Four
+// 16-bit lines of a slot are what one transposing read of 16 lanes takes
+// (8 bytes each: lane q reads line q / 4, rows 4 (q % 4) on, and gets row q of
+// the four lines), in single precision a line's slot is one read.  The slots
+// of a line are permuted by the line's number so that lines read together
+// spread over the banks.
+template <typename T>
+__device__ inline int slot_turn(int line) {
+  return sizeof(T) == 2 ? (line & 3) | ((line >> 1) & 4) : (line >> 2) & 3;
+}
+
+template <typename T, int B, int WAVES, typename Op>
+struct Stage {
+  static constexpr int LOADS = B / 8 / WAVES;
+  static constexpr int LINE = B * int(sizeof(T));  // bytes, rows contiguous
+  const char *src[LOADS];
+  int k0[LOADS];  // of the lane's chunk in a step (k contiguous: the same in every load)
+
+  __device__ Stage(const Op &op, int row0, int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int load = i * WAVES + wave;
+      if (Op::kContiguous) {
+        k0[i] = ((lane & 7) ^ (lane >> 3)) * kChunk<T>;
+        src[i] = op.base(row0 + load * 8 + (lane >> 3), k0[i]);
+      } else {
+        const int at = load * 1024 + lane * 16, line = at / LINE, part = at % LINE / 16;
+        constexpr int per_slot = int(sizeof(T));  // 16-byte parts of 16 elements
+        const int slot = (part / per_slot) ^ slot_turn<T>(line);
+        k0[i] = line;
+        src[i] = op.base(row0 + slot * 16 + part % per_slot * kChunk<T>, line);
+      }
+    }
+  }
+  __device__ void load(const Op &op, int step, char *to, int wave) const {
+    const int64_t ahead = step * op.stride();
+    if (step < op.full()) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        __builtin_amdgcn_global_load_lds((global_ptr)(src[i] + ahead), (lds_ptr)(to + (i * WAVES + wave) * 1024), 16, 0,
+                                         0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const char *p = op.in(step, k0[i]) ? src[i] + ahead : reinterpret_cast<const char *>(&kZeroChunk);
+        __builtin_amdgcn_global_load_lds((global_ptr)p, (lds_ptr)(to + (i * WAVES + wave) * 1024), 16, 0, 0);
+      }
+    }
+  }
+  // The fragment of rows row0..row0+15 (of the tile), half s of the step.
+  static __device__ u32x4 fragment(const char *tile, int row0, int s, int lane) {
+    const int q = lane & 15, group = lane >> 4;
+    if (Op::kContiguous) {
+      const int place = (s * 4 + group) ^ (q & 7);
+      return *reinterpret_cast<const u32x4 *>(tile + (row0 + q) * 128 + place * 16);
+    }
+    if (sizeof(T) == 2) {
+      const int line = s * 32 + group * 8 + (q >> 2);
+      const char *p = tile + line * LINE + (((row0 >> 4) ^ slot_turn<T>(line)) * 32) + (q & 3) * 8;
+      const u32x2 lo = transposed(p), hi = transposed(p + 4 * LINE);
+      return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
+    u32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int line = (s * 4 + group) * 4 + e;
+      v[e] = *reinterpret_cast<const uint32_t *>(tile + line * LINE + (((row0 >> 4) ^ slot_turn<T>(line)) * 64) + q * 4);
+    }
+    return v;
+  }
+  static __device__ u32x2 transposed(const char *p) {
+    return __builtin_bit_cast(
+        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p));
+  }
+};
+
+// C tile of BM x BN by WM x WN waves: two stages in LDS, the next step's loads
+// (straight into LDS) in flight while this step's fragments are multiplied.
 template <typename T, int BM, int BN, int WM, int WN, typename L, typename R, typename Epilogue>
 __global__ __launch_bounds__(64 * WM *WN) void k_product(Grid g, L left, R right, Epilogue epilogue) {
   constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16, WAVES = WM * WN;
-  constexpr int LOADS = (BM + BN) / 8 / WAVES;  // 1 KiB loads of one wave and step
   constexpr int STAGE = (BM + BN) * 128;
-  static_assert((BM / 8) % WAVES == 0 && (BN / 8) % WAVES == 0, "a wave's loads are all of one operand's kind");
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   int mt, nt;
   if (!tile_of(g, mt, nt)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
-
-  const int chunk = (lane & 7) ^ (lane >> 3);
-  const char *src[LOADS];
-#pragma unroll
-  for (int i = 0; i < LOADS; ++i) {
-    const int r = (i * WAVES + wave) * 8 + (lane >> 3);
-    src[i] = (i * WAVES * 8 < BM ? left.row(mt * BM + r) : right.row(nt * BN + r - BM)) + chunk * 16;
-  }
+  typedef Stage<T, BM, WAVES, L> StageL;
+  typedef Stage<T, BN, WAVES, R> StageR;
+  const StageL from_l(left, mt * BM, wave, lane);
+  const StageR from_r(right, nt * BN, wave, lane);
   const int begin = int(blockIdx.z) * g.split, end = min(g.steps, begin + g.split);
 
   auto load = [&](int step, int stage) {
-    char *to = lds + stage * STAGE + wave * 1024;
-    if (step * 8 + 8 <= g.chunks) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i)
-        __builtin_amdgcn_global_load_lds((global_ptr)(src[i] + int64_t(step) * 128),
-                                         (lds_ptr)(to + i * WAVES * 1024), 16, 0, 0);
-    } else {
-      const bool in = step * 8 + chunk < g.chunks;
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const char *p = in ? src[i] + int64_t(step) * 128 : reinterpret_cast<const char *>(&kZeroChunk);
-        __builtin_amdgcn_global_load_lds((global_ptr)p, (lds_ptr)(to + i * WAVES * 1024), 16, 0, 0);
-      }
-    }
+    from_l.load(left, step, lds + stage * STAGE, wave);
+    from_r.load(right, step, lds + stage * STAGE + BM * 128, wave);
   };
 
   f32x4 acc[MI][NI];
@@ -173,15 +286,14 @@ __global__ __launch_bounds__(64 * WM *WN) void k_product(Grid g, L left, R right
   for (int step = begin; step < end; ++step) {
     const int stage = (step - begin) & 1;
     if (step + 1 < end) load(step + 1, stage ^ 1);
-    const char *tl = lds + stage * STAGE + wm * TM * 128, *tr = lds + stage * STAGE + (BM + wn * TN) * 128;
+    const char *tl = lds + stage * STAGE, *tr = tl + BM * 128;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const int place = (((s * 4 + (lane >> 4)) ^ (lane & 7)) * 16) + (lane & 15) * 128;
       u32x4 fl[MI], fr[NI];
 #pragma unroll
-      for (int i = 0; i < MI; ++i) fl[i] = *reinterpret_cast<const u32x4 *>(tl + i * 2048 + place);
+      for (int i = 0; i < MI; ++i) fl[i] = StageL::fragment(tl, wm * TM + i * 16, s, lane);
 #pragma unroll
-      for (int j = 0; j < NI; ++j) fr[j] = *reinterpret_cast<const u32x4 *>(tr + j * 2048 + place);
+      for (int j = 0; j < NI; ++j) fr[j] = StageR::fragment(tr, wn * TN + j * 16, s, lane);
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -232,7 +344,9 @@ struct Target {
   int rows;  // of p (and q)
   bool pair;
   bool whole;           // four columns can be stored at once
-  const float *factor;  // of the result, on the device; NULL = 1
+  const float *factor;  // of the result, on the device: one for all (step 0) or one a row (step 1); NULL = 1
+  int factor_step;
+  __device__ float scale(int m) const { return factor ? factor[m * factor_step] : 1.0f; }
   __device__ T *row(int m) const {
     const int f = pair ? pair_row(m) : m;
     if (f >= rows) return nullptr;
@@ -246,11 +360,12 @@ struct Store {
   int cols;
   template <int MI, int NI>
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
-    const float f = out.factor ? *out.factor : 1.0f;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      T *row = out.row(at.m0 + i * 16 + (at.lane & 15));
+      const int m = at.m0 + i * 16 + (at.lane & 15);
+      T *row = out.row(m);
       if (!row) continue;
+      const float f = out.scale(m);
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
         const int n = at.n0 + j * 16 + (at.lane >> 4) * 4;
@@ -371,11 +486,43 @@ struct GatedBackward {
 
 __device__ inline float exp_diff(float z, float top) { return __builtin_amdgcn_exp2f((z - top) * kLog2e); }
 
-// The logits of four words: past the vocabulary -inf.
-__device__ inline f32x4 logits(f32x4 c, const float *bias, int v, int vocab) {
+// Two parts of a softmax: (largest logit, sum of exp(z - it)).
+__device__ inline float2 softmax_join(float2 a, float2 b) {
+  const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.0f : top;
+  return make_float2(top, a.y * exp_diff(a.x, ref) + b.y * exp_diff(b.x, ref));
+}
+
+// The logits of a wave's words, in place: the bias added, and -inf past the
+// vocabulary.
+template <int MI, int NI>
+__device__ inline void add_bias(f32x4 (&c)[MI][NI], const float *bias, int n0, int lane, int first, int vocab) {
+  const int v0 = first + n0 + (lane >> 4) * 4;
+  const bool inside = first + n0 + NI * 16 <= vocab;  // the same for the whole wave
 #pragma unroll
-  for (int r = 0; r < 4; ++r) c[r] = v + r < vocab ? (bias ? c[r] + bias[v + r] : c[r]) : -INFINITY;
-  return c;
+  for (int j = 0; j < NI; ++j) {
+    f32x4 b = {0, 0, 0, 0};
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int v = v0 + j * 16 + r;
+      if (bias) b[r] = bias[min(v, vocab - 1)];
+      if (!inside && v >= vocab) {
+        b[r] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) c[i][j][r] = -INFINITY;
+      }
+    }
+    if (bias)
+#pragma unroll
+      for (int i = 0; i < MI; ++i) c[i][j] += b;
+  }
+}
+
+// Where a row's label is among the wave's words, if this lane holds it: the
+// word's index, else -1.
+template <int NI>
+__device__ inline int label_at(int label, int n0, int lane, int first, int vocab) {
+  const int at = label - first - n0 - (lane >> 4) * 4;
+  return label >= 0 && label < vocab && at >= 0 && at < NI * 16 && (at & 12) == 0 ? at : -1;
 }
 
 // Per row and tile of words: the largest logit and the sum of exp(z - it), and
@@ -390,21 +537,23 @@ struct SoftmaxPart {
   template <int MI, int NI>
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
     float2 *shared = reinterpret_cast<float2 *>(at.lds);  // [WN][BM]
+    add_bias(c, bias, at.n0, at.lane, 0, vocab);
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       const int m = at.m0 + i * 16 + (at.lane & 15);
-      const int label = m < rows ? labels[m] : -1;
+      const int hit = label_at<NI>(m < rows ? labels[m] : -1, at.n0, at.lane, 0, vocab);
+      if (__ballot(hit >= 0)) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (hit == j * 16 + r) label_logit[m] = c[i][j][r];
+      }
       float top = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        const int v = at.n0 + j * 16 + (at.lane >> 4) * 4;
-        c[i][j] = logits(c[i][j], bias, v, vocab);
+      for (int j = 0; j < NI; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          top = fmaxf(top, c[i][j][r]);
-          if (v + r == label && label < vocab) label_logit[m] = c[i][j][r];
-        }
-      }
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, c[i][j][r]);
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       // nothing but -inf: the sum is 0 against any finite reference
@@ -423,29 +572,39 @@ struct SoftmaxPart {
     if (threadIdx.x < BM && m < rows) {
       float2 a = shared[threadIdx.x];
 #pragma unroll
-      for (int w = 1; w < WN; ++w) {
-        const float2 b = shared[w * BM + threadIdx.x];
-        const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.0f : top;
-        a = make_float2(top, a.y * exp_diff(a.x, ref) + b.y * exp_diff(b.x, ref));
-      }
+      for (int w = 1; w < WN; ++w) a = softmax_join(a, shared[w * BM + threadIdx.x]);
       part[int64_t(at.nt) * rows + m] = a;
     }
   }
 };
 
-// G of one piece of the vocabulary (words from `first` on), and its column
-// sums by tile of rows.
+// G of one piece of the vocabulary (words from `first` on) without the rows'
+// own gradients, S (exp(z - lse) - [v = label]), and the column sums of the
+// rows' gradients times it by tile of rows.  |exp(z - lse) - 1| <= 1 wherever
+// G has one value that leads its row, so the label's -S is exact and what is
+// rounded is small beside it.  S is 1, in half precision 2^14, so that
+// probabilities down to 2^-28 are normal numbers.
+template <typename T>
+constexpr float kGradLog2 = 0.0f;
+template <>
+constexpr float kGradLog2<f16> = 14.0f;
+template <typename T>
+constexpr float kGradUnit = 1.0f;
+template <>
+constexpr float kGradUnit<f16> = 16384.0f;
+
 template <typename T, int BN, int WM>
 struct SoftmaxGrad {
   const float *bias;
   const int32_t *labels;
-  const float *lse, *dloss, *scale;  // scale[0]: of G's values in type T
-  T *grad;                           // [rows][ldg]
+  const float *lse, *row_factor;  // row_factor: dloss / S, 0 for a row that is left out
+  T *grad;                        // [rows][ldg]
   int64_t ldg;
   float *col_part;  // [mtiles][piece], NULL without a bias
   int rows, vocab, first, piece;
   template <int MI, int NI>
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
+    add_bias(c, bias, at.n0, at.lane, first, vocab);
     f32x4 sums[NI];
 #pragma unroll
     for (int j = 0; j < NI; ++j) sums[j] = f32x4{0, 0, 0, 0};
@@ -453,19 +612,26 @@ struct SoftmaxGrad {
     for (int i = 0; i < MI; ++i) {
       const int m = at.m0 + i * 16 + (at.lane & 15);
       const int label = m < rows ? labels[m] : -1;
-      const float l = m < rows ? lse[m] : 0.0f;
+      const float l = m < rows ? lse[m] : 0.0f, d = m < rows ? row_factor[m] : 0.0f;
       const bool kept = label >= 0 && label < vocab && l != -INFINITY;
-      const float d = kept ? dloss[m] * scale[0] : 0.0f;
 #pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        const int n = at.n0 + j * 16 + (at.lane >> 4) * 4, v = first + n;
-        const f32x4 z = logits(c[i][j], bias, v, vocab);
-        f32x4 grad;
+      for (int j = 0; j < NI; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          grad[r] = kept ? d * (exp_diff(z[r], l) - (v + r == label ? 1.0f : 0.0f)) : 0.0f;
-        if (m < rows && n < ldg) store4(grad_row(m) + n, grad, 4, true);
-        sums[j] += grad;
+          c[i][j][r] = kept ? __builtin_amdgcn_exp2f((c[i][j][r] - l) * kLog2e + kGradLog2<T>) : 0.0f;
+      const int hit = kept ? label_at<NI>(label, at.n0, at.lane, first, vocab) : -1;
+      if (__ballot(hit >= 0)) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (hit == j * 16 + r) c[i][j][r] -= kGradUnit<T>;
+      }
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        const int n = at.n0 + j * 16 + (at.lane >> 4) * 4;
+        if (m < rows && n < ldg) store4(grad + m * ldg + n, c[i][j], 4, true);
+        if (col_part) sums[j] += c[i][j] * d;
       }
     }
     if (!col_part) return;
@@ -488,7 +654,6 @@ struct SoftmaxGrad {
       col_part[int64_t(at.mt) * piece + n] = s;
     }
   }
-  __device__ T *grad_row(int m) const { return grad + m * ldg; }
 };
 
 // ---------------------------------------------------------- small kernels ---
@@ -499,19 +664,11 @@ __global__ __launch_bounds__(256) void k_lse_join(const float2 *part, int ntiles
   const int m = blockIdx.x * 16 + (threadIdx.x & 15), way = threadIdx.x >> 4;
   float2 a = make_float2(-INFINITY, 0.0f);
   if (m < rows)
-    for (int t = way; t < ntiles; t += 16) {
-      const float2 b = part[int64_t(t) * rows + m];
-      const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.0f : top;
-      a = make_float2(top, a.y * exp_diff(a.x, ref) + b.y * exp_diff(b.x, ref));
-    }
+    for (int t = way; t < ntiles; t += 16) a = softmax_join(a, part[int64_t(t) * rows + m]);
   shared[way][threadIdx.x & 15] = a;
   __syncthreads();
   if (threadIdx.x < 16 && m < rows) {
-    for (int w = 1; w < 16; ++w) {
-      const float2 b = shared[w][threadIdx.x];
-      const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.0f : top;
-      a = make_float2(top, a.y * exp_diff(a.x, ref) + b.y * exp_diff(b.x, ref));
-    }
+    for (int w = 1; w < 16; ++w) a = softmax_join(a, shared[w][threadIdx.x]);
     const float total = a.x == -INFINITY && a.y == 0.0f ? -INFINITY : a.x + kLn2 * __builtin_amdgcn_logf(a.y);
     lse[m] = total;
     const int label = labels[m];
@@ -524,11 +681,13 @@ __global__ __launch_bounds__(256) void k_lse_join(const float2 *part, int ntiles
   }
 }
 
-// The largest finite |dloss| of the rows kept, as a factor that brings G to
-// the range of its type and its inverse: out[0] = unit / top, out[1] = top /
-// unit (0 and 0 where no row has a gradient).
-__global__ __launch_bounds__(1024) void k_grad_scale(const float *dloss, const int32_t *labels, int rows, int vocab,
-                                                     float unit, float *out) {
+// The rows' gradients as factors of the products: row_factor = dloss / unit for
+// dx and dbias, and x_factor = dloss / (the largest finite |dloss|) for the rows
+// of x in dweight, whose result is then multiplied by out[0], that largest
+// value / unit.  All are 0 for rows that are left out.
+__global__ __launch_bounds__(1024) void k_grad_factors(const float *dloss, const float *lse, const int32_t *labels,
+                                                       int rows, int vocab, float unit, float *out, float *row_factor,
+                                                       float *x_factor) {
   __shared__ float shared[16];
   float top = 0.0f;
   for (int m = threadIdx.x; m < rows; m += 1024) {
@@ -538,23 +697,24 @@ __global__ __launch_bounds__(1024) void k_grad_scale(const float *dloss, const i
   for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
   if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = top;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < 16; ++w) top = fmaxf(top, shared[w]);
-    // a top below 2^-100 would overflow its inverse: it counts as that
-    top = top > 0.0f ? fmaxf(top, 0x1p-100f) : 0.0f;
-    out[0] = top > 0.0f ? unit / top : 0.0f;
-    out[1] = top / unit;
+  for (int w = 0; w < 16; ++w) top = fmaxf(top, shared[w]);
+  // below 2^-100 the quotients would leave the range: such a value counts as that
+  top = fmaxf(top, 0x1p-100f);
+  if (threadIdx.x == 0) out[0] = top / unit;
+  for (int m = threadIdx.x; m < rows; m += 1024) {
+    const bool kept = labels[m] >= 0 && labels[m] < vocab && lse[m] != -INFINITY;
+    row_factor[m] = kept ? dloss[m] / unit : 0.0f;
+    x_factor[m] = kept ? dloss[m] / top : 0.0f;
   }
 }
 
-// out[n] = factor * sum over t of part[t][n]
-__global__ __launch_bounds__(256) void k_sum_parts(const float *part, int count, int n_all, const float *factor,
-                                                   float *out) {
+// out[n] = sum over t of part[t][n]
+__global__ __launch_bounds__(256) void k_sum_parts(const float *part, int count, int n_all, float *out) {
   const int n = blockIdx.x * 256 + threadIdx.x;
   if (n >= n_all) return;
   float s = 0.0f;
   for (int t = 0; t < count; ++t) s += part[int64_t(t) * n_all + n];
-  out[n] = s * *factor;
+  out[n] = s;
 }
 
 // Joins the splits of a product.
@@ -568,7 +728,7 @@ __global__ __launch_bounds__(256) void k_join(const float *part, int splits, int
     if (!row || n >= cols) continue;
     f32x4 s = *reinterpret_cast<const f32x4 *>(part + at);
     for (int z = 1; z < splits; ++z) s += *reinterpret_cast<const f32x4 *>(part + z * all + at);
-    if (out.factor) s *= *out.factor;
+    s *= out.scale(m);
     store4(row + n, s, cols - n, out.whole);
   }
 }
@@ -578,45 +738,22 @@ __global__ __launch_bounds__(256) void k_zero(T *p, int64_t n) {
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) p[i] = T(0.0f);
 }
 
-// Copies for the products, zero where the source ends: dst[r][c] = src[r][c],
-// or transposed dst[c][r] = src[r][c], in 64 x 64 tiles.
+// A copy of a matrix for the products: its rows at multiples of 16 bytes, zero
+// past their end; each row times its factor, a row of factor 0 zero whatever it
+// holds (factor NULL = 1).
 template <typename T>
-struct Pack {
-  const T *src;
-  int64_t ld;
-  int rows, cols;
-  T *dst;
-  int64_t ldd;
-  int dst_rows, dst_cols;
-  const int32_t *labels;  // rows whose label is outside [0, vocab) are zero; NULL = none
-  int vocab;
-  int pair;  // transposed only: 0 = dst column r; 1, 2 = the places of w_gate's, w_value's rows among the pair's
-};
-
-template <typename T, bool Transposed>
-__global__ __launch_bounds__(256) void k_pack(Pack<T> a) {
-  __shared__ T tile[64][65];
-  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
-  for (int i = threadIdx.x; i < 4096; i += 256) {
-    const int r = r0 + (i >> 6), c = c0 + (i & 63);
+__global__ __launch_bounds__(256) void k_pack(const T *src, int64_t ld, int64_t rows, int cols, const float *factor,
+                                              T *dst, int ldd) {
+  const int64_t all = rows * ldd, step = int64_t(gridDim.x) * 256;
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += step) {
+    const int64_t r = i / ldd;
+    const int c = int(i % ldd);
     T v = T(0.0f);
-    if (r < a.rows && c < a.cols) {
-      v = a.src[int64_t(r) * a.ld + c];
-      if (a.labels && (a.labels[r] < 0 || a.labels[r] >= a.vocab)) v = T(0.0f);
+    if (c < cols) {
+      v = src[r * ld + c];
+      if (factor) v = factor[r] == 0.0f ? T(0.0f) : T(float(v) * factor[r]);
     }
-    tile[i >> 6][i & 63] = v;
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < 4096; i += 256) {
-    const int u = i >> 6, w = i & 63;
-    if (Transposed) {
-      const int c = c0 + u, r = r0 + w;
-      const int at = a.pair ? (r >> 4) * 32 + (r & 15) + (a.pair - 1) * 16 : r;
-      if (c < a.dst_rows && at < a.dst_cols) a.dst[int64_t(c) * a.ldd + at] = tile[w][u];
-    } else {
-      const int r = r0 + u, c = c0 + w;
-      if (r < a.dst_rows && c < a.dst_cols) a.dst[int64_t(r) * a.ldd + c] = tile[u][w];
-    }
+    dst[i] = v;
   }
 }
 
@@ -633,11 +770,6 @@ unsigned strided(int64_t workgroups) { return unsigned(workgroups < 65536 ? work
   } while (0)
 
 template <typename T>
-constexpr int chunk_elems() {
-  return 16 / int(sizeof(T));
-}
-
-template <typename T>
 bool whole4(const void *p, int64_t ld) {
   return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0 && ld % 4 == 0;
 }
@@ -646,45 +778,35 @@ bool whole4(const void *p, int64_t ld) {
 // 16 bytes and hold whole chunks.
 template <typename T>
 bool in_place(const void *p, int64_t ld, int64_t cols) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % chunk_elems<T>() == 0 && cols % chunk_elems<T>() == 0;
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % kChunk<T> == 0 && cols % kChunk<T> == 0;
 }
 
 template <typename T>
-hipError_t pack(const Pack<T> &a, bool transposed, hipStream_t s) {
-  // the tiles cover the source and the padding of the copy
-  const int64_t rows = transposed ? (a.pair ? ceil_div(a.dst_cols, 2) : a.dst_cols) : a.dst_rows;
-  const int64_t cols = transposed ? a.dst_rows : a.dst_cols;
-  const int64_t most = 65535 * 64;  // of one launch's grid along the rows
-  for (int64_t r = 0; r < rows; r += most) {
-    Pack<T> b = a;
-    if (r) {
-      b.src += r * a.ld;
-      b.rows = int(a.rows - r);
-      b.dst += transposed ? (a.pair ? 2 * r : r) : r * a.ldd;
-      if (transposed) b.dst_cols -= int(a.pair ? 2 * r : r);
-      else b.dst_rows -= int(r);
-      if (a.labels) b.labels += r;
-    }
-    const dim3 grid(unsigned(ceil_div(cols, 64)), unsigned(ceil_div(rows - r < most ? rows - r : most, 64)));
-    if (transposed) k_pack<T, true><<<grid, 256, 0, s>>>(b);
-    else k_pack<T, false><<<grid, 256, 0, s>>>(b);
-    OPS_TRY(hipGetLastError());
-  }
-  return hipSuccess;
+struct Matrix {
+  const T *p;
+  int64_t ld;
+};
+
+template <typename T>
+hipError_t pack(const void *p, int64_t ld, int64_t rows, int cols, const float *factor, T *copy, int64_t ldd,
+                hipStream_t s) {
+  k_pack<T><<<strided(ceil_div(rows * ldd, 256)), 256, 0, s>>>(static_cast<const T *>(p), ld, rows, cols, factor, copy,
+                                                              int(ldd));
+  return hipGetLastError();
 }
 
-// An operand of a product over its columns, copied where it has to be.
+// A matrix as the products read it, copied where it has to be.
 template <typename T>
-hipError_t operand(const void *p, int64_t ld, int rows, int cols, Arena &ws, bool dry, hipStream_t s, Rows<T> &out) {
+hipError_t operand(const void *p, int64_t ld, int64_t rows, int cols, Arena &ws, bool dry, hipStream_t s,
+                   Matrix<T> &out) {
   if (in_place<T>(p, ld, cols)) {
-    out = Rows<T>{static_cast<const T *>(p), ld, rows};
+    out = Matrix<T>{static_cast<const T *>(p), ld};
     return hipSuccess;
   }
-  const int64_t ldd = round_up(cols, chunk_elems<T>());
-  T *copy = ws.take<T>(int64_t(rows) * ldd);
-  out = Rows<T>{copy, ldd, rows};
-  if (dry) return hipSuccess;
-  return pack(Pack<T>{static_cast<const T *>(p), ld, rows, cols, copy, ldd, rows, int(ldd), nullptr, 0, 0}, false, s);
+  const int64_t ldd = round_up(cols, kChunk<T>);
+  T *copy = ws.take<T>(rows * ldd);
+  out = Matrix<T>{copy, ldd};
+  return dry ? hipSuccess : pack<T>(p, ld, rows, cols, nullptr, copy, ldd, s);
 }
 
 template <typename T, typename L, typename R, typename Epilogue>
@@ -693,8 +815,7 @@ hipError_t product(int64_t m, int64_t n, int64_t k, int splits, const L &left, c
   Grid g;
   g.mtiles = int(ceil_div(m, kTile));
   g.ntiles = int(ceil_div(n, kTile));
-  g.chunks = int(ceil_div(k, chunk_elems<T>()));
-  g.steps = (g.chunks + 7) / 8;
+  g.steps = int(ceil_div(k, kStep<T>));
   g.split = int(ceil_div(g.steps, splits));
   const dim3 grid(unsigned(round_up(int64_t(g.mtiles) * g.ntiles, 8)), 1, unsigned(splits));
   auto kernel = k_product<T, kTile, kTile, 2, 2, L, R, Epilogue>;
@@ -708,7 +829,7 @@ hipError_t product(int64_t m, int64_t n, int64_t k, int splits, const L &left, c
 template <typename T>
 int splits_for(int64_t m, int64_t n, int64_t k) {
   const int64_t tiles = ceil_div(m, kTile) * ceil_div(n, kTile);
-  const int64_t steps = ceil_div(k, 8 * chunk_elems<T>());
+  const int64_t steps = ceil_div(k, kStep<T>);
   int64_t want = ceil_div(512, tiles);
   if (want > steps / 8) want = steps / 8;
   return int(want < 1 ? 1 : want > 64 ? 64 : want);
@@ -737,12 +858,21 @@ hipError_t zero(T *p, int64_t n, hipStream_t s) {
 // The places of w_gate's and w_value's rows among the pair's, padding included.
 int64_t pair_cols(int hidden) { return 2 * round_up(hidden, 64); }
 
+// Both weights as the products read them, with one row stride if `same` (they
+// are copied for that where they have two).
 template <typename T>
-hipError_t pair_operands(const lda_gated_args &a, Arena &ws, bool dry, hipStream_t s, PairRows<T> &out) {
-  Rows<T> g, v;
-  OPS_TRY(operand<T>(a.w_gate, a.ld_gate, a.hidden, a.width, ws, dry, s, g));
-  OPS_TRY(operand<T>(a.w_value, a.ld_value, a.hidden, a.width, ws, dry, s, v));
-  out = PairRows<T>{g.p, v.p, g.ld, v.ld, a.hidden};
+hipError_t pair_operands(const lda_gated_args &a, bool same, Arena &ws, bool dry, hipStream_t s, Matrix<T> &gate,
+                         Matrix<T> &value) {
+  OPS_TRY(operand<T>(a.w_gate, a.ld_gate, a.hidden, a.width, ws, dry, s, gate));
+  OPS_TRY(operand<T>(a.w_value, a.ld_value, a.hidden, a.width, ws, dry, s, value));
+  if (!same || gate.ld == value.ld) return hipSuccess;
+  const int64_t ldd = round_up(a.width, kChunk<T>);
+  for (Matrix<T> *m : {&gate, &value}) {
+    if (m->ld == ldd) continue;
+    T *copy = ws.take<T>(a.hidden * ldd);
+    if (!dry) OPS_TRY(pack<T>(m->p, m->ld, a.hidden, a.width, nullptr, copy, ldd, s));
+    *m = Matrix<T>{copy, ldd};
+  }
   return hipSuccess;
 }
 
@@ -750,13 +880,14 @@ template <typename T>
 hipError_t gated_forward_t(const lda_gated_args &a, Arena &ws, bool dry) {
   if (a.rows == 0) return hipSuccess;
   const hipStream_t s = static_cast<hipStream_t>(a.stream);
-  Rows<T> x;
-  PairRows<T> w;
-  OPS_TRY(operand<T>(a.x, a.ldx, int(a.rows), a.width, ws, dry, s, x));
-  OPS_TRY(pair_operands<T>(a, ws, dry, s, w));
+  const int rows = int(a.rows), k = int(round_up(a.width, kChunk<T>));
+  Matrix<T> x, gate, value;
+  OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
+  OPS_TRY(pair_operands<T>(a, false, ws, dry, s, gate, value));
   if (dry) return hipSuccess;
-  const GatedForward<T> epi{static_cast<T *>(a.h), a.ldh, int(a.rows), a.hidden, a.act, whole4<T>(a.h, a.ldh)};
-  return product<T>(a.rows, pair_cols(a.hidden), a.width, 1, x, w, epi, s);
+  const GatedForward<T> epi{static_cast<T *>(a.h), a.ldh, rows, a.hidden, a.act, whole4<T>(a.h, a.ldh)};
+  return product<T>(a.rows, pair_cols(a.hidden), k, 1, Rows<T>{x.p, x.ld, rows, k},
+                    PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s);
 }
 
 template <typename T>
@@ -768,48 +899,38 @@ hipError_t gated_backward_t(const lda_gated_args &a, Arena &ws, bool dry) {
     OPS_TRY(zero(dwg, int64_t(a.hidden) * a.width, s));
     return zero(dwv, int64_t(a.hidden) * a.width, s);
   }
-  const int rows = int(a.rows), pc = int(pair_cols(a.hidden));
-  const int64_t rows_k = round_up(a.rows, chunk_elems<T>());
-  Rows<T> x;
-  PairRows<T> w;
-  OPS_TRY(operand<T>(a.x, a.ldx, rows, a.width, ws, dry, s, x));
-  OPS_TRY(pair_operands<T>(a, ws, dry, s, w));
+  const int rows = int(a.rows), pc = int(pair_cols(a.hidden)), k = int(round_up(a.width, kChunk<T>));
+  Matrix<T> x, gate, value;
+  OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
+  OPS_TRY(pair_operands<T>(a, true, ws, dry, s, gate, value));
   T *dab = ws.take<T>(a.rows * pc);
-  T *dab_t = ws.take<T>(int64_t(pc) * rows_k);
-  T *x_t = ws.take<T>(int64_t(a.width) * rows_k);
-  T *w_t = ws.take<T>(int64_t(a.width) * pc);
   if (!dry) {
     const GatedBackward<T> epi{static_cast<const T *>(a.dh), a.lddh, dab, rows, a.hidden, pc, a.act,
                                whole4<T>(a.dh, a.lddh)};
-    OPS_TRY(product<T>(a.rows, pc, a.width, 1, x, w, epi, s));
-    OPS_TRY(pack(Pack<T>{dab, pc, rows, pc, dab_t, rows_k, pc, int(rows_k), nullptr, 0, 0}, true, s));
-    OPS_TRY(pack(Pack<T>{static_cast<const T *>(a.x), a.ldx, rows, a.width, x_t, rows_k, a.width, int(rows_k), nullptr,
-                         0, 0}, true, s));
-    OPS_TRY(pack(Pack<T>{static_cast<const T *>(a.w_gate), a.ld_gate, a.hidden, a.width, w_t, pc, a.width, pc, nullptr,
-                         0, 1}, true, s));
-    OPS_TRY(pack(Pack<T>{static_cast<const T *>(a.w_value), a.ld_value, a.hidden, a.width, w_t, pc, a.width, pc,
-                         nullptr, 0, 2}, true, s));
+    OPS_TRY(product<T>(a.rows, pc, k, 1, Rows<T>{x.p, x.ld, rows, k},
+                       PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s));
   }
-  const Target<T> dx{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, whole4<T>(a.dx, a.lddx), nullptr};
-  OPS_TRY(product_into<T>(a.rows, a.width, pc, Rows<T>{dab, pc, rows}, Rows<T>{w_t, pc, a.width}, dx, ws, dry, s));
-  const Target<T> dw{dwg, dwv, a.width, a.hidden, true, whole4<T>(dwg, a.width) && whole4<T>(dwv, a.width), nullptr};
-  return product_into<T>(pc, a.width, a.rows, Rows<T>{dab_t, rows_k, pc}, Rows<T>{x_t, rows_k, a.width}, dw, ws, dry,
-                         s);
+  const Target<T> dx{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, whole4<T>(a.dx, a.lddx), nullptr, 0};
+  OPS_TRY(product_into<T>(a.rows, a.width, pc, Rows<T>{dab, pc, rows, pc},
+                          PairColumns<T>{gate.p, value.p, gate.ld, a.width, a.hidden}, dx, ws, dry, s));
+  const Target<T> dw{dwg, dwv, a.width, a.hidden, true, whole4<T>(dwg, a.width) && whole4<T>(dwv, a.width), nullptr, 0};
+  return product_into<T>(pc, a.width, a.rows, Columns<T>{dab, pc, pc, rows}, Columns<T>{x.p, x.ld, a.width, rows}, dw,
+                         ws, dry, s);
 }
 
 template <typename T>
 hipError_t xent_forward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   if (a.rows == 0) return hipSuccess;
   const hipStream_t s = static_cast<hipStream_t>(a.stream);
-  const int rows = int(a.rows), ntiles = int(ceil_div(a.vocab, kTile));
-  Rows<T> x, w;
-  OPS_TRY(operand<T>(a.x, a.ldx, rows, a.width, ws, dry, s, x));
+  const int rows = int(a.rows), ntiles = int(ceil_div(a.vocab, kTile)), k = int(round_up(a.width, kChunk<T>));
+  Matrix<T> x, w;
+  OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
   OPS_TRY(operand<T>(a.weight, a.ld_weight, a.vocab, a.width, ws, dry, s, w));
   float2 *part = ws.take<float2>(int64_t(ntiles) * rows);
   float *label_logit = ws.take<float>(rows);
   if (dry) return hipSuccess;
   const SoftmaxPart<kTile, 2> epi{a.bias, a.labels, label_logit, part, rows, a.vocab};
-  OPS_TRY(product<T>(a.rows, a.vocab, a.width, 1, x, w, epi, s));
+  OPS_TRY(product<T>(a.rows, a.vocab, k, 1, Rows<T>{x.p, x.ld, rows, k}, Rows<T>{w.p, w.ld, a.vocab, k}, epi, s));
   k_lse_join<<<unsigned(ceil_div(rows, 16)), 256, 0, s>>>(part, ntiles, label_logit, a.labels, rows, a.vocab, a.loss,
                                                           a.lse);
   return hipGetLastError();
@@ -832,60 +953,51 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
     OPS_TRY(zero(dw, int64_t(a.vocab) * a.width, s));
     return a.dbias ? zero(a.dbias, a.vocab, s) : hipSuccess;
   }
-  const int rows = int(a.rows), piece = piece_words<T>(a.rows, a.vocab);
-  const int64_t rows_k = round_up(a.rows, chunk_elems<T>());
+  const int rows = int(a.rows), piece = piece_words<T>(a.rows, a.vocab), k = int(round_up(a.width, kChunk<T>));
   const int mtiles = int(ceil_div(a.rows, kTile));
-  Rows<T> x, w;
-  OPS_TRY(operand<T>(a.x, a.ldx, rows, a.width, ws, dry, s, x));
+  Matrix<T> x, w;
+  OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
   OPS_TRY(operand<T>(a.weight, a.ld_weight, a.vocab, a.width, ws, dry, s, w));
-  float *scale = ws.take<float>(2);
+  float *top = ws.take<float>(1), *row_factor = ws.take<float>(rows), *x_factor = ws.take<float>(rows);
+  T *x_scaled = ws.take<T>(a.rows * k);
   T *grad = ws.take<T>(a.rows * piece);
-  T *grad_t = ws.take<T>(int64_t(piece) * rows_k);
-  T *x_t = ws.take<T>(int64_t(a.width) * rows_k);
-  T *w_t = ws.take<T>(int64_t(a.width) * piece);
   float *col_part = a.bias ? ws.take<float>(int64_t(mtiles) * piece) : nullptr;
   const int splits = splits_for<T>(a.rows, a.width, piece);
   const int64_t cols4 = round_up(a.width, 4);
   float *dx_part = ws.take<float>(splits * a.rows * cols4);
   if (!dry) {
-    // half precision: G up to 2^14, so that small probabilities are not lost
-    // below its smallest normal value
-    k_grad_scale<<<1, 1024, 0, s>>>(a.dloss, a.labels, rows, a.vocab, sizeof(T) == 2 ? 16384.0f : 1.0f, scale);
+    k_grad_factors<<<1, 1024, 0, s>>>(a.dloss, a.lse, a.labels, rows, a.vocab, kGradUnit<T>, top, row_factor, x_factor);
     OPS_TRY(hipGetLastError());
-    OPS_TRY(pack(Pack<T>{static_cast<const T *>(a.x), a.ldx, rows, a.width, x_t, rows_k, a.width, int(rows_k),
-                         a.labels, a.vocab, 0}, true, s));
+    OPS_TRY(pack<T>(a.x, a.ldx, a.rows, a.width, x_factor, x_scaled, k, s));
   }
   // the pieces' products share the scratch of their parts
   const size_t mark = ws.used;
   size_t most = mark;
   for (int first = 0; first < a.vocab; first += piece) {
     const int words = a.vocab - first < piece ? a.vocab - first : piece;
-    const int words_k = int(round_up(words, chunk_elems<T>()));
-    const Rows<T> wp{w.p + int64_t(first) * w.ld, w.ld, words};
+    const int words_k = int(round_up(words, kChunk<T>));
+    const T *wp = w.p + int64_t(first) * w.ld;
     ws.used = mark;
     if (!dry) {
-      const SoftmaxGrad<T, kTile, 2> epi{a.bias, a.labels, a.lse, a.dloss, scale, grad, words_k, col_part, rows, a.vocab,
+      const SoftmaxGrad<T, kTile, 2> epi{a.bias, a.labels, a.lse, row_factor, grad, words_k, col_part, rows, a.vocab,
                                          first, words};
-      OPS_TRY(product<T>(a.rows, words_k, a.width, 1, x, wp, epi, s));
+      OPS_TRY(product<T>(a.rows, words_k, k, 1, Rows<T>{x.p, x.ld, rows, k}, Rows<T>{wp, w.ld, words, k}, epi, s));
       if (a.dbias) {
-        k_sum_parts<<<unsigned(ceil_div(words, 256)), 256, 0, s>>>(col_part, mtiles, words, scale + 1,
-                                                                   a.dbias + first);
+        k_sum_parts<<<unsigned(ceil_div(words, 256)), 256, 0, s>>>(col_part, mtiles, words, a.dbias + first);
         OPS_TRY(hipGetLastError());
       }
-      OPS_TRY(pack(Pack<T>{grad, words_k, rows, words, grad_t, rows_k, words, int(rows_k), nullptr, 0, 0}, true, s));
-      OPS_TRY(pack(Pack<T>{wp.p, wp.ld, words, a.width, w_t, words_k, a.width, words_k, nullptr, 0, 0}, true, s));
-      OPS_TRY(product<T>(a.rows, a.width, words_k, splits, Rows<T>{grad, words_k, rows}, Rows<T>{w_t, words_k, a.width},
-                         StorePart{dx_part, rows, int(cols4), first > 0}, s));
+      OPS_TRY(product<T>(a.rows, a.width, words, splits, Rows<T>{grad, words_k, rows, words_k},
+                         Columns<T>{wp, w.ld, a.width, words}, StorePart{dx_part, rows, int(cols4), first > 0}, s));
     }
     T *dwp = dw + int64_t(first) * a.width;
-    const Target<T> out{dwp, nullptr, a.width, words, false, whole4<T>(dwp, a.width), scale + 1};
-    OPS_TRY(product_into<T>(words, a.width, a.rows, Rows<T>{grad_t, rows_k, words}, Rows<T>{x_t, rows_k, a.width}, out,
-                            ws, dry, s));
+    const Target<T> out{dwp, nullptr, a.width, words, false, whole4<T>(dwp, a.width), top, 0};
+    OPS_TRY(product_into<T>(words, a.width, a.rows, Columns<T>{grad, words_k, words, rows},
+                            Columns<T>{x_scaled, k, a.width, rows}, out, ws, dry, s));
     if (ws.used > most) most = ws.used;
   }
   ws.used = most;
   if (dry) return hipSuccess;
-  const Target<T> out{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, whole4<T>(a.dx, a.lddx), scale + 1};
+  const Target<T> out{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, whole4<T>(a.dx, a.lddx), row_factor, 1};
   k_join<T><<<strided(ceil_div(a.rows * cols4, 1024)), 256, 0, s>>>(dx_part, splits, rows, a.width, int(cols4), out);
   return hipGetLastError();
 }
