@@ -54,19 +54,20 @@ __device__ inline f32x4 mma<float>(u32x4 r, u32x4 l, f32x4 c) {
   return c;
 }
 
-// Operands.  A step of the product takes 128 bytes of k of every row (kStep
+// Operands.  A step of the product takes 64 bytes of k of every row (kStep
 // elements), in 16-byte chunks (kChunk elements).  An operand lies in memory
 // either with k contiguous ("rows") or with its rows contiguous ("columns":
 // the transposed matrix, element (row, k) at p[k * ld + row]); neither is
 // copied for the other, LDS is read transposed.  `base` gives the address of
-// the chunk that a lane loads in step 0, `in` whether its chunk of a later
+// the chunk that a lane loads in step 0, `ahead` how far on it lies in a later
+// step, `in` whether its chunk of a later
 // step lies inside k; steps before `full` need no check.  Rows past the end
 // repeat the last one (or chunk): their products go nowhere, and no read
 // leaves the matrix.
 template <typename T>
 constexpr int kChunk = 16 / int(sizeof(T));
 template <typename T>
-constexpr int kStep = 128 / int(sizeof(T));
+constexpr int kStep = 64 / int(sizeof(T));
 
 template <typename T>
 struct Rows {
@@ -75,7 +76,7 @@ struct Rows {
   int64_t ld;
   int rows, k;
   __device__ int full() const { return k / kStep<T>; }
-  __device__ int64_t stride() const { return 128; }
+  __device__ int64_t ahead(int step) const { return int64_t(step) * 64; }
   __device__ const char *base(int row, int k0) const {
     return reinterpret_cast<const char *>(p + int64_t(min(row, rows - 1)) * ld + k0);
   }
@@ -89,7 +90,7 @@ struct Columns {
   int64_t ld;
   int rows, k;
   __device__ int full() const { return k / kStep<T>; }
-  __device__ int64_t stride() const { return 128 * ld; }
+  __device__ int64_t ahead(int step) const { return step * 64 * ld; }
   __device__ const char *base(int row, int k0) const {
     return reinterpret_cast<const char *>(p + int64_t(k0) * ld + min(row, (rows - 1) / kChunk<T> * kChunk<T>));
   }
@@ -108,7 +109,7 @@ struct PairRows {
   int64_t ld_gate, ld_value;
   int hidden, k;
   __device__ int full() const { return k / kStep<T>; }
-  __device__ int64_t stride() const { return 128; }
+  __device__ int64_t ahead(int step) const { return int64_t(step) * 64; }
   __device__ const char *base(int n, int k0) const {
     const int64_t f = min(pair_row(n), hidden - 1);
     return reinterpret_cast<const char *>((n & 16 ? value + f * ld_value : gate + f * ld_gate) + k0);
@@ -123,8 +124,13 @@ struct PairColumns {
   const T *gate, *value;
   int64_t ld;  // of both
   int width, hidden;
-  __device__ int full() const { return 2 * hidden / kStep<T>; }
-  __device__ int64_t stride() const { return 64 * ld; }
+  __device__ int full() const { return hidden / 16 * (32 / kStep<T>); }
+  // a step is one turn of the pair in 16-bit types, half of one in 32 bits
+  __device__ int64_t ahead(int step) const {
+    if (sizeof(T) == 2) return step * 32 * ld;
+    const int64_t other = reinterpret_cast<const char *>(value) - reinterpret_cast<const char *>(gate);
+    return (step >> 1) * 64 * ld + (step & 1 ? other : 0);
+  }
   __device__ const char *base(int row, int k0) const {
     return reinterpret_cast<const char *>((k0 & 16 ? value : gate) + int64_t(pair_row(k0)) * ld +
                                           min(row, (width - 1) / kChunk<T> * kChunk<T>));
@@ -170,11 +176,11 @@ __device__ inline bool tile_of(const Grid &g, int &mt, int &nt) {
   return true;
 }
 
-// An operand's part of a stage in LDS, B rows: B/8 loads of 1 KiB, dealt to the
+// An operand's part of a stage in LDS, B rows: B/16 loads of 1 KiB, dealt to the
 // waves in turns.
 //
-// k contiguous: 128 bytes a row; chunk c of row r lies at place c ^ (r & 7), so
-// that the 16 rows that a fragment read touches spread over the banks.
+// k contiguous: 64 bytes a row; chunk c of row r lies at place c ^ (r / 2 & 3),
+// so that the 16 rows that a fragment read touches spread over the banks.
 //
 // Rows contiguous: kStep lines of B elements, in slots of 16 rows.  Four
 // 16-bit lines of a slot are what one transposing read of 16 lanes takes
@@ -182,14 +188,16 @@ __device__ inline bool tile_of(const Grid &g, int &mt, int &nt) {
 // the four lines), in single precision a line's slot is one read.  The slots
 // of a line are permuted by the line's number so that lines read together
 // spread over the banks.
-template <typename T>
+__device__ inline int chunk_turn(int row) { return (row >> 1) & 3; }
+template <typename T, int B>
 __device__ inline int slot_turn(int line) {
-  return sizeof(T) == 2 ? (line & 3) | ((line >> 1) & 4) : (line >> 2) & 3;
+  return (sizeof(T) == 2 ? (line & 3) | ((line >> 1) & 4) : (line >> 2) & 3) & (B / 16 - 1);
 }
 
 template <typename T, int B, int WAVES, typename Op>
 struct Stage {
-  static constexpr int LOADS = B / 8 / WAVES;
+  static constexpr int LOADS = B / 16 / WAVES;
+  static_assert(LOADS >= 1 && B % (16 * WAVES) == 0, "every wave loads the same number of times");
   static constexpr int LINE = B * int(sizeof(T));  // bytes, rows contiguous
   const char *src[LOADS];
   int k0[LOADS];  // of the lane's chunk in a step (k contiguous: the same in every load)
@@ -199,19 +207,20 @@ struct Stage {
     for (int i = 0; i < LOADS; ++i) {
       const int load = i * WAVES + wave;
       if (Op::kContiguous) {
-        k0[i] = ((lane & 7) ^ (lane >> 3)) * kChunk<T>;
-        src[i] = op.base(row0 + load * 8 + (lane >> 3), k0[i]);
+        const int row = load * 16 + (lane >> 2);
+        k0[i] = ((lane & 3) ^ chunk_turn(row)) * kChunk<T>;
+        src[i] = op.base(row0 + row, k0[i]);
       } else {
         const int at = load * 1024 + lane * 16, line = at / LINE, part = at % LINE / 16;
         constexpr int per_slot = int(sizeof(T));  // 16-byte parts of 16 elements
-        const int slot = (part / per_slot) ^ slot_turn<T>(line);
+        const int slot = (part / per_slot) ^ slot_turn<T, B>(line);
         k0[i] = line;
         src[i] = op.base(row0 + slot * 16 + part % per_slot * kChunk<T>, line);
       }
     }
   }
   __device__ void load(const Op &op, int step, char *to, int wave) const {
-    const int64_t ahead = step * op.stride();
+    const int64_t ahead = op.ahead(step);
     if (step < op.full()) {
 #pragma unroll
       for (int i = 0; i < LOADS; ++i)
@@ -225,24 +234,23 @@ struct Stage {
       }
     }
   }
-  // The fragment of rows row0..row0+15 (of the tile), half s of the step.
-  static __device__ u32x4 fragment(const char *tile, int row0, int s, int lane) {
+  // The fragment of rows row0..row0+15 (of the tile).
+  static __device__ u32x4 fragment(const char *tile, int row0, int lane) {
     const int q = lane & 15, group = lane >> 4;
-    if (Op::kContiguous) {
-      const int place = (s * 4 + group) ^ (q & 7);
-      return *reinterpret_cast<const u32x4 *>(tile + (row0 + q) * 128 + place * 16);
-    }
+    if (Op::kContiguous)
+      return *reinterpret_cast<const u32x4 *>(tile + (row0 + q) * 64 + (group ^ chunk_turn(q)) * 16);
     if (sizeof(T) == 2) {
-      const int line = s * 32 + group * 8 + (q >> 2);
-      const char *p = tile + line * LINE + (((row0 >> 4) ^ slot_turn<T>(line)) * 32) + (q & 3) * 8;
+      const int line = group * 8 + (q >> 2);
+      const char *p = tile + line * LINE + (((row0 >> 4) ^ slot_turn<T, B>(line)) * 32) + (q & 3) * 8;
       const u32x2 lo = transposed(p), hi = transposed(p + 4 * LINE);
       return u32x4{lo[0], lo[1], hi[0], hi[1]};
     }
     u32x4 v;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int line = (s * 4 + group) * 4 + e;
-      v[e] = *reinterpret_cast<const uint32_t *>(tile + line * LINE + (((row0 >> 4) ^ slot_turn<T>(line)) * 64) + q * 4);
+      const int line = group * 4 + e;
+      v[e] = *reinterpret_cast<const uint32_t *>(tile + line * LINE + (((row0 >> 4) ^ slot_turn<T, B>(line)) * 64) +
+                                                 q * 4);
     }
     return v;
   }
@@ -252,12 +260,21 @@ struct Stage {
   }
 };
 
-// C tile of BM x BN by WM x WN waves: two stages in LDS, the next step's loads
-// (straight into LDS) in flight while this step's fragments are multiplied.
+// The last step's barrier, and one with the loads of the step after next still
+// in flight.
+template <int LOADS>
+__device__ inline void stage_barrier(bool more) {
+  if (more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+  else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// C tile of BM x BN by WM x WN waves, three stages in LDS: while a step's
+// fragments are multiplied, the loads of the next two steps (straight into
+// LDS) are in flight.
 template <typename T, int BM, int BN, int WM, int WN, typename L, typename R, typename Epilogue>
-__global__ __launch_bounds__(64 * WM *WN) void k_product(Grid g, L left, R right, Epilogue epilogue) {
+__global__ __launch_bounds__(64 * WM *WN, 2) void k_product(Grid g, L left, R right, Epilogue epilogue) {
   constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16, WAVES = WM * WN;
-  constexpr int STAGE = (BM + BN) * 128;
+  constexpr int STAGE = (BM + BN) * 64;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   int mt, nt;
   if (!tile_of(g, mt, nt)) return;
@@ -265,13 +282,14 @@ __global__ __launch_bounds__(64 * WM *WN) void k_product(Grid g, L left, R right
   const int wm = wave / WN, wn = wave % WN;
   typedef Stage<T, BM, WAVES, L> StageL;
   typedef Stage<T, BN, WAVES, R> StageR;
+  constexpr int LOADS = StageL::LOADS + StageR::LOADS;
   const StageL from_l(left, mt * BM, wave, lane);
   const StageR from_r(right, nt * BN, wave, lane);
   const int begin = int(blockIdx.z) * g.split, end = min(g.steps, begin + g.split);
 
-  auto load = [&](int step, int stage) {
-    from_l.load(left, step, lds + stage * STAGE, wave);
-    from_r.load(right, step, lds + stage * STAGE + BM * 128, wave);
+  auto load = [&](int step, char *stage) {
+    from_l.load(left, step, stage, wave);
+    from_r.load(right, step, stage + BM * 64, wave);
   };
 
   f32x4 acc[MI][NI];
@@ -280,28 +298,28 @@ __global__ __launch_bounds__(64 * WM *WN) void k_product(Grid g, L left, R right
 #pragma unroll
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
 
-  if (begin < end) load(begin, 0);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
+  // the stages of this step, the next and the one after
+  char *now = lds, *next = lds + STAGE, *after = lds + 2 * STAGE;
+  if (begin < end) load(begin, now);
+  if (begin + 1 < end) load(begin + 1, next);
+  stage_barrier<LOADS>(begin + 1 < end);
   for (int step = begin; step < end; ++step) {
-    const int stage = (step - begin) & 1;
-    if (step + 1 < end) load(step + 1, stage ^ 1);
-    const char *tl = lds + stage * STAGE, *tr = tl + BM * 128;
+    if (step + 2 < end) load(step + 2, after);
+    u32x4 fl[MI], fr[NI];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      u32x4 fl[MI], fr[NI];
+    for (int i = 0; i < MI; ++i) fl[i] = StageL::fragment(now, wm * TM + i * 16, lane);
 #pragma unroll
-      for (int i = 0; i < MI; ++i) fl[i] = StageL::fragment(tl, wm * TM + i * 16, s, lane);
+    for (int j = 0; j < NI; ++j) fr[j] = StageR::fragment(now + BM * 64, wn * TN + j * 16, lane);
 #pragma unroll
-      for (int j = 0; j < NI; ++j) fr[j] = StageR::fragment(tr, wn * TN + j * 16, s, lane);
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NI; ++j) acc[i][j] = mma<T>(fr[j], fl[i], acc[i][j]);
-    }
+      for (int j = 0; j < NI; ++j) acc[i][j] = mma<T>(fr[j], fl[i], acc[i][j]);
     // the next step's loads have landed, and every wave is done with this one
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+    stage_barrier<LOADS>(step + 2 < end);
+    char *done = now;
+    now = next;
+    next = after;
+    after = done;
   }
   epilogue(Place{mt * BM + wm * TM, nt * BN + wn * TN, mt, nt, wm, wn, lane, int(blockIdx.z), lds}, acc);
 }
@@ -758,8 +776,6 @@ __global__ __launch_bounds__(256) void k_pack(const T *src, int64_t ld, int64_t 
 }
 
 // ------------------------------------------------------------------- host ---
-constexpr int kTile = 128;
-
 // Workgroups of a kernel that strides over its elements.
 unsigned strided(int64_t workgroups) { return unsigned(workgroups < 65536 ? workgroups : 65536); }
 
@@ -809,42 +825,79 @@ hipError_t operand(const void *p, int64_t ld, int64_t rows, int cols, Arena &ws,
   return dry ? hipSuccess : pack<T>(p, ld, rows, cols, nullptr, copy, ldd, s);
 }
 
-template <typename T, typename L, typename R, typename Epilogue>
+// Tiles of a product and the parts its sum over k is split into: large tiles
+// where they fill the device (with the splits: at least 32 steps each), else
+// small ones.  Only a product whose result is stored plainly can be split.
+struct Tiles {
+  bool large = true;
+  int m = 128, n = 256, splits = 1;
+  Tiles(int64_t rows, int64_t cols, int64_t steps = 0) {
+    const int64_t most = steps / 32 < 1 ? 1 : steps / 32 > 64 ? 64 : steps / 32;
+    int64_t tiles = ceil_div(rows, 128) * ceil_div(cols, 256);
+    int64_t want = 512;
+    if (tiles * most < 192) {
+      large = false;
+      m = n = 64;
+      tiles = ceil_div(rows, 64) * ceil_div(cols, 64);
+      want = 768;
+    }
+    want = ceil_div(want, tiles);
+    if (steps) splits = int(want < most ? want : most);
+  }
+};
+
+template <typename T>
+int64_t steps_of(int64_t k) {
+  return ceil_div(k, kStep<T>);
+}
+
+template <int BM_, int BN_>
+struct Shape {
+  static constexpr int BM = BM_, BN = BN_, WM = 2, WN = 2;
+};
+
+// Calls fn with the shape of the tiles.
+template <typename Fn>
+hipError_t with_shape(const Tiles &t, Fn fn) {
+  return t.large ? fn(Shape<128, 256>()) : fn(Shape<64, 64>());
+}
+
+template <typename T, typename S, typename L, typename R, typename Epilogue>
 hipError_t product(int64_t m, int64_t n, int64_t k, int splits, const L &left, const R &right, const Epilogue &epi,
                    hipStream_t s) {
   Grid g;
-  g.mtiles = int(ceil_div(m, kTile));
-  g.ntiles = int(ceil_div(n, kTile));
-  g.steps = int(ceil_div(k, kStep<T>));
+  g.mtiles = int(ceil_div(m, S::BM));
+  g.ntiles = int(ceil_div(n, S::BN));
+  g.steps = int(steps_of<T>(k));
   g.split = int(ceil_div(g.steps, splits));
   const dim3 grid(unsigned(round_up(int64_t(g.mtiles) * g.ntiles, 8)), 1, unsigned(splits));
-  auto kernel = k_product<T, kTile, kTile, 2, 2, L, R, Epilogue>;
-  const size_t lds = 2 * (kTile + kTile) * 128;
-  kernel<<<grid, 256, lds, s>>>(g, left, right, epi);
+  auto kernel = k_product<T, S::BM, S::BN, S::WM, S::WN, L, R, Epilogue>;
+  constexpr size_t lds = 3 * (S::BM + S::BN) * 64;
+  if (lds > 65536) {
+    static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                                          hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+    OPS_TRY(allowed);
+  }
+  kernel<<<grid, 64 * S::WM * S::WN, lds, s>>>(g, left, right, epi);
   return hipGetLastError();
-}
-
-// How many ways the sum over k is split: enough workgroups for the device,
-// each with at least eight steps.
-template <typename T>
-int splits_for(int64_t m, int64_t n, int64_t k) {
-  const int64_t tiles = ceil_div(m, kTile) * ceil_div(n, kTile);
-  const int64_t steps = ceil_div(k, kStep<T>);
-  int64_t want = ceil_div(512, tiles);
-  if (want > steps / 8) want = steps / 8;
-  return int(want < 1 ? 1 : want > 64 ? 64 : want);
 }
 
 // A whole product into `out`, split over k where it has few tiles.
 template <typename T, typename L, typename R>
 hipError_t product_into(int64_t m, int64_t n, int64_t k, const L &left, const R &right, const Target<T> &out, Arena &ws,
                         bool dry, hipStream_t s) {
-  const int splits = splits_for<T>(m, n, k);
+  const Tiles tiles(m, n, steps_of<T>(k));
+  const int splits = tiles.splits;
   const int64_t cols4 = round_up(n, 4);
   float *part = splits > 1 ? ws.take<float>(splits * m * cols4) : nullptr;
   if (dry) return hipSuccess;
-  if (splits == 1) return product<T>(m, n, k, 1, left, right, Store<T>{out, int(n)}, s);
-  OPS_TRY(product<T>(m, n, k, splits, left, right, StorePart{part, int(m), int(cols4), false}, s));
+  if (splits == 1)
+    return with_shape(tiles, [&](auto shape) {
+      return product<T, decltype(shape)>(m, n, k, 1, left, right, Store<T>{out, int(n)}, s);
+    });
+  OPS_TRY(with_shape(tiles, [&](auto shape) {
+    return product<T, decltype(shape)>(m, n, k, splits, left, right, StorePart{part, int(m), int(cols4), false}, s);
+  }));
   k_join<T><<<strided(ceil_div(m * cols4, 1024)), 256, 0, s>>>(part, splits, int(m), int(n), int(cols4), out);
   return hipGetLastError();
 }
@@ -886,8 +939,10 @@ hipError_t gated_forward_t(const lda_gated_args &a, Arena &ws, bool dry) {
   OPS_TRY(pair_operands<T>(a, false, ws, dry, s, gate, value));
   if (dry) return hipSuccess;
   const GatedForward<T> epi{static_cast<T *>(a.h), a.ldh, rows, a.hidden, a.act, whole4<T>(a.h, a.ldh)};
-  return product<T>(a.rows, pair_cols(a.hidden), k, 1, Rows<T>{x.p, x.ld, rows, k},
-                    PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s);
+  return with_shape(Tiles(a.rows, pair_cols(a.hidden)), [&](auto shape) {
+    return product<T, decltype(shape)>(a.rows, pair_cols(a.hidden), k, 1, Rows<T>{x.p, x.ld, rows, k},
+                                       PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s);
+  });
 }
 
 template <typename T>
@@ -907,8 +962,10 @@ hipError_t gated_backward_t(const lda_gated_args &a, Arena &ws, bool dry) {
   if (!dry) {
     const GatedBackward<T> epi{static_cast<const T *>(a.dh), a.lddh, dab, rows, a.hidden, pc, a.act,
                                whole4<T>(a.dh, a.lddh)};
-    OPS_TRY(product<T>(a.rows, pc, k, 1, Rows<T>{x.p, x.ld, rows, k},
-                       PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s));
+    OPS_TRY(with_shape(Tiles(a.rows, pc), [&](auto shape) {
+      return product<T, decltype(shape)>(a.rows, pc, k, 1, Rows<T>{x.p, x.ld, rows, k},
+                                         PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s);
+    }));
   }
   const Target<T> dx{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, whole4<T>(a.dx, a.lddx), nullptr, 0};
   OPS_TRY(product_into<T>(a.rows, a.width, pc, Rows<T>{dab, pc, rows, pc},
@@ -922,15 +979,20 @@ template <typename T>
 hipError_t xent_forward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   if (a.rows == 0) return hipSuccess;
   const hipStream_t s = static_cast<hipStream_t>(a.stream);
-  const int rows = int(a.rows), ntiles = int(ceil_div(a.vocab, kTile)), k = int(round_up(a.width, kChunk<T>));
+  const int rows = int(a.rows), k = int(round_up(a.width, kChunk<T>));
+  const Tiles tiles(a.rows, a.vocab);
+  const int ntiles = int(ceil_div(a.vocab, tiles.n));
   Matrix<T> x, w;
   OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
   OPS_TRY(operand<T>(a.weight, a.ld_weight, a.vocab, a.width, ws, dry, s, w));
   float2 *part = ws.take<float2>(int64_t(ntiles) * rows);
   float *label_logit = ws.take<float>(rows);
   if (dry) return hipSuccess;
-  const SoftmaxPart<kTile, 2> epi{a.bias, a.labels, label_logit, part, rows, a.vocab};
-  OPS_TRY(product<T>(a.rows, a.vocab, k, 1, Rows<T>{x.p, x.ld, rows, k}, Rows<T>{w.p, w.ld, a.vocab, k}, epi, s));
+  OPS_TRY(with_shape(tiles, [&](auto shape) {
+    typedef decltype(shape) S;
+    const SoftmaxPart<S::BM, S::WN> epi{a.bias, a.labels, label_logit, part, rows, a.vocab};
+    return product<T, S>(a.rows, a.vocab, k, 1, Rows<T>{x.p, x.ld, rows, k}, Rows<T>{w.p, w.ld, a.vocab, k}, epi, s);
+  }));
   k_lse_join<<<unsigned(ceil_div(rows, 16)), 256, 0, s>>>(part, ntiles, label_logit, a.labels, rows, a.vocab, a.loss,
                                                           a.lse);
   return hipGetLastError();
@@ -939,8 +1001,8 @@ hipError_t xent_forward_t(const lda_xent_args &a, Arena &ws, bool dry) {
 // Words of one piece: G of a piece takes at most 256 MiB.
 template <typename T>
 int piece_words(int64_t rows, int vocab) {
-  const int64_t most = (int64_t(256) << 20) / (rows * int64_t(sizeof(T))) / kTile * kTile;
-  const int64_t all = round_up(vocab, kTile);
+  const int64_t most = (int64_t(256) << 20) / (rows * int64_t(sizeof(T))) / 256 * 256;
+  const int64_t all = round_up(vocab, 256);
   return int(most < 1024 ? (all < 1024 ? all : 1024) : most < all ? most : all);
 }
 
@@ -954,7 +1016,7 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
     return a.dbias ? zero(a.dbias, a.vocab, s) : hipSuccess;
   }
   const int rows = int(a.rows), piece = piece_words<T>(a.rows, a.vocab), k = int(round_up(a.width, kChunk<T>));
-  const int mtiles = int(ceil_div(a.rows, kTile));
+  const int mtiles = int(ceil_div(a.rows, Tiles(a.rows, piece).m));
   Matrix<T> x, w;
   OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
   OPS_TRY(operand<T>(a.weight, a.ld_weight, a.vocab, a.width, ws, dry, s, w));
@@ -962,7 +1024,8 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   T *x_scaled = ws.take<T>(a.rows * k);
   T *grad = ws.take<T>(a.rows * piece);
   float *col_part = a.bias ? ws.take<float>(int64_t(mtiles) * piece) : nullptr;
-  const int splits = splits_for<T>(a.rows, a.width, piece);
+  const Tiles dx_tiles(a.rows, a.width, steps_of<T>(piece));
+  const int splits = dx_tiles.splits;
   const int64_t cols4 = round_up(a.width, 4);
   float *dx_part = ws.take<float>(splits * a.rows * cols4);
   if (!dry) {
@@ -979,15 +1042,21 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
     const T *wp = w.p + int64_t(first) * w.ld;
     ws.used = mark;
     if (!dry) {
-      const SoftmaxGrad<T, kTile, 2> epi{a.bias, a.labels, a.lse, row_factor, grad, words_k, col_part, rows, a.vocab,
-                                         first, words};
-      OPS_TRY(product<T>(a.rows, words_k, k, 1, Rows<T>{x.p, x.ld, rows, k}, Rows<T>{wp, w.ld, words, k}, epi, s));
+      OPS_TRY(with_shape(Tiles(a.rows, piece), [&](auto shape) {
+        typedef decltype(shape) S;
+        const SoftmaxGrad<T, S::BN, S::WM> epi{a.bias, a.labels, a.lse, row_factor, grad, words_k, col_part, rows,
+                                               a.vocab, first, words};
+        return product<T, S>(a.rows, words_k, k, 1, Rows<T>{x.p, x.ld, rows, k}, Rows<T>{wp, w.ld, words, k}, epi, s);
+      }));
       if (a.dbias) {
         k_sum_parts<<<unsigned(ceil_div(words, 256)), 256, 0, s>>>(col_part, mtiles, words, a.dbias + first);
         OPS_TRY(hipGetLastError());
       }
-      OPS_TRY(product<T>(a.rows, a.width, words, splits, Rows<T>{grad, words_k, rows, words_k},
-                         Columns<T>{wp, w.ld, a.width, words}, StorePart{dx_part, rows, int(cols4), first > 0}, s));
+      OPS_TRY(with_shape(dx_tiles, [&](auto shape) {
+        return product<T, decltype(shape)>(a.rows, a.width, words, splits, Rows<T>{grad, words_k, rows, words_k},
+                                           Columns<T>{wp, w.ld, a.width, words},
+                                           StorePart{dx_part, rows, int(cols4), first > 0}, s);
+      }));
     }
     T *dwp = dw + int64_t(first) * a.width;
     const Target<T> out{dwp, nullptr, a.width, words, false, whole4<T>(dwp, a.width), top, 0};
