@@ -9,6 +9,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "ops_internal.h"
 
 #pragma clang fp contract(fast)
@@ -54,20 +56,20 @@ __device__ inline f32x4 mma<float>(u32x4 r, u32x4 l, f32x4 c) {
   return c;
 }
 
-// Operands.  A step of the product takes 64 bytes of k of every row (kStep
-// elements), in 16-byte chunks (kChunk elements).  An operand lies in memory
+// Operands.  A step of the product takes 128 bytes of k of every row (kStep
+// elements; whole cache lines), in 16-byte chunks (kChunk elements).  An operand lies in memory
 // either with k contiguous ("rows") or with its rows contiguous ("columns":
 // the transposed matrix, element (row, k) at p[k * ld + row]); neither is
 // copied for the other, LDS is read transposed.  `base` gives the address of
 // the chunk that a lane loads in step 0, `ahead` how far on it lies in a later
-// step, `in` whether its chunk of a later
-// step lies inside k; steps before `full` need no check.  Rows past the end
+// step, `in` whether its chunk of a
+// step lies inside k.  Rows past the end
 // repeat the last one (or chunk): their products go nowhere, and no read
 // leaves the matrix.
 template <typename T>
 constexpr int kChunk = 16 / int(sizeof(T));
 template <typename T>
-constexpr int kStep = 64 / int(sizeof(T));
+constexpr int kStep = 128 / int(sizeof(T));
 
 template <typename T>
 struct Rows {
@@ -75,8 +77,7 @@ struct Rows {
   const T *p;
   int64_t ld;
   int rows, k;
-  __device__ int full() const { return k / kStep<T>; }
-  __device__ int64_t ahead(int step) const { return int64_t(step) * 64; }
+  __device__ int64_t ahead(int step) const { return int64_t(step) * 128; }
   __device__ const char *base(int row, int k0) const {
     return reinterpret_cast<const char *>(p + int64_t(min(row, rows - 1)) * ld + k0);
   }
@@ -89,8 +90,7 @@ struct Columns {
   const T *p;
   int64_t ld;
   int rows, k;
-  __device__ int full() const { return k / kStep<T>; }
-  __device__ int64_t ahead(int step) const { return step * 64 * ld; }
+  __device__ int64_t ahead(int step) const { return step * 128 * ld; }
   __device__ const char *base(int row, int k0) const {
     return reinterpret_cast<const char *>(p + int64_t(k0) * ld + min(row, (rows - 1) / kChunk<T> * kChunk<T>));
   }
@@ -108,8 +108,7 @@ struct PairRows {
   const T *gate, *value;
   int64_t ld_gate, ld_value;
   int hidden, k;
-  __device__ int full() const { return k / kStep<T>; }
-  __device__ int64_t ahead(int step) const { return int64_t(step) * 64; }
+  __device__ int64_t ahead(int step) const { return int64_t(step) * 128; }
   __device__ const char *base(int n, int k0) const {
     const int64_t f = min(pair_row(n), hidden - 1);
     return reinterpret_cast<const char *>((n & 16 ? value + f * ld_value : gate + f * ld_gate) + k0);
@@ -124,13 +123,7 @@ struct PairColumns {
   const T *gate, *value;
   int64_t ld;  // of both
   int width, hidden;
-  __device__ int full() const { return hidden / 16 * (32 / kStep<T>); }
-  // a step is one turn of the pair in 16-bit types, half of one in 32 bits
-  __device__ int64_t ahead(int step) const {
-    if (sizeof(T) == 2) return step * 32 * ld;
-    const int64_t other = reinterpret_cast<const char *>(value) - reinterpret_cast<const char *>(gate);
-    return (step >> 1) * 64 * ld + (step & 1 ? other : 0);
-  }
+  __device__ int64_t ahead(int step) const { return step * 64 * ld; }
   __device__ const char *base(int row, int k0) const {
     return reinterpret_cast<const char *>((k0 & 16 ? value : gate) + int64_t(pair_row(k0)) * ld +
                                           min(row, (width - 1) / kChunk<T> * kChunk<T>));
@@ -149,7 +142,7 @@ struct Place {
 
 struct Grid {
   int mtiles, ntiles;
-  int steps, split;  // steps of k in all, and of one split
+  int steps, split, splits;  // steps of k in all, of one split, and the splits (none is empty)
 };
 
 // what a lane whose chunk lies past the end of k reads instead
@@ -159,28 +152,26 @@ typedef const __attribute__((address_space(1))) void *global_ptr;
 typedef __attribute__((address_space(3))) void *lds_ptr;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) uint32_t lds_u32;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // Tile order: the tiles are cut into eight runs, one for each accelerator die
 // (workgroups go to the dies in turn), and a run walks groups of eight tile
 // rows column by column, so that the tiles a die works on at one time share
 // their operands in its L2.
-__device__ inline bool tile_of(const Grid &g, int &mt, int &nt) {
-  const int tiles = g.mtiles * g.ntiles;
-  const int per = (tiles + 7) >> 3;
-  const int t = int(blockIdx.x & 7) * per + int(blockIdx.x >> 3);
-  if (int(blockIdx.x >> 3) >= per || t >= tiles) return false;
+__device__ inline void tile_at(const Grid &g, int t, int &mt, int &nt) {
   const int group = 8 * g.ntiles, first = t / group * 8;
   const int high = min(8, g.mtiles - first), in = t % group;
   mt = first + in % high;
   nt = in / high;
-  return true;
 }
-
-// An operand's part of a stage in LDS, B rows: B/16 loads of 1 KiB, dealt to the
+// An operand's part of a stage in LDS, B rows: B/8 loads of 1 KiB, dealt to the
 // waves in turns.
 //
-// k contiguous: 64 bytes a row; chunk c of row r lies at place c ^ (r / 2 & 3),
-// so that the 16 rows that a fragment read touches spread over the banks.
+// k contiguous: 128 bytes a row; chunk c of row r lies at place c ^ (r & 7), so
+// that the 16 rows that a fragment read touches spread over the banks.
 //
 // Rows contiguous: kStep lines of B elements, in slots of 16 rows.  Four
 // 16-bit lines of a slot are what one transposing read of 16 lanes takes
@@ -188,7 +179,8 @@ __device__ inline bool tile_of(const Grid &g, int &mt, int &nt) {
 // the four lines), in single precision a line's slot is one read.  The slots
 // of a line are permuted by the line's number so that lines read together
 // spread over the banks.
-__device__ inline int chunk_turn(int row) { return (row >> 1) & 3; }
+//
+// Measured: no bank conflicts with either layout.
 template <typename T, int B>
 __device__ inline int slot_turn(int line) {
   return (sizeof(T) == 2 ? (line & 3) | ((line >> 1) & 4) : (line >> 2) & 3) & (B / 16 - 1);
@@ -196,135 +188,231 @@ __device__ inline int slot_turn(int line) {
 
 template <typename T, int B, int WAVES, typename Op>
 struct Stage {
-  static constexpr int LOADS = B / 16 / WAVES;
-  static_assert(LOADS >= 1 && B % (16 * WAVES) == 0, "every wave loads the same number of times");
+  static constexpr int LOADS = B / 8 / WAVES;
+  static_assert(LOADS >= 1 && B % (8 * WAVES) == 0, "every wave loads the same number of times");
   static constexpr int LINE = B * int(sizeof(T));  // bytes, rows contiguous
+  // rows contiguous: lines from one load of a wave to its next
+  static constexpr int NEXT = Op::kContiguous ? 0 : WAVES * 1024 / LINE;
+  static_assert(Op::kContiguous || (WAVES * 1024) % LINE == 0, "a wave's loads are whole lines apart");
   const char *src[LOADS];
-  int k0[LOADS];  // of the lane's chunk in a step (k contiguous: the same in every load)
+  int k0;  // of the lane's chunk in a step, in the first load
 
-  __device__ Stage(const Op &op, int row0, int wave, int lane) {
+  __device__ void aim(const Op &op, int row0, int wave, int lane) {
+    if (Op::kContiguous) {
+      k0 = ((lane & 7) ^ (lane >> 3)) * kChunk<T>;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int load = i * WAVES + wave;
-      if (Op::kContiguous) {
-        const int row = load * 16 + (lane >> 2);
-        k0[i] = ((lane & 3) ^ chunk_turn(row)) * kChunk<T>;
-        src[i] = op.base(row0 + row, k0[i]);
-      } else {
-        const int at = load * 1024 + lane * 16, line = at / LINE, part = at % LINE / 16;
-        constexpr int per_slot = int(sizeof(T));  // 16-byte parts of 16 elements
-        const int slot = (part / per_slot) ^ slot_turn<T, B>(line);
-        k0[i] = line;
+      for (int i = 0; i < LOADS; ++i) src[i] = op.base(row0 + (i * WAVES + wave) * 8 + (lane >> 3), k0);
+    } else {
+      k0 = (wave * 1024 + lane * 16) / LINE;
+      const int part = (wave * 1024 + lane * 16) % LINE / 16;
+      constexpr int per_slot = int(sizeof(T));  // 16-byte parts of 16 elements
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int line = k0 + i * NEXT, slot = (part / per_slot) ^ slot_turn<T, B>(line);
         src[i] = op.base(row0 + slot * 16 + part % per_slot * kChunk<T>, line);
       }
     }
   }
-  __device__ void load(const Op &op, int step, char *to, int wave) const {
+  __device__ void load(const Op &op, int step, lds_char *to, int wave) const {
     const int64_t ahead = op.ahead(step);
-    if (step < op.full()) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i)
-        __builtin_amdgcn_global_load_lds((global_ptr)(src[i] + ahead), (lds_ptr)(to + (i * WAVES + wave) * 1024), 16, 0,
-                                         0);
-    } else {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const char *p = op.in(step, k0[i]) ? src[i] + ahead : reinterpret_cast<const char *>(&kZeroChunk);
-        __builtin_amdgcn_global_load_lds((global_ptr)p, (lds_ptr)(to + (i * WAVES + wave) * 1024), 16, 0, 0);
-      }
+    for (int i = 0; i < LOADS; ++i) {
+      const char *p = op.in(step, k0 + i * NEXT) ? src[i] + ahead : reinterpret_cast<const char *>(&kZeroChunk);
+      __builtin_amdgcn_global_load_lds((global_ptr)p, (lds_ptr)(to + (i * WAVES + wave) * 1024), 16, 0, 0);
     }
   }
-  // The fragment of rows row0..row0+15 (of the tile).
-  static __device__ u32x4 fragment(const char *tile, int row0, int lane) {
+  // The fragment of rows row0..row0+15 (of the tile), half s of the step.
+  static __device__ u32x4 fragment(const lds_char *tile, int row0, int s, int lane) {
     const int q = lane & 15, group = lane >> 4;
     if (Op::kContiguous)
-      return *reinterpret_cast<const u32x4 *>(tile + (row0 + q) * 64 + (group ^ chunk_turn(q)) * 16);
+      return *(const lds_u32x4 *)(tile + (row0 + q) * 128 + ((s * 4 + group) ^ (q & 7)) * 16);
     if (sizeof(T) == 2) {
-      const int line = group * 8 + (q >> 2);
-      const char *p = tile + line * LINE + (((row0 >> 4) ^ slot_turn<T, B>(line)) * 32) + (q & 3) * 8;
+      const int line = s * 32 + group * 8 + (q >> 2);
+      const lds_char *p = tile + line * LINE + (((row0 >> 4) ^ slot_turn<T, B>(line)) * 32) + (q & 3) * 8;
       const u32x2 lo = transposed(p), hi = transposed(p + 4 * LINE);
       return u32x4{lo[0], lo[1], hi[0], hi[1]};
     }
     u32x4 v;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int line = group * 4 + e;
-      v[e] = *reinterpret_cast<const uint32_t *>(tile + line * LINE + (((row0 >> 4) ^ slot_turn<T, B>(line)) * 64) +
-                                                 q * 4);
+      const int line = (s * 4 + group) * 4 + e;
+      v[e] = *(const lds_u32 *)(tile + line * LINE + (((row0 >> 4) ^ slot_turn<T, B>(line)) * 64) + q * 4);
     }
     return v;
   }
-  static __device__ u32x2 transposed(const char *p) {
-    return __builtin_bit_cast(
-        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p));
+  static __device__ u32x2 transposed(const lds_char *p) {
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
   }
 };
 
-// The last step's barrier, and one with the loads of the step after next still
-// in flight.
-template <int LOADS>
-__device__ inline void stage_barrier(bool more) {
-  if (more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
-  else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+// Tells the compiler that a row of accumulators is in the matrix unit's
+// registers here.  Without it, it keeps some of 256 in others and moves them
+// back and forth in the loop over k.
+template <int NI>
+__device__ inline void keep_accumulators(f32x4 (&row)[NI]) {
+  if constexpr (NI == 8) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) asm volatile("" : "+a"(row[j]));
+  }
 }
 
-// C tile of BM x BN by WM x WN waves, three stages in LDS: while a step's
-// fragments are multiplied, the loads of the next two steps (straight into
-// LDS) are in flight.
+// C tiles of BM x BN by WM x WN waves, on a grid that stays on the device and
+// walks through the tiles.  Two stages in LDS and two sets of fragments: while
+// the first half of a step is multiplied, its second half is read; then the
+// next step has landed and this one's stage is free, and while the second half
+// is multiplied, the step after next is loaded into it and the first half of
+// the next step is read.  The loads run over the ends of tiles, so that a
+// tile's first step is there when the epilogue of the tile before is done.
+//
+// `fill` and `data` are both the stages in LDS: between two barriers the stage
+// that is filled is not the one that is read, and as restricted pointers they
+// let the compiler see that (else it waits for the loads before it reads).
 template <typename T, int BM, int BN, int WM, int WN, typename L, typename R, typename Epilogue>
-__global__ __launch_bounds__(64 * WM *WN, 2) void k_product(Grid g, L left, R right, Epilogue epilogue) {
+__device__ __attribute__((always_inline)) inline void walk_tiles(const Grid &g, const L &left, const R &right,
+                                                                 const Epilogue &epilogue, lds_char *__restrict fill,
+                                                                 const lds_char *__restrict data, char *scratch) {
   constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16, WAVES = WM * WN;
-  constexpr int STAGE = (BM + BN) * 64;
-  extern __shared__ __attribute__((aligned(1024))) char lds[];
-  int mt, nt;
-  if (!tile_of(g, mt, nt)) return;
+  constexpr int STAGE = (BM + BN) * 128;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
   typedef Stage<T, BM, WAVES, L> StageL;
   typedef Stage<T, BN, WAVES, R> StageR;
-  constexpr int LOADS = StageL::LOADS + StageR::LOADS;
-  const StageL from_l(left, mt * BM, wave, lane);
-  const StageR from_r(right, nt * BN, wave, lane);
-  const int begin = int(blockIdx.z) * g.split, end = min(g.steps, begin + g.split);
 
-  auto load = [&](int step, char *stage) {
-    from_l.load(left, step, stage, wave);
-    from_r.load(right, step, stage + BM * 64, wave);
+  // this workgroup's items (a tile and a split of k): every width-th of its
+  // die's run of them
+  const int tiles = g.mtiles * g.ntiles, items = tiles * g.splits;
+  const int per = (items + 7) >> 3, width = int(gridDim.x >> 3);
+  const int last = min(items, (int(blockIdx.x & 7) + 1) * per);
+  int item = int(blockIdx.x & 7) * per + int(blockIdx.x >> 3);
+  if (item >= last) return;
+
+  // the loads' place in the items
+  StageL from_l;
+  StageR from_r;
+  int ahead_item = item, ahead_step, ahead_end, slot = 0;
+  auto aim = [&]() {
+    int mt, nt;
+    tile_at(g, ahead_item % tiles, mt, nt);
+    ahead_step = ahead_item / tiles * g.split;
+    ahead_end = min(g.steps, ahead_step + g.split);
+    from_l.aim(left, mt * BM, wave, lane);
+    from_r.aim(right, nt * BN, wave, lane);
+  };
+  aim();
+  // the next step into the stage that is not `slot`; at the end of the items the last step
+  // once more, so that the loop has no branch around it
+  auto load = [&]() {
+    from_l.load(left, ahead_step, fill + (slot ^ 1) * STAGE, wave);
+    from_r.load(right, ahead_step, fill + (slot ^ 1) * STAGE + BM * 128, wave);
+  };
+  auto advance = [&]() {
+    if (ahead_step + 1 < ahead_end) {
+      ++ahead_step;
+    } else if (ahead_item + width < last) {
+      ahead_item += width;
+      aim();
+    }
   };
 
+  struct Fragments {
+    u32x4 l[MI], r[NI];
+  };
+  auto read = [&](Fragments &f, int half) {
+    const lds_char *tl = data + slot * STAGE, *tr = tl + BM * 128;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) f.l[i] = StageL::fragment(tl, wm * TM + i * 16, half, lane);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) f.r[j] = StageR::fragment(tr, wn * TN + j * 16, half, lane);
+  };
   f32x4 acc[MI][NI];
-#pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
-
-  // the stages of this step, the next and the one after
-  char *now = lds, *next = lds + STAGE, *after = lds + 2 * STAGE;
-  if (begin < end) load(begin, now);
-  if (begin + 1 < end) load(begin + 1, next);
-  stage_barrier<LOADS>(begin + 1 < end);
-  for (int step = begin; step < end; ++step) {
-    if (step + 2 < end) load(step + 2, after);
-    u32x4 fl[MI], fr[NI];
-#pragma unroll
-    for (int i = 0; i < MI; ++i) fl[i] = StageL::fragment(now, wm * TM + i * 16, lane);
-#pragma unroll
-    for (int j = 0; j < NI; ++j) fr[j] = StageR::fragment(now + BM * 64, wn * TN + j * 16, lane);
+  auto multiply = [&](const Fragments &f) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NI; ++j) acc[i][j] = mma<T>(fr[j], fl[i], acc[i][j]);
-    // the next step's loads have landed, and every wave is done with this one
-    stage_barrier<LOADS>(step + 2 < end);
-    char *done = now;
-    now = next;
-    next = after;
-    after = done;
+      for (int j = 0; j < NI; ++j) acc[i][j] = mma<T>(f.r[j], f.l[i], acc[i][j]);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) keep_accumulators(acc[i]);
+  };
+  // this wave's loads have landed and its reads are done; then all waves' are
+  auto barrier = [] {
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // the order of a half step's instructions: its reads (and loads) among the
+  // first half of its products
+  constexpr int kReads = MI * (L::kContiguous ? 1 : sizeof(T) == 2 ? 2 : 4) + NI * (R::kContiguous ? 1 : sizeof(T) == 2 ? 2 : 4);
+  auto interleave = [](auto loads) {
+    if constexpr (MI * NI == 64) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, kReads / 16, 0);          // LDS reads
+        if (loads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);         // loads
+        __builtin_amdgcn_sched_group_barrier(0x008, sizeof(T) == 2 ? 2 : 8, 0);  // products
+      }
+    }
+  };
+
+  Fragments first, second;
+  slot = 1;
+  load();
+  advance();
+  barrier();
+  slot = 0;
+  read(first, 0);
+  load();
+  advance();
+  for (; item < last; item += width) {
+    int mt, nt;
+    tile_at(g, item % tiles, mt, nt);
+    const int split = item / tiles;
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+    for (int steps = min(g.split, g.steps - split * g.split); steps > 0; --steps) {
+      read(second, 1);
+      multiply(first);
+      interleave(std::false_type());
+      barrier();
+      slot ^= 1;
+      read(first, 0);  // past the last step: what an older one left, and nothing uses it
+      load();
+      multiply(second);
+      interleave(std::true_type());
+      advance();
+    }
+    epilogue(Place{mt * BM + wm * TM, nt * BN + wn * TN, mt, nt, wm, wn, lane, split, scratch}, acc);
   }
-  epilogue(Place{mt * BM + wm * TM, nt * BN + wn * TN, mt, nt, wm, wn, lane, int(blockIdx.z), lds}, acc);
+}
+
+// Many tiles: eight waves of 128 x 64, two on each SIMD.
+template <typename T, typename L, typename R, typename Epilogue>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_product_large(Grid g, L left, R right,
+                                                                                                 Epilogue epilogue) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  lds_char *stages = (lds_char *)lds;
+  walk_tiles<T, 256, 256, 2, 4>(g, left, right, epilogue, stages, stages, lds + 2 * (256 + 256) * 128);
+}
+
+// Few tiles: waves of 32 x 32, several workgroups a CU.
+template <typename T, typename L, typename R, typename Epilogue>
+__global__ __launch_bounds__(256) void k_product_small(Grid g, L left, R right, Epilogue epilogue) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  lds_char *stages = (lds_char *)lds;
+  walk_tiles<T, 64, 64, 2, 2>(g, left, right, epilogue, stages, stages, lds + 2 * (64 + 64) * 128);
 }
 
 // ------------------------------------------------------------- epilogues ----
+// At the head of an epilogue's row of fragments: no work of other rows is mixed
+// with this one's (beside 256 accumulators there are no registers for it).
+template <int NI>
+__device__ inline void one_row_at_a_time(f32x4 (&row)[NI]) {
+  __builtin_amdgcn_sched_barrier(0);
+  keep_accumulators(row);
+}
+
 template <typename T>
 __device__ inline void store4(T *p, f32x4 v, int count, bool whole) {
   if (whole && count >= 4) {
@@ -380,6 +468,7 @@ struct Store {
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
+      one_row_at_a_time(c[i]);
       const int m = at.m0 + i * 16 + (at.lane & 15);
       T *row = out.row(m);
       if (!row) continue;
@@ -394,15 +483,16 @@ struct Store {
 };
 
 // One split's part of the result, in 32 bits: [split][rows][cols4], added to
-// what an earlier launch left there if `add`.
+// what an earlier launch left there if Add.
+template <bool Add>
 struct StorePart {
   float *part;
   int rows, cols4;
-  bool add;
   template <int MI, int NI>
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
+      one_row_at_a_time(c[i]);
       const int m = at.m0 + i * 16 + (at.lane & 15);
       if (m >= rows) continue;
       float *row = part + (int64_t(at.split) * rows + m) * cols4;
@@ -411,7 +501,8 @@ struct StorePart {
         const int n = at.n0 + j * 16 + (at.lane >> 4) * 4;
         if (n >= cols4) continue;
         f32x4 *p = reinterpret_cast<f32x4 *>(row + n);
-        *p = add ? *p + c[i][j] : c[i][j];
+        if constexpr (Add) *p += c[i][j];
+        else *p = c[i][j];
       }
     }
   }
@@ -447,6 +538,7 @@ struct GatedForward {
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
+      one_row_at_a_time(c[i]);
       const int m = at.m0 + i * 16 + (at.lane & 15);
       if (m >= rows) continue;
 #pragma unroll
@@ -479,6 +571,7 @@ struct GatedBackward {
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
+      one_row_at_a_time(c[i]);
       const int m = at.m0 + i * 16 + (at.lane & 15);
       if (m >= rows) continue;
 #pragma unroll
@@ -510,29 +603,18 @@ __device__ inline float2 softmax_join(float2 a, float2 b) {
   return make_float2(top, a.y * exp_diff(a.x, ref) + b.y * exp_diff(b.x, ref));
 }
 
-// The logits of a wave's words, in place: the bias added, and -inf past the
-// vocabulary.
-template <int MI, int NI>
-__device__ inline void add_bias(f32x4 (&c)[MI][NI], const float *bias, int n0, int lane, int first, int vocab) {
-  const int v0 = first + n0 + (lane >> 4) * 4;
-  const bool inside = first + n0 + NI * 16 <= vocab;  // the same for the whole wave
+// The bias of a lane's words; -inf past the vocabulary, where the products are
+// of some row of the weights that is in it.
+template <int NI>
+__device__ inline void word_bias(f32x4 (&b)[NI], const float *bias, int n0, int lane, int first, int vocab) {
 #pragma unroll
-  for (int j = 0; j < NI; ++j) {
-    f32x4 b = {0, 0, 0, 0};
+  for (int j = 0; j < NI; ++j)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int v = v0 + j * 16 + r;
-      if (bias) b[r] = bias[min(v, vocab - 1)];
-      if (!inside && v >= vocab) {
-        b[r] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < MI; ++i) c[i][j][r] = -INFINITY;
-      }
+      const int v = first + n0 + j * 16 + (lane >> 4) * 4 + r;
+      b[j][r] = bias ? bias[min(v, vocab - 1)] : 0.0f;
+      if (v >= vocab) b[j][r] = -INFINITY;
     }
-    if (bias)
-#pragma unroll
-      for (int i = 0; i < MI; ++i) c[i][j] += b;
-  }
 }
 
 // Where a row's label is among the wave's words, if this lane holds it: the
@@ -555,9 +637,14 @@ struct SoftmaxPart {
   template <int MI, int NI>
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
     float2 *shared = reinterpret_cast<float2 *>(at.lds);  // [WN][BM]
-    add_bias(c, bias, at.n0, at.lane, 0, vocab);
+    f32x4 b[NI];
+    word_bias(b, bias, at.n0, at.lane, 0, vocab);
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
+      one_row_at_a_time(c[i]);
+      f32x4 z[NI];
+#pragma unroll
+      for (int j = 0; j < NI; ++j) z[j] = c[i][j] + b[j];
       const int m = at.m0 + i * 16 + (at.lane & 15);
       const int hit = label_at<NI>(m < rows ? labels[m] : -1, at.n0, at.lane, 0, vocab);
       if (__ballot(hit >= 0)) {
@@ -565,13 +652,13 @@ struct SoftmaxPart {
         for (int j = 0; j < NI; ++j)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (hit == j * 16 + r) label_logit[m] = c[i][j][r];
+            if (hit == j * 16 + r) label_logit[m] = z[j][r];
       }
       float top = -INFINITY;
 #pragma unroll
       for (int j = 0; j < NI; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) top = fmaxf(top, c[i][j][r]);
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, z[j][r]);
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       // nothing but -inf: the sum is 0 against any finite reference
@@ -580,7 +667,7 @@ struct SoftmaxPart {
 #pragma unroll
       for (int j = 0; j < NI; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sum += exp_diff(c[i][j][r], ref);
+        for (int r = 0; r < 4; ++r) sum += exp_diff(z[j][r], ref);
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
       if (at.lane < 16) shared[at.wn * BM + at.wm * MI * 16 + i * 16 + at.lane] = make_float2(top, sum);
@@ -622,34 +709,36 @@ struct SoftmaxGrad {
   int rows, vocab, first, piece;
   template <int MI, int NI>
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
-    add_bias(c, bias, at.n0, at.lane, first, vocab);
-    f32x4 sums[NI];
+    f32x4 b[NI], sums[NI];
+    word_bias(b, bias, at.n0, at.lane, first, vocab);
 #pragma unroll
     for (int j = 0; j < NI; ++j) sums[j] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
+      one_row_at_a_time(c[i]);
       const int m = at.m0 + i * 16 + (at.lane & 15);
       const int label = m < rows ? labels[m] : -1;
       const float l = m < rows ? lse[m] : 0.0f, d = m < rows ? row_factor[m] : 0.0f;
       const bool kept = label >= 0 && label < vocab && l != -INFINITY;
+      f32x4 z[NI];
 #pragma unroll
       for (int j = 0; j < NI; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          c[i][j][r] = kept ? __builtin_amdgcn_exp2f((c[i][j][r] - l) * kLog2e + kGradLog2<T>) : 0.0f;
+          z[j][r] = kept ? __builtin_amdgcn_exp2f((c[i][j][r] + b[j][r] - l) * kLog2e + kGradLog2<T>) : 0.0f;
       const int hit = kept ? label_at<NI>(label, at.n0, at.lane, first, vocab) : -1;
       if (__ballot(hit >= 0)) {
 #pragma unroll
         for (int j = 0; j < NI; ++j)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (hit == j * 16 + r) c[i][j][r] -= kGradUnit<T>;
+            if (hit == j * 16 + r) z[j][r] -= kGradUnit<T>;
       }
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
         const int n = at.n0 + j * 16 + (at.lane >> 4) * 4;
-        if (m < rows && n < ldg) store4(grad + m * ldg + n, c[i][j], 4, true);
-        if (col_part) sums[j] += c[i][j] * d;
+        if (m < rows && n < ldg) store4(grad + m * ldg + n, z[j], 4, true);
+        sums[j] += z[j] * d;
       }
     }
     if (!col_part) return;
@@ -699,30 +788,49 @@ __global__ __launch_bounds__(256) void k_lse_join(const float2 *part, int ntiles
   }
 }
 
-// The rows' gradients as factors of the products: row_factor = dloss / unit for
-// dx and dbias, and x_factor = dloss / (the largest finite |dloss|) for the rows
-// of x in dweight, whose result is then multiplied by out[0], that largest
-// value / unit.  All are 0 for rows that are left out.
+// The rows' gradients as factors of the products: row_factor = dloss / S for dx
+// and dbias, and x_factor = dloss / unit for the rows of x in dweight, whose
+// result is then multiplied by out[0] = unit / S.  The unit is the smallest
+// finite |dloss| above 0, by the power of two that brings it to the largest's
+// magnitude: equal gradients, and power-of-two multiples of one (a word that
+// counts once, twice, four times), then leave the rows of x unrounded.  The
+// factors are 0 for rows that are left out.
 __global__ __launch_bounds__(1024) void k_grad_factors(const float *dloss, const float *lse, const int32_t *labels,
-                                                       int rows, int vocab, float unit, float *out, float *row_factor,
+                                                       int rows, int vocab, float s, float *out, float *row_factor,
                                                        float *x_factor) {
-  __shared__ float shared[16];
-  float top = 0.0f;
+  __shared__ float tops[16], lows[16];
+  float top = 0.0f, low = INFINITY;
   for (int m = threadIdx.x; m < rows; m += 1024) {
     const float d = fabsf(dloss[m]);
-    if (labels[m] >= 0 && labels[m] < vocab && d < INFINITY) top = fmaxf(top, d);
+    if (labels[m] >= 0 && labels[m] < vocab && d < INFINITY && d > 0.0f) {
+      top = fmaxf(top, d);
+      low = fminf(low, d);
+    }
   }
-  for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
-  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = top;
+  for (int x = 1; x < 64; x <<= 1) {
+    top = fmaxf(top, __shfl_xor(top, x));
+    low = fminf(low, __shfl_xor(low, x));
+  }
+  if ((threadIdx.x & 63) == 0) {
+    tops[threadIdx.x >> 6] = top;
+    lows[threadIdx.x >> 6] = low;
+  }
   __syncthreads();
-  for (int w = 0; w < 16; ++w) top = fmaxf(top, shared[w]);
-  // below 2^-100 the quotients would leave the range: such a value counts as that
-  top = fmaxf(top, 0x1p-100f);
-  if (threadIdx.x == 0) out[0] = top / unit;
+  for (int w = 0; w < 16; ++w) {
+    top = fmaxf(top, tops[w]);
+    low = fminf(low, lows[w]);
+  }
+  float unit = 0x1p-100f;  // at least: below, the quotients would leave the range
+  if (top > unit) {
+    int e_top, e_low;
+    frexpf(top, &e_top);
+    unit = ldexpf(frexpf(low, &e_low), e_top);
+  }
+  if (threadIdx.x == 0) out[0] = unit / s;
   for (int m = threadIdx.x; m < rows; m += 1024) {
     const bool kept = labels[m] >= 0 && labels[m] < vocab && lse[m] != -INFINITY;
-    row_factor[m] = kept ? dloss[m] / unit : 0.0f;
-    x_factor[m] = kept ? dloss[m] / top : 0.0f;
+    row_factor[m] = kept ? dloss[m] / s : 0.0f;
+    x_factor[m] = kept ? dloss[m] / unit : 0.0f;
   }
 }
 
@@ -826,23 +934,24 @@ hipError_t operand(const void *p, int64_t ld, int64_t rows, int cols, Arena &ws,
 }
 
 // Tiles of a product and the parts its sum over k is split into: large tiles
-// where they fill the device (with the splits: at least 32 steps each), else
+// where they fill the device (with the splits: at least 16 steps each), else
 // small ones.  Only a product whose result is stored plainly can be split.
 struct Tiles {
   bool large = true;
-  int m = 128, n = 256, splits = 1;
+  int m = 256, n = 256, splits = 1;
   Tiles(int64_t rows, int64_t cols, int64_t steps = 0) {
-    const int64_t most = steps / 32 < 1 ? 1 : steps / 32 > 64 ? 64 : steps / 32;
-    int64_t tiles = ceil_div(rows, 128) * ceil_div(cols, 256);
-    int64_t want = 512;
-    if (tiles * most < 192) {
+    const int64_t most = steps / 16 < 1 ? 1 : steps / 16 > 64 ? 64 : steps / 16;
+    int64_t tiles = ceil_div(rows, 256) * ceil_div(cols, 256);
+    int64_t want = 256;
+    if (tiles * most < 128) {
       large = false;
       m = n = 64;
       tiles = ceil_div(rows, 64) * ceil_div(cols, 64);
       want = 768;
     }
     want = ceil_div(want, tiles);
-    if (steps) splits = int(want < most ? want : most);
+    if (want > most) want = most;
+    if (steps) splits = int(ceil_div(steps, ceil_div(steps, want)));  // none is empty
   }
 };
 
@@ -851,15 +960,17 @@ int64_t steps_of(int64_t k) {
   return ceil_div(k, kStep<T>);
 }
 
-template <int BM_, int BN_>
+constexpr size_t kEpilogueLds = 8192;  // of the softmax epilogues: four waves' parts of 256 rows
+
+template <int BM_, int BN_, int WM_, int WN_>
 struct Shape {
-  static constexpr int BM = BM_, BN = BN_, WM = 2, WN = 2;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
 };
 
 // Calls fn with the shape of the tiles.
 template <typename Fn>
 hipError_t with_shape(const Tiles &t, Fn fn) {
-  return t.large ? fn(Shape<128, 256>()) : fn(Shape<64, 64>());
+  return t.large ? fn(Shape<256, 256, 2, 4>()) : fn(Shape<64, 64, 2, 2>());
 }
 
 template <typename T, typename S, typename L, typename R, typename Epilogue>
@@ -870,15 +981,18 @@ hipError_t product(int64_t m, int64_t n, int64_t k, int splits, const L &left, c
   g.ntiles = int(ceil_div(n, S::BN));
   g.steps = int(steps_of<T>(k));
   g.split = int(ceil_div(g.steps, splits));
-  const dim3 grid(unsigned(round_up(int64_t(g.mtiles) * g.ntiles, 8)), 1, unsigned(splits));
-  auto kernel = k_product<T, S::BM, S::BN, S::WM, S::WN, L, R, Epilogue>;
-  constexpr size_t lds = 3 * (S::BM + S::BN) * 64;
-  if (lds > 65536) {
+  g.splits = splits;
+  const int64_t items = round_up(int64_t(g.mtiles) * g.ntiles * splits, 8);
+  constexpr size_t lds = 2 * (S::BM + S::BN) * 128 + kEpilogueLds;
+  if constexpr (S::BM == 256) {
+    auto kernel = k_product_large<T, L, R, Epilogue>;
     static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                                           hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
     OPS_TRY(allowed);
+    kernel<<<unsigned(items < 256 ? items : 256), 512, lds, s>>>(g, left, right, epi);
+  } else {
+    k_product_small<T, L, R, Epilogue><<<unsigned(items < 1024 ? items : 1024), 256, lds, s>>>(g, left, right, epi);
   }
-  kernel<<<grid, 64 * S::WM * S::WN, lds, s>>>(g, left, right, epi);
   return hipGetLastError();
 }
 
@@ -896,7 +1010,7 @@ hipError_t product_into(int64_t m, int64_t n, int64_t k, const L &left, const R 
       return product<T, decltype(shape)>(m, n, k, 1, left, right, Store<T>{out, int(n)}, s);
     });
   OPS_TRY(with_shape(tiles, [&](auto shape) {
-    return product<T, decltype(shape)>(m, n, k, splits, left, right, StorePart{part, int(m), int(cols4), false}, s);
+    return product<T, decltype(shape)>(m, n, k, splits, left, right, StorePart<false>{part, int(m), int(cols4)}, s);
   }));
   k_join<T><<<strided(ceil_div(m * cols4, 1024)), 256, 0, s>>>(part, splits, int(m), int(n), int(cols4), out);
   return hipGetLastError();
@@ -1053,9 +1167,13 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
         OPS_TRY(hipGetLastError());
       }
       OPS_TRY(with_shape(dx_tiles, [&](auto shape) {
-        return product<T, decltype(shape)>(a.rows, a.width, words, splits, Rows<T>{grad, words_k, rows, words_k},
-                                           Columns<T>{wp, w.ld, a.width, words},
-                                           StorePart{dx_part, rows, int(cols4), first > 0}, s);
+        const Rows<T> gr{grad, words_k, rows, words_k};
+        const Columns<T> wc{wp, w.ld, a.width, words};
+        if (first == 0)
+          return product<T, decltype(shape)>(a.rows, a.width, words, splits, gr, wc,
+                                             StorePart<false>{dx_part, rows, int(cols4)}, s);
+        return product<T, decltype(shape)>(a.rows, a.width, words, splits, gr, wc,
+                                           StorePart<true>{dx_part, rows, int(cols4)}, s);
       }));
     }
     T *dwp = dw + int64_t(first) * a.width;
