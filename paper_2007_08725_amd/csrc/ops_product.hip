@@ -9,8 +9,6 @@
 #include <math.h>
 #include <stdint.h>
 
-#include <type_traits>
-
 #include "ops_internal.h"
 
 #pragma clang fp contract(fast)
@@ -56,8 +54,8 @@ __device__ inline f32x4 mma<float>(u32x4 r, u32x4 l, f32x4 c) {
   return c;
 }
 
-// Operands.  A step of the product takes 128 bytes of k of every row (kStep
-// elements; whole cache lines), in 16-byte chunks (kChunk elements).  An operand lies in memory
+// Operands.  A step of the product takes 64 bytes of k of every row (kStep
+// elements), in 16-byte chunks (kChunk elements).  An operand lies in memory
 // either with k contiguous ("rows") or with its rows contiguous ("columns":
 // the transposed matrix, element (row, k) at p[k * ld + row]); neither is
 // copied for the other, LDS is read transposed.  `base` gives the address of
@@ -69,7 +67,7 @@ __device__ inline f32x4 mma<float>(u32x4 r, u32x4 l, f32x4 c) {
 template <typename T>
 constexpr int kChunk = 16 / int(sizeof(T));
 template <typename T>
-constexpr int kStep = 128 / int(sizeof(T));
+constexpr int kStep = 64 / int(sizeof(T));
 
 template <typename T>
 struct Rows {
@@ -77,7 +75,7 @@ struct Rows {
   const T *p;
   int64_t ld;
   int rows, k;
-  __device__ int64_t ahead(int step) const { return int64_t(step) * 128; }
+  __device__ int64_t ahead(int step) const { return int64_t(step) * 64; }
   __device__ const char *base(int row, int k0) const {
     return reinterpret_cast<const char *>(p + int64_t(min(row, rows - 1)) * ld + k0);
   }
@@ -90,7 +88,7 @@ struct Columns {
   const T *p;
   int64_t ld;
   int rows, k;
-  __device__ int64_t ahead(int step) const { return step * 128 * ld; }
+  __device__ int64_t ahead(int step) const { return step * 64 * ld; }
   __device__ const char *base(int row, int k0) const {
     return reinterpret_cast<const char *>(p + int64_t(k0) * ld + min(row, (rows - 1) / kChunk<T> * kChunk<T>));
   }
@@ -108,7 +106,7 @@ struct PairRows {
   const T *gate, *value;
   int64_t ld_gate, ld_value;
   int hidden, k;
-  __device__ int64_t ahead(int step) const { return int64_t(step) * 128; }
+  __device__ int64_t ahead(int step) const { return int64_t(step) * 64; }
   __device__ const char *base(int n, int k0) const {
     const int64_t f = min(pair_row(n), hidden - 1);
     return reinterpret_cast<const char *>((n & 16 ? value + f * ld_value : gate + f * ld_gate) + k0);
@@ -123,7 +121,12 @@ struct PairColumns {
   const T *gate, *value;
   int64_t ld;  // of both
   int width, hidden;
-  __device__ int64_t ahead(int step) const { return step * 64 * ld; }
+  // a step is one turn of the pair in 16-bit types, half of one in 32 bits
+  __device__ int64_t ahead(int step) const {
+    if (sizeof(T) == 2) return step * 32 * ld;
+    const int64_t other = reinterpret_cast<const char *>(value) - reinterpret_cast<const char *>(gate);
+    return (step >> 1) * 64 * ld + (step & 1 ? other : 0);
+  }
   __device__ const char *base(int row, int k0) const {
     return reinterpret_cast<const char *>((k0 & 16 ? value : gate) + int64_t(pair_row(k0)) * ld +
                                           min(row, (width - 1) / kChunk<T> * kChunk<T>));
@@ -142,7 +145,9 @@ struct Place {
 
 struct Grid {
   int mtiles, ntiles;
-  int steps, split, splits;  // steps of k in all, of one split, and the splits (none is empty)
+  // steps of k in all and of one split, both even (past the end of k all is
+  // zero), and the splits (none is empty)
+  int steps, split, splits;
 };
 
 // what a lane whose chunk lies past the end of k reads instead
@@ -167,11 +172,11 @@ __device__ inline void tile_at(const Grid &g, int t, int &mt, int &nt) {
   mt = first + in % high;
   nt = in / high;
 }
-// An operand's part of a stage in LDS, B rows: B/8 loads of 1 KiB, dealt to the
+// An operand's part of a stage in LDS, B rows: B/16 loads of 1 KiB, dealt to the
 // waves in turns.
 //
-// k contiguous: 128 bytes a row; chunk c of row r lies at place c ^ (r & 7), so
-// that the 16 rows that a fragment read touches spread over the banks.
+// k contiguous: 64 bytes a row; chunk c of row r lies at place c ^ (r / 2 & 3),
+// so that the 16 rows that a fragment read touches spread over the banks.
 //
 // Rows contiguous: kStep lines of B elements, in slots of 16 rows.  Four
 // 16-bit lines of a slot are what one transposing read of 16 lanes takes
@@ -181,6 +186,7 @@ __device__ inline void tile_at(const Grid &g, int t, int &mt, int &nt) {
 // spread over the banks.
 //
 // Measured: no bank conflicts with either layout.
+__device__ inline int chunk_turn(int row) { return (row >> 1) & 3; }
 template <typename T, int B>
 __device__ inline int slot_turn(int line) {
   return (sizeof(T) == 2 ? (line & 3) | ((line >> 1) & 4) : (line >> 2) & 3) & (B / 16 - 1);
@@ -188,20 +194,22 @@ __device__ inline int slot_turn(int line) {
 
 template <typename T, int B, int WAVES, typename Op>
 struct Stage {
-  static constexpr int LOADS = B / 8 / WAVES;
-  static_assert(LOADS >= 1 && B % (8 * WAVES) == 0, "every wave loads the same number of times");
+  static constexpr int LOADS = B / 16 / WAVES;
+  static_assert(LOADS >= 1 && B % (16 * WAVES) == 0, "every wave loads the same number of times");
   static constexpr int LINE = B * int(sizeof(T));  // bytes, rows contiguous
   // rows contiguous: lines from one load of a wave to its next
   static constexpr int NEXT = Op::kContiguous ? 0 : WAVES * 1024 / LINE;
   static_assert(Op::kContiguous || (WAVES * 1024) % LINE == 0, "a wave's loads are whole lines apart");
+  static constexpr int WAVES_ = WAVES, ROWS = B;
+  static constexpr bool CONTIGUOUS = Op::kContiguous;
   const char *src[LOADS];
   int k0;  // of the lane's chunk in a step, in the first load
 
   __device__ void aim(const Op &op, int row0, int wave, int lane) {
     if (Op::kContiguous) {
-      k0 = ((lane & 7) ^ (lane >> 3)) * kChunk<T>;
+      k0 = ((lane & 3) ^ chunk_turn(lane >> 2)) * kChunk<T>;
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) src[i] = op.base(row0 + (i * WAVES + wave) * 8 + (lane >> 3), k0);
+      for (int i = 0; i < LOADS; ++i) src[i] = op.base(row0 + (i * WAVES + wave) * 16 + (lane >> 2), k0);
     } else {
       k0 = (wave * 1024 + lane * 16) / LINE;
       const int part = (wave * 1024 + lane * 16) % LINE / 16;
@@ -213,70 +221,80 @@ struct Stage {
       }
     }
   }
-  __device__ void load(const Op &op, int step, lds_char *to, int wave) const {
-    const int64_t ahead = op.ahead(step);
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const char *p = op.in(step, k0 + i * NEXT) ? src[i] + ahead : reinterpret_cast<const char *>(&kZeroChunk);
-      __builtin_amdgcn_global_load_lds((global_ptr)p, (lds_ptr)(to + (i * WAVES + wave) * 1024), 16, 0, 0);
-    }
-  }
-  // The fragment of rows row0..row0+15 (of the tile), half s of the step.
-  static __device__ u32x4 fragment(const lds_char *tile, int row0, int s, int lane) {
-    const int q = lane & 15, group = lane >> 4;
-    if (Op::kContiguous)
-      return *(const lds_u32x4 *)(tile + (row0 + q) * 128 + ((s * 4 + group) ^ (q & 7)) * 16);
-    if (sizeof(T) == 2) {
-      const int line = s * 32 + group * 8 + (q >> 2);
-      const lds_char *p = tile + line * LINE + (((row0 >> 4) ^ slot_turn<T, B>(line)) * 32) + (q & 3) * 8;
-      const u32x2 lo = transposed(p), hi = transposed(p + 4 * LINE);
-      return u32x4{lo[0], lo[1], hi[0], hi[1]};
-    }
-    u32x4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int line = (s * 4 + group) * 4 + e;
-      v[e] = *(const lds_u32 *)(tile + line * LINE + (((row0 >> 4) ^ slot_turn<T, B>(line)) * 64) + q * 4);
-    }
-    return v;
-  }
-  static __device__ u32x2 transposed(const lds_char *p) {
-    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
+  // where a lane's load i of a step comes from
+  __device__ const char *from(const Op &op, int step, int64_t ahead, int i) const {
+    return op.in(step, k0 + i * NEXT) ? src[i] + ahead : reinterpret_cast<const char *>(&kZeroChunk);
   }
 };
 
-// Tells the compiler that a row of accumulators is in the matrix unit's
-// registers here.  Without it, it keeps some of 256 in others and moves them
-// back and forth in the loop over k.
-template <int NI>
-__device__ inline void keep_accumulators(f32x4 (&row)[NI]) {
-  if constexpr (NI == 8) {
-#pragma unroll
-    for (int j = 0; j < NI; ++j) asm volatile("" : "+a"(row[j]));
-  }
+// The loads of a step into LDS and the reads of a step's fragments.  Macros,
+// because the compiler has to see both in one function whose restricted
+// arguments say that they touch different stages: else it waits for every load
+// in flight before it reads.
+#define LOAD_STEP(stage, op, step, to)                                                                       \
+  do {                                                                                                       \
+    const int64_t ahead_ = (op).ahead(step);                                                                 \
+    _Pragma("unroll") for (int i_ = 0; i_ < decltype(stage)::LOADS; ++i_) __builtin_amdgcn_global_load_lds(  \
+        (global_ptr)(stage).from(op, step, ahead_, i_),                                                      \
+        (lds_ptr)((to) + (i_ * decltype(stage)::WAVES_ + wave) * 1024), 16, 0, 0);                           \
+  } while (0)
+
+#define READ_FRAGMENTS(stage, f, count, tile, row0)                                                          \
+  do {                                                                                                       \
+    typedef decltype(stage) S_;                                                                              \
+    const int q_ = lane & 15, group_ = lane >> 4;                                                            \
+    _Pragma("unroll") for (int i_ = 0; i_ < (count); ++i_) {                                                 \
+      const int slot_ = ((row0) >> 4) + i_;                                                                  \
+      if constexpr (S_::CONTIGUOUS) {                                                                        \
+        (f)[i_] = *(const lds_u32x4 *)((tile) + (slot_ * 16 + q_) * 64 + (group_ ^ chunk_turn(q_)) * 16);    \
+      } else if constexpr (sizeof(T) == 2) {                                                                 \
+        const int line_ = group_ * 8 + (q_ >> 2);                                                            \
+        const int at_ = line_ * S_::LINE + (slot_ ^ slot_turn<T, S_::ROWS>(line_)) * 32 + (q_ & 3) * 8;      \
+        const s16x4 lo_ = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((tile) + at_));              \
+        const s16x4 hi_ = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((tile) + at_ + 4 * S_::LINE)); \
+        const u32x2 l_ = __builtin_bit_cast(u32x2, lo_), h_ = __builtin_bit_cast(u32x2, hi_);                \
+        (f)[i_] = u32x4{l_[0], l_[1], h_[0], h_[1]};                                                         \
+      } else {                                                                                               \
+        _Pragma("unroll") for (int e_ = 0; e_ < 4; ++e_) {                                                   \
+          const int line_ = group_ * 4 + e_;                                                                 \
+          (f)[i_][e_] = *(const lds_u32 *)((tile) + line_ * S_::LINE +                                       \
+                                           (slot_ ^ slot_turn<T, S_::ROWS>(line_)) * 64 + q_ * 4);           \
+        }                                                                                                    \
+      }                                                                                                      \
+    }                                                                                                        \
+  } while (0)
+
+constexpr int kEpilogueLds = 8192;  // of the softmax epilogues: four waves' parts of 256 rows
+
+// Every wave's reads and its older loads are done; those of the last `Flying`
+// loads of each wave may be in flight.
+template <int Flying>
+__device__ inline void stage_barrier() {
+  static_assert(Flying < 16, "vmcnt's low field");
+  __builtin_amdgcn_s_waitcnt(0x0070 | Flying);  // vmcnt(Flying) lgkmcnt(0)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 // C tiles of BM x BN by WM x WN waves, on a grid that stays on the device and
-// walks through the tiles.  Two stages in LDS and two sets of fragments: while
-// the first half of a step is multiplied, its second half is read; then the
-// next step has landed and this one's stage is free, and while the second half
-// is multiplied, the step after next is loaded into it and the first half of
-// the next step is read.  The loads run over the ends of tiles, so that a
-// tile's first step is there when the epilogue of the tile before is done.
+// walks through the tiles.  Four stages in LDS: while a step's fragments are
+// multiplied, the next step's are read and three steps' loads are in flight.
+// The loads run over the ends of tiles, so that a tile's first steps are there
+// when the epilogue of the tile before is done.
 //
 // `fill` and `data` are both the stages in LDS: between two barriers the stage
-// that is filled is not the one that is read, and as restricted pointers they
-// let the compiler see that (else it waits for the loads before it reads).
+// that is filled is not the one that is read.
 template <typename T, int BM, int BN, int WM, int WN, typename L, typename R, typename Epilogue>
-__device__ __attribute__((always_inline)) inline void walk_tiles(const Grid &g, const L &left, const R &right,
-                                                                 const Epilogue &epilogue, lds_char *__restrict fill,
-                                                                 const lds_char *__restrict data, char *scratch) {
+__device__ inline void walk_tiles(const Grid &g, const L &left, const R &right, const Epilogue &epilogue,
+                                  lds_char *__restrict fill, const lds_char *__restrict data, char *scratch) {
   constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16, WAVES = WM * WN;
-  constexpr int STAGE = (BM + BN) * 128;
+  constexpr int STAGE = (BM + BN) * 64;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
   typedef Stage<T, BM, WAVES, L> StageL;
   typedef Stage<T, BN, WAVES, R> StageR;
+  constexpr int LOADS = StageL::LOADS + StageR::LOADS;
 
   // this workgroup's items (a tile and a split of k): every width-th of its
   // die's run of them
@@ -286,10 +304,11 @@ __device__ __attribute__((always_inline)) inline void walk_tiles(const Grid &g, 
   int item = int(blockIdx.x & 7) * per + int(blockIdx.x >> 3);
   if (item >= last) return;
 
-  // the loads' place in the items
+  // the loads' place in the items; at their end the last step is loaded once
+  // more, so that every wave has the same number of loads in flight
   StageL from_l;
   StageR from_r;
-  int ahead_item = item, ahead_step, ahead_end, slot = 0;
+  int ahead_item = item, ahead_step, ahead_end;
   auto aim = [&]() {
     int mt, nt;
     tile_at(g, ahead_item % tiles, mt, nt);
@@ -297,13 +316,6 @@ __device__ __attribute__((always_inline)) inline void walk_tiles(const Grid &g, 
     ahead_end = min(g.steps, ahead_step + g.split);
     from_l.aim(left, mt * BM, wave, lane);
     from_r.aim(right, nt * BN, wave, lane);
-  };
-  aim();
-  // the next step into the stage that is not `slot`; at the end of the items the last step
-  // once more, so that the loop has no branch around it
-  auto load = [&]() {
-    from_l.load(left, ahead_step, fill + (slot ^ 1) * STAGE, wave);
-    from_r.load(right, ahead_step, fill + (slot ^ 1) * STAGE + BM * 128, wave);
   };
   auto advance = [&]() {
     if (ahead_step + 1 < ahead_end) {
@@ -313,56 +325,26 @@ __device__ __attribute__((always_inline)) inline void walk_tiles(const Grid &g, 
       aim();
     }
   };
-
-  struct Fragments {
-    u32x4 l[MI], r[NI];
-  };
-  auto read = [&](Fragments &f, int half) {
-    const lds_char *tl = data + slot * STAGE, *tr = tl + BM * 128;
-#pragma unroll
-    for (int i = 0; i < MI; ++i) f.l[i] = StageL::fragment(tl, wm * TM + i * 16, half, lane);
-#pragma unroll
-    for (int j = 0; j < NI; ++j) f.r[j] = StageR::fragment(tr, wn * TN + j * 16, half, lane);
-  };
   f32x4 acc[MI][NI];
-  auto multiply = [&](const Fragments &f) {
+  auto multiply = [&](const u32x4(&l)[MI], const u32x4(&r)[NI]) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NI; ++j) acc[i][j] = mma<T>(f.r[j], f.l[i], acc[i][j]);
-#pragma unroll
-    for (int i = 0; i < MI; ++i) keep_accumulators(acc[i]);
-  };
-  // this wave's loads have landed and its reads are done; then all waves' are
-  auto barrier = [] {
-    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
-  // the order of a half step's instructions: its reads (and loads) among the
-  // first half of its products
-  constexpr int kReads = MI * (L::kContiguous ? 1 : sizeof(T) == 2 ? 2 : 4) + NI * (R::kContiguous ? 1 : sizeof(T) == 2 ? 2 : 4);
-  auto interleave = [](auto loads) {
-    if constexpr (MI * NI == 64) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x100, kReads / 16, 0);          // LDS reads
-        if (loads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);         // loads
-        __builtin_amdgcn_sched_group_barrier(0x008, sizeof(T) == 2 ? 2 : 8, 0);  // products
-      }
-    }
+      for (int j = 0; j < NI; ++j) acc[i][j] = mma<T>(r[j], l[i], acc[i][j]);
   };
 
-  Fragments first, second;
-  slot = 1;
-  load();
-  advance();
-  barrier();
-  slot = 0;
-  read(first, 0);
-  load();
-  advance();
+  aim();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    LOAD_STEP(from_l, left, ahead_step, fill + i * STAGE);
+    LOAD_STEP(from_r, right, ahead_step, fill + i * STAGE + BM * 64);
+    advance();
+  }
+  stage_barrier<0>();
+  u32x4 al[MI], ar[NI], bl[MI], br[NI];
+  READ_FRAGMENTS(from_l, al, MI, data, wm * TM);
+  READ_FRAGMENTS(from_r, ar, NI, data + BM * 64, wn * TN);
+  int slot = 0;  // the stage of the step that is multiplied
   for (; item < last; item += width) {
     int mt, nt;
     tile_at(g, item % tiles, mt, nt);
@@ -371,20 +353,37 @@ __device__ __attribute__((always_inline)) inline void walk_tiles(const Grid &g, 
     for (int i = 0; i < MI; ++i)
 #pragma unroll
       for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
-    for (int steps = min(g.split, g.steps - split * g.split); steps > 0; --steps) {
-      read(second, 1);
-      multiply(first);
-      interleave(std::false_type());
-      barrier();
-      slot ^= 1;
-      read(first, 0);  // past the last step: what an older one left, and nothing uses it
-      load();
-      multiply(second);
-      interleave(std::true_type());
+    // a step: the next one's fragments are read (past the last step: the last
+    // one's once more, which nothing uses), and its own stage, which every wave
+    // has read, is loaded
+    for (int steps = min(g.split, g.steps - split * g.split); steps > 0; steps -= 2) {
+      stage_barrier<2 * LOADS>();
+      const int odd = (slot + 1) & 3, even = (slot + 2) & 3;
+      READ_FRAGMENTS(from_l, bl, MI, data + odd * STAGE, wm * TM);
+      READ_FRAGMENTS(from_r, br, NI, data + odd * STAGE + BM * 64, wn * TN);
+      LOAD_STEP(from_l, left, ahead_step, fill + slot * STAGE);
+      LOAD_STEP(from_r, right, ahead_step, fill + slot * STAGE + BM * 64);
+      multiply(al, ar);
       advance();
+      stage_barrier<2 * LOADS>();
+      READ_FRAGMENTS(from_l, al, MI, data + even * STAGE, wm * TM);
+      READ_FRAGMENTS(from_r, ar, NI, data + even * STAGE + BM * 64, wn * TN);
+      LOAD_STEP(from_l, left, ahead_step, fill + odd * STAGE);
+      LOAD_STEP(from_r, right, ahead_step, fill + odd * STAGE + BM * 64);
+      multiply(bl, br);
+      advance();
+      slot = even;
     }
     epilogue(Place{mt * BM + wm * TM, nt * BN + wn * TN, mt, nt, wm, wn, lane, split, scratch}, acc);
   }
+}
+
+// The LDS address, as one that the compiler does not know: two arguments that
+// it can prove equal lose their `restrict`.
+__device__ inline lds_char *unfolded(char *lds) {
+  uint32_t none = 0;
+  asm volatile("" : "+s"(none));
+  return (lds_char *)lds + none;
 }
 
 // Many tiles: eight waves of 128 x 64, two on each SIMD.
@@ -392,26 +391,20 @@ template <typename T, typename L, typename R, typename Epilogue>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_product_large(Grid g, L left, R right,
                                                                                                  Epilogue epilogue) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  lds_char *stages = (lds_char *)lds;
-  walk_tiles<T, 256, 256, 2, 4>(g, left, right, epilogue, stages, stages, lds + 2 * (256 + 256) * 128);
+  walk_tiles<T, 256, 256, 2, 4>(g, left, right, epilogue, unfolded(lds), unfolded(lds), lds + 4 * (256 + 256) * 64);
 }
 
 // Few tiles: waves of 32 x 32, several workgroups a CU.
 template <typename T, typename L, typename R, typename Epilogue>
 __global__ __launch_bounds__(256) void k_product_small(Grid g, L left, R right, Epilogue epilogue) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  lds_char *stages = (lds_char *)lds;
-  walk_tiles<T, 64, 64, 2, 2>(g, left, right, epilogue, stages, stages, lds + 2 * (64 + 64) * 128);
+  walk_tiles<T, 64, 64, 2, 2>(g, left, right, epilogue, unfolded(lds), unfolded(lds), lds + 4 * (64 + 64) * 64);
 }
 
 // ------------------------------------------------------------- epilogues ----
 // At the head of an epilogue's row of fragments: no work of other rows is mixed
-// with this one's (beside 256 accumulators there are no registers for it).
-template <int NI>
-__device__ inline void one_row_at_a_time(f32x4 (&row)[NI]) {
-  __builtin_amdgcn_sched_barrier(0);
-  keep_accumulators(row);
-}
+// with this one's (beside 128 accumulators there are no registers for it).
+__device__ inline void one_row_at_a_time() { __builtin_amdgcn_sched_barrier(0); }
 
 template <typename T>
 __device__ inline void store4(T *p, f32x4 v, int count, bool whole) {
@@ -468,7 +461,7 @@ struct Store {
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      one_row_at_a_time(c[i]);
+      one_row_at_a_time();
       const int m = at.m0 + i * 16 + (at.lane & 15);
       T *row = out.row(m);
       if (!row) continue;
@@ -492,7 +485,7 @@ struct StorePart {
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      one_row_at_a_time(c[i]);
+      one_row_at_a_time();
       const int m = at.m0 + i * 16 + (at.lane & 15);
       if (m >= rows) continue;
       float *row = part + (int64_t(at.split) * rows + m) * cols4;
@@ -538,7 +531,7 @@ struct GatedForward {
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      one_row_at_a_time(c[i]);
+      one_row_at_a_time();
       const int m = at.m0 + i * 16 + (at.lane & 15);
       if (m >= rows) continue;
 #pragma unroll
@@ -571,7 +564,7 @@ struct GatedBackward {
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      one_row_at_a_time(c[i]);
+      one_row_at_a_time();
       const int m = at.m0 + i * 16 + (at.lane & 15);
       if (m >= rows) continue;
 #pragma unroll
@@ -641,7 +634,7 @@ struct SoftmaxPart {
     word_bias(b, bias, at.n0, at.lane, 0, vocab);
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      one_row_at_a_time(c[i]);
+      one_row_at_a_time();
       f32x4 z[NI];
 #pragma unroll
       for (int j = 0; j < NI; ++j) z[j] = c[i][j] + b[j];
@@ -715,7 +708,7 @@ struct SoftmaxGrad {
     for (int j = 0; j < NI; ++j) sums[j] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      one_row_at_a_time(c[i]);
+      one_row_at_a_time();
       const int m = at.m0 + i * 16 + (at.lane & 15);
       const int label = m < rows ? labels[m] : -1;
       const float l = m < rows ? lse[m] : 0.0f, d = m < rows ? row_factor[m] : 0.0f;
@@ -934,13 +927,13 @@ hipError_t operand(const void *p, int64_t ld, int64_t rows, int cols, Arena &ws,
 }
 
 // Tiles of a product and the parts its sum over k is split into: large tiles
-// where they fill the device (with the splits: at least 16 steps each), else
+// where they fill the device (with the splits: at least 32 steps each), else
 // small ones.  Only a product whose result is stored plainly can be split.
 struct Tiles {
   bool large = true;
   int m = 256, n = 256, splits = 1;
   Tiles(int64_t rows, int64_t cols, int64_t steps = 0) {
-    const int64_t most = steps / 16 < 1 ? 1 : steps / 16 > 64 ? 64 : steps / 16;
+    const int64_t most = steps / 32 < 1 ? 1 : steps / 32 > 64 ? 64 : steps / 32;
     int64_t tiles = ceil_div(rows, 256) * ceil_div(cols, 256);
     int64_t want = 256;
     if (tiles * most < 128) {
@@ -951,16 +944,15 @@ struct Tiles {
     }
     want = ceil_div(want, tiles);
     if (want > most) want = most;
-    if (steps) splits = int(ceil_div(steps, ceil_div(steps, want)));  // none is empty
+    if (steps) splits = int(ceil_div(steps, split_steps(steps, want)));  // none is empty
   }
+  static int64_t split_steps(int64_t steps, int64_t splits) { return round_up(ceil_div(steps, splits), 2); }
 };
 
 template <typename T>
 int64_t steps_of(int64_t k) {
-  return ceil_div(k, kStep<T>);
+  return round_up(ceil_div(k, kStep<T>), 2);
 }
-
-constexpr size_t kEpilogueLds = 8192;  // of the softmax epilogues: four waves' parts of 256 rows
 
 template <int BM_, int BN_, int WM_, int WN_>
 struct Shape {
@@ -980,10 +972,10 @@ hipError_t product(int64_t m, int64_t n, int64_t k, int splits, const L &left, c
   g.mtiles = int(ceil_div(m, S::BM));
   g.ntiles = int(ceil_div(n, S::BN));
   g.steps = int(steps_of<T>(k));
-  g.split = int(ceil_div(g.steps, splits));
+  g.split = int(Tiles::split_steps(g.steps, splits));
   g.splits = splits;
   const int64_t items = round_up(int64_t(g.mtiles) * g.ntiles * splits, 8);
-  constexpr size_t lds = 2 * (S::BM + S::BN) * 128 + kEpilogueLds;
+  constexpr size_t lds = 4 * (S::BM + S::BN) * 64 + kEpilogueLds;
   if constexpr (S::BM == 256) {
     auto kernel = k_product_large<T, L, R, Epilogue>;
     static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
