@@ -1,4 +1,10 @@
 // Layer norm, forward and backward (include/lda_ops.h).
+//
+// Both passes are bound by memory: a row is read once, kept in the registers of
+// the lanes that share it, reduced across them, and written once.  The backward
+// pass walks several rows with the same lanes and keeps its columns' sums of
+// dweight and dbias in registers meanwhile; they are joined in a fixed order.
+// Rows too wide for that are read from the caches again.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -13,32 +19,275 @@ namespace {
 
 typedef __bf16 bf16;
 typedef _Float16 f16;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-__device__ inline float block_sum(float v, float *shared) {
-  for (int x = 1; x < 64; x <<= 1) v += __shfl_xor(v, x);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return shared[0] + shared[1] + shared[2] + shared[3];
+template <typename T>
+constexpr int kChunk = 16 / int(sizeof(T));
+
+// 16 bytes of a row as they lie in memory.
+template <typename T>
+struct Chunk {
+  typedef T vec __attribute__((ext_vector_type(kChunk<T>)));
+  vec v;
+  __device__ float operator[](int e) const { return float(v[e]); }
+};
+
+// The columns of a row that a lane holds: V chunks, LANES chunks apart.  Rows
+// that do not start at multiples of 16 bytes, or do not end at one, are moved
+// element by element.
+template <typename T, int LANES, int V, bool Aligned>
+struct Cols {
+  static constexpr int C = kChunk<T>;
+  static __device__ int first(int v, int lane) { return (v * LANES + lane) * C; }
+  static __device__ void load_one(const T *row, int cols, int lane, int v, Chunk<T> &x) {
+    const int c = first(v, lane);
+    if (Aligned) {
+      if (c < cols) x.v = *reinterpret_cast<const typename Chunk<T>::vec *>(row + c);
+      else x.v = typename Chunk<T>::vec(T(0.0f));
+    } else {
+#pragma unroll
+      for (int e = 0; e < C; ++e) x.v[e] = c + e < cols ? row[c + e] : T(0.0f);
+    }
+  }
+  static __device__ void load(const T *row, int cols, int lane, Chunk<T> (&x)[V]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) load_one(row, cols, lane, v, x[v]);
+  }
+  static __device__ void store(T *row, int cols, int c, typename Chunk<T>::vec x) {
+    if (Aligned) {
+      if (c < cols) *reinterpret_cast<typename Chunk<T>::vec *>(row + c) = x;
+    } else {
+#pragma unroll
+      for (int e = 0; e < C; ++e)
+        if (c + e < cols) row[c + e] = x[e];
+    }
+  }
+};
+
+// Sums over the LANES lanes that share a row; every lane gets them.
+template <int LANES>
+__device__ inline float2 row_sum(float2 s, float2 *shared) {
+#pragma unroll
+  for (int x = 1; x < (LANES < 64 ? LANES : 64); x <<= 1) {
+    s.x += __shfl_xor(s.x, x);
+    s.y += __shfl_xor(s.y, x);
+  }
+  if (LANES > 64) {
+    constexpr int WAVES = LANES / 64;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = shared[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+      s.x += shared[w].x;
+      s.y += shared[w].y;
+    }
+  }
+  return s;
 }
 
-// One workgroup per row.
+constexpr int threads_of(int lanes) { return lanes > 256 ? lanes : 256; }
+constexpr bool grad_in_registers(int threads, int columns) { return threads < 1024 || columns < 32; }
+
+template <typename T, int LANES, int V, bool Aligned>
+__global__ __launch_bounds__(threads_of(LANES)) void k_norm(const T *x, int64_t ldx, const T *weight, const T *bias,
+                                                            int64_t rows, int cols, float eps, T *y, int64_t ldy,
+                                                            float *mean, float *rstd) {
+  typedef Cols<T, LANES, V, Aligned> At;
+  constexpr int C = At::C;
+  __shared__ float2 shared[16];
+  const int lane = threadIdx.x % LANES;
+  const int64_t row = int64_t(blockIdx.x) * (threads_of(LANES) / LANES) + threadIdx.x / LANES;
+  if (LANES <= 64 && row >= rows) return;
+  Chunk<T> v[V];
+  At::load(x + row * ldx, cols, lane, v);
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+#pragma unroll
+    for (int e = 0; e < C; ++e) s += v[i][e];
+  const float mu = row_sum<LANES>(make_float2(s, 0.0f), shared).x / cols;
+  // the squares of the deviations, not the sum of squares: exact where a row's
+  // mean is large beside its spread
+  float q = 0.0f;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+      const float d = At::first(i, lane) + e < cols ? v[i][e] - mu : 0.0f;
+      q += d * d;
+    }
+  const float r = 1.0f / sqrtf(row_sum<LANES>(make_float2(q, 0.0f), shared).x / cols + eps);
+  if (lane == 0) {
+    mean[row] = mu;
+    rstd[row] = r;
+  }
+  Chunk<T> w[V], b[V];
+  if (weight) {
+    At::load(weight, cols, lane, w);
+    At::load(bias, cols, lane, b);
+  }
+  T *out = y + row * ldy;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    typename Chunk<T>::vec o;
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+      const float h = (v[i][e] - mu) * r;
+      o[e] = T(weight ? h * w[i][e] + b[i][e] : h);
+    }
+    At::store(out, cols, At::first(i, lane), o);
+  }
+}
+
+// Each group of LANES lanes takes every (gridDim.x * groups)-th row.  part
+// [2][gridDim.x][cols]: the workgroup's sums of dy h and of dy by column.
+template <typename T, int LANES, int V, bool Aligned>
+__global__ __launch_bounds__(threads_of(LANES)) void k_norm_grad(const T *dy, int64_t lddy, const T *x, int64_t ldx,
+                                                                 const T *weight, const float *mean, const float *rstd,
+                                                                 int64_t rows, int cols, T *dx, int64_t lddx,
+                                                                 float *part) {
+  typedef Cols<T, LANES, V, Aligned> At;
+  constexpr int C = At::C, THREADS = threads_of(LANES), GROUPS = THREADS / LANES;
+  __shared__ float2 shared[GROUPS > 1 ? THREADS * C : 16];
+  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+  // The weight and both sums stay in registers.  With 32 columns a lane and
+  // 1,024 lanes (128 registers each) only one sum does: the weight is read from
+  // the caches and the sum of dy is kept in LDS, by the lane that owns it.
+  constexpr bool kHold = grad_in_registers(THREADS, V * C);
+  extern __shared__ f32x4 in_lds[];  // [V][C / 4][THREADS]
+  float sw[V][C], sb[kHold ? V : 1][C];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+      sw[i][e] = 0.0f;
+      if (kHold) sb[i][e] = 0.0f;
+    }
+    if (!kHold)
+#pragma unroll
+      for (int q = 0; q < C / 4; ++q) in_lds[(i * (C / 4) + q) * THREADS + threadIdx.x] = f32x4{0, 0, 0, 0};
+  }
+  Chunk<T> w[V];
+  if (kHold && weight) At::load(weight, cols, lane, w);
+  // every lane of a workgroup that meets at barriers has the same rows
+  for (int64_t row = int64_t(blockIdx.x) * GROUPS + group; row < rows; row += int64_t(gridDim.x) * GROUPS) {
+    Chunk<T> v[V], d[V];
+    At::load(x + row * ldx, cols, lane, v);
+    At::load(dy + row * lddy, cols, lane, d);
+    const float mu = mean[row], r = rstd[row];
+    float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (!kHold && weight) At::load_one(weight, cols, lane, i, w[i]);
+#pragma unroll
+      for (int e = 0; e < C; ++e) {
+        const float h = (v[i][e] - mu) * r;
+        const float g = weight ? d[i][e] * w[i][e] : d[i][e];
+        // past the columns dy is 0
+        s.x += g;
+        s.y += g * h;
+        sw[i][e] += d[i][e] * h;
+        if (kHold) sb[i][e] += d[i][e];
+      }
+      if (!kHold)
+#pragma unroll
+        for (int q = 0; q < C / 4; ++q)
+          in_lds[(i * (C / 4) + q) * THREADS + threadIdx.x] +=
+              f32x4{d[i][4 * q], d[i][4 * q + 1], d[i][4 * q + 2], d[i][4 * q + 3]};
+    }
+    s = row_sum<LANES>(s, shared);
+    s.x /= cols;
+    s.y /= cols;
+    T *out = dx + row * lddx;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (!kHold && weight) At::load_one(weight, cols, lane, i, w[i]);
+      typename Chunk<T>::vec o;
+#pragma unroll
+      for (int e = 0; e < C; ++e) {
+        const float h = (v[i][e] - mu) * r;
+        const float g = weight ? d[i][e] * w[i][e] : d[i][e];
+        o[e] = T(r * (g - s.x - h * s.y));
+      }
+      At::store(out, cols, At::first(i, lane), o);
+    }
+  }
+  if (!part) return;
+  float *pw = part + int64_t(blockIdx.x) * cols, *pb = pw + int64_t(gridDim.x) * cols;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    if (GROUPS > 1) {
+      // the groups' sums, in the order of the groups
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < C; ++e) shared[e * THREADS + threadIdx.x] = make_float2(sw[i][e], sb[kHold ? i : 0][e]);
+      __syncthreads();
+      for (int at = threadIdx.x; at < LANES * C; at += THREADS) {
+        const int e = at % C, l = at / C, c = At::first(i, l) + e;
+        float2 t = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+          const float2 o = shared[e * THREADS + g * LANES + l];
+          t.x += o.x;
+          t.y += o.y;
+        }
+        if (c < cols) {
+          pw[c] = t.x;
+          pb[c] = t.y;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < C; ++e) {
+        const int c = At::first(i, lane) + e;
+        if (c < cols) {
+          pw[c] = sw[i][e];
+          pb[c] = kHold ? sb[kHold ? i : 0][e] : in_lds[(i * (C / 4) + e / 4) * THREADS + threadIdx.x][e % 4];
+        }
+      }
+    }
+  }
+}
+
+// dweight (blockIdx.y = 0) and dbias (1) from their parts: 16 columns a
+// workgroup, 16 threads a column.
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm(const T *x, int64_t ldx, const T *weight, const T *bias, int cols,
-                                              float eps, T *y, int64_t ldy, float *mean, float *rstd) {
-  __shared__ float shared[4];
+__global__ __launch_bounds__(256) void k_norm_join(const float *part, int parts, int cols, T *dweight, T *dbias) {
+  __shared__ float shared[16][17];
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15), way = threadIdx.x >> 4;
+  float s = 0.0f;
+  if (c < cols) {
+    const float *p = part + int64_t(blockIdx.y) * parts * cols + c;
+#pragma unroll 4
+    for (int i = way; i < parts; i += 16) s += p[int64_t(i) * cols];
+  }
+  shared[way][threadIdx.x & 15] = s;
+  __syncthreads();
+  if (threadIdx.x < 16 && c < cols) {
+    for (int w = 1; w < 16; ++w) s += shared[w][threadIdx.x];
+    (blockIdx.y ? dbias : dweight)[c] = T(s);
+  }
+}
+
+// ---------------------------------------------- rows wider than registers ---
+template <typename T>
+__global__ __launch_bounds__(1024) void k_norm_wide(const T *x, int64_t ldx, const T *weight, const T *bias, int cols,
+                                                    float eps, T *y, int64_t ldy, float *mean, float *rstd) {
+  __shared__ float2 shared[16];
   const T *row = x + int64_t(blockIdx.x) * ldx;
   float s = 0.0f;
-  for (int c = threadIdx.x; c < cols; c += 256) s += float(row[c]);
-  const float mu = block_sum(s, shared) / cols;
+  for (int c = threadIdx.x; c < cols; c += 1024) s += float(row[c]);
+  const float mu = row_sum<1024>(make_float2(s, 0.0f), shared).x / cols;
   float q = 0.0f;
-  for (int c = threadIdx.x; c < cols; c += 256) {
+  for (int c = threadIdx.x; c < cols; c += 1024) {
     const float d = float(row[c]) - mu;
     q += d * d;
   }
-  const float r = 1.0f / sqrtf(block_sum(q, shared) / cols + eps);
+  const float r = 1.0f / sqrtf(row_sum<1024>(make_float2(q, 0.0f), shared).x / cols + eps);
   T *out = y + int64_t(blockIdx.x) * ldy;
-  for (int c = threadIdx.x; c < cols; c += 256) {
+  for (int c = threadIdx.x; c < cols; c += 1024) {
     const float h = (float(row[c]) - mu) * r;
     out[c] = T(weight ? h * float(weight[c]) + float(bias[c]) : h);
   }
@@ -49,30 +298,33 @@ __global__ __launch_bounds__(256) void k_norm(const T *x, int64_t ldx, const T *
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm_dx(const T *dy, int64_t lddy, const T *x, int64_t ldx, const T *weight,
-                                                 const float *mean, const float *rstd, int cols, T *dx, int64_t lddx) {
-  __shared__ float shared[4];
+__global__ __launch_bounds__(1024) void k_norm_wide_dx(const T *dy, int64_t lddy, const T *x, int64_t ldx,
+                                                       const T *weight, const float *mean, const float *rstd, int cols,
+                                                       T *dx, int64_t lddx) {
+  __shared__ float2 shared[16];
   const T *row = x + int64_t(blockIdx.x) * ldx, *grad = dy + int64_t(blockIdx.x) * lddy;
   const float mu = mean[blockIdx.x], r = rstd[blockIdx.x];
-  float sg = 0.0f, sh = 0.0f;
-  for (int c = threadIdx.x; c < cols; c += 256) {
+  float2 s = make_float2(0.0f, 0.0f);
+  for (int c = threadIdx.x; c < cols; c += 1024) {
     const float g = float(grad[c]) * (weight ? float(weight[c]) : 1.0f);
-    sg += g;
-    sh += g * (float(row[c]) - mu) * r;
+    s.x += g;
+    s.y += g * (float(row[c]) - mu) * r;
   }
-  sg = block_sum(sg, shared) / cols;
-  sh = block_sum(sh, shared) / cols;
+  s = row_sum<1024>(s, shared);
+  s.x /= cols;
+  s.y /= cols;
   T *out = dx + int64_t(blockIdx.x) * lddx;
-  for (int c = threadIdx.x; c < cols; c += 256) {
+  for (int c = threadIdx.x; c < cols; c += 1024) {
     const float g = float(grad[c]) * (weight ? float(weight[c]) : 1.0f);
-    out[c] = T(r * (g - sg - (float(row[c]) - mu) * r * sh));
+    out[c] = T(r * (g - s.x - (float(row[c]) - mu) * r * s.y));
   }
 }
 
-// Column sums of dy h and dy over `per` rows a workgroup: part[2][parts][cols].
+// Column sums of dy h and dy over `per` rows a workgroup: part[2][gridDim.y][cols].
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm_dw(const T *dy, int64_t lddy, const T *x, int64_t ldx, const float *mean,
-                                                 const float *rstd, int64_t rows, int cols, int64_t per, float *part) {
+__global__ __launch_bounds__(256) void k_norm_wide_dw(const T *dy, int64_t lddy, const T *x, int64_t ldx,
+                                                      const float *mean, const float *rstd, int64_t rows, int cols,
+                                                      int64_t per, float *part) {
   const int c = blockIdx.x * 256 + threadIdx.x;
   if (c >= cols) return;
   const int64_t first = blockIdx.y * per, last = first + per < rows ? first + per : rows;
@@ -86,46 +338,109 @@ __global__ __launch_bounds__(256) void k_norm_dw(const T *dy, int64_t lddy, cons
   part[(int64_t(gridDim.y) + blockIdx.y) * cols + c] = sb;
 }
 
+// ------------------------------------------------------------------- host ---
+template <int LANES_, int V_, bool Aligned_>
+struct Shape {
+  static constexpr int LANES = LANES_, V = V_;
+  static constexpr bool Aligned = Aligned_;
+};
+
+// Calls fn with the lanes that share a row of `chunks` 16-byte chunks and the
+// chunks that each holds; false if no lanes hold them all.  A wave a row up to
+// 256 chunks (of 8 lanes up to 8), then workgroups of 256 and of 1,024 threads.
+template <bool Aligned, typename Fn>
+bool with_lanes(int64_t chunks, Fn fn) {
+  if (chunks <= 8) fn(Shape<8, 1, Aligned>());
+  else if (chunks <= 64) fn(Shape<64, 1, Aligned>());
+  else if (chunks <= 128) fn(Shape<64, 2, Aligned>());
+  else if (chunks <= 256) fn(Shape<64, 4, Aligned>());
+  else if (chunks <= 512) fn(Shape<256, 2, Aligned>());
+  else if (chunks <= 1024) fn(Shape<256, 4, Aligned>());
+  else if (chunks <= 2048) fn(Shape<1024, 2, Aligned>());
+  else if (chunks <= 4096) fn(Shape<1024, 4, Aligned>());
+  else return false;
+  return true;
+}
+
+template <typename T, typename Fn>
+bool with_shape(bool aligned, int cols, Fn fn) {
+  const int64_t chunks = ceil_div(cols, kChunk<T>);
+  return aligned ? with_lanes<true>(chunks, fn) : with_lanes<false>(chunks, fn);
+}
+
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm_join(const float *part, int parts, int cols, T *dweight, T *dbias) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= cols) return;
-  const float *p = part + int64_t(blockIdx.y) * parts * cols + c;
-  float s = 0.0f;
-  for (int i = 0; i < parts; ++i) s += p[int64_t(i) * cols];
-  (blockIdx.y ? dbias : dweight)[c] = T(s);
+bool aligned16(const void *p, int64_t ld) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % kChunk<T> == 0;
 }
 
 template <typename T>
 hipError_t norm_forward_t(const lda_norm_args &a) {
   if (a.rows == 0) return hipSuccess;
-  k_norm<T><<<unsigned(a.rows), 256, 0, static_cast<hipStream_t>(a.stream)>>>(
-      static_cast<const T *>(a.x), a.ldx, static_cast<const T *>(a.weight), static_cast<const T *>(a.bias), a.cols,
-      a.eps, static_cast<T *>(a.y), a.ldy, a.mean, a.rstd);
+  const hipStream_t s = static_cast<hipStream_t>(a.stream);
+  const T *x = static_cast<const T *>(a.x), *w = static_cast<const T *>(a.weight), *b = static_cast<const T *>(a.bias);
+  T *y = static_cast<T *>(a.y);
+  const bool aligned = a.cols % kChunk<T> == 0 && aligned16<T>(x, a.ldx) && aligned16<T>(y, a.ldy) &&
+                       aligned16<T>(w, 0) && aligned16<T>(b, 0);
+  const bool done = with_shape<T>(aligned, a.cols, [&](auto shape) {
+    typedef decltype(shape) S;
+    constexpr int threads = threads_of(S::LANES);
+    k_norm<T, S::LANES, S::V, S::Aligned><<<unsigned(ceil_div(a.rows, threads / S::LANES)), threads, 0, s>>>(
+        x, a.ldx, w, b, a.rows, a.cols, a.eps, y, a.ldy, a.mean, a.rstd);
+  });
+  if (!done)
+    k_norm_wide<T><<<unsigned(a.rows), 1024, 0, s>>>(x, a.ldx, w, b, a.cols, a.eps, y, a.ldy, a.mean, a.rstd);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t norm_backward_t(const lda_norm_args &a, Arena &ws, bool dry) {
   const hipStream_t s = static_cast<hipStream_t>(a.stream);
-  const int64_t parts = a.rows < 64 ? (a.rows ? a.rows : 1) : 64, per = ceil_div(a.rows, parts);
-  float *part = a.dweight ? ws.take<float>(2 * parts * a.cols) : nullptr;
-  if (dry) return hipSuccess;
-  const T *dy = static_cast<const T *>(a.dy), *x = static_cast<const T *>(a.x);
-  if (a.rows) {
-    k_norm_dx<T><<<unsigned(a.rows), 256, 0, s>>>(dy, a.lddy, x, a.ldx, static_cast<const T *>(a.weight), a.mean,
-                                                  a.rstd, a.cols, static_cast<T *>(a.dx), a.lddx);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+  const T *dy = static_cast<const T *>(a.dy), *x = static_cast<const T *>(a.x), *w = static_cast<const T *>(a.weight);
+  T *dx = static_cast<T *>(a.dx);
+  const bool aligned = a.cols % kChunk<T> == 0 && aligned16<T>(x, a.ldx) && aligned16<T>(dy, a.lddy) &&
+                       aligned16<T>(dx, a.lddx) && aligned16<T>(w, 0);
+  hipError_t e = hipSuccess;
+  int64_t parts = 0;
+  float *part = nullptr;
+  const bool done = with_shape<T>(aligned, a.cols, [&](auto shape) {
+    typedef decltype(shape) S;
+    constexpr int threads = threads_of(S::LANES), groups = threads / S::LANES;
+    // workgroups: enough to fill the device, each with several rows, so that
+    // the parts stay small beside x and dy
+    const int64_t most = threads == 1024 ? 256 : 1024;
+    parts = ceil_div(a.rows, groups * 4);
+    parts = parts > most ? most : parts < 1 ? 1 : parts;
+    part = a.dweight ? ws.take<float>(2 * parts * a.cols) : nullptr;
+    if (dry) return;
+    auto kernel = k_norm_grad<T, S::LANES, S::V, S::Aligned>;
+    constexpr size_t lds = grad_in_registers(threads, S::V * kChunk<T>) ? 0 : threads * S::V * kChunk<T> * sizeof(float);
+    if (lds) {
+      static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                                            hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+      e = allowed;
+      if (e != hipSuccess) return;
+    }
+    kernel<<<unsigned(parts), threads, lds, s>>>(dy, a.lddy, x, a.ldx, w, a.mean, a.rstd, a.rows, a.cols, dx, a.lddx,
+                                                 part);
+    e = hipGetLastError();
+  });
+  if (!done) {
+    parts = a.rows < 64 ? (a.rows ? a.rows : 1) : 64;
+    part = a.dweight ? ws.take<float>(2 * parts * a.cols) : nullptr;
+    if (!dry && a.rows) {
+      k_norm_wide_dx<T><<<unsigned(a.rows), 1024, 0, s>>>(dy, a.lddy, x, a.ldx, w, a.mean, a.rstd, a.cols, dx, a.lddx);
+      e = hipGetLastError();
+    }
+    if (!dry && part && e == hipSuccess) {
+      k_norm_wide_dw<T><<<dim3(unsigned(ceil_div(a.cols, 256)), unsigned(parts)), 256, 0, s>>>(
+          dy, a.lddy, x, a.ldx, a.mean, a.rstd, a.rows, a.cols, ceil_div(a.rows, parts), part);
+      e = hipGetLastError();
+    }
   }
-  if (!a.dweight) return hipSuccess;
-  const unsigned wide = unsigned(ceil_div(a.cols, 256));
-  k_norm_dw<T><<<dim3(wide, unsigned(parts)), 256, 0, s>>>(dy, a.lddy, x, a.ldx, a.mean, a.rstd, a.rows, a.cols, per,
-                                                          part);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  k_norm_join<T><<<dim3(wide, 2), 256, 0, s>>>(part, int(parts), a.cols, static_cast<T *>(a.dweight),
-                                               static_cast<T *>(a.dbias));
+  if (dry || !part || e != hipSuccess) return e;
+  k_norm_join<T><<<dim3(unsigned(ceil_div(a.cols, 16)), 2), 256, 0, s>>>(part, int(parts), a.cols,
+                                                                         static_cast<T *>(a.dweight),
+                                                                         static_cast<T *>(a.dbias));
   return hipGetLastError();
 }
 

@@ -756,8 +756,135 @@ struct SoftmaxGrad {
   }
 };
 
+// ---------------------------------------------------------------- few rows ---
+// At most 16 rows of x (single tokens in serving): the weights are read once,
+// from HBM straight into fragments, 16 of their rows a wave, and nothing is
+// staged; x comes from the caches.  Bound by the weights' bytes.
+constexpr int kFewRows = 16;
+
+// Chunk `c` of a row of `cols` elements, zero past its end; rows that do not
+// start at multiples of 16 bytes, or do not end at one, element by element.
+template <typename T, bool Aligned>
+__device__ inline u32x4 row_chunk(const T *row, int c, int cols) {
+  if (Aligned) return c * kChunk<T> < cols ? *reinterpret_cast<const u32x4 *>(row + c * kChunk<T>) : u32x4{0, 0, 0, 0};
+  typedef T vec __attribute__((ext_vector_type(kChunk<T>)));
+  vec v;
+#pragma unroll
+  for (int e = 0; e < kChunk<T>; ++e) v[e] = c * kChunk<T> + e < cols ? row[c * kChunk<T> + e] : T(0.0f);
+  return __builtin_bit_cast(u32x4, v);
+}
+
+// Products of TILES x 16 rows of weights (this lane's: w[t]) with x, over the
+// groups of four chunks part, part + parts, ..: C[m = lane & 15][n = 4 (lane >> 4) + r].
+template <typename T, bool Aligned, int TILES>
+__device__ inline void few_products(const T *x, const T *const (&w)[TILES], int cols, int part, int parts, int lane,
+                                    f32x4 (&c)[TILES]) {
+  constexpr int U = Aligned ? 8 / TILES : 2;  // groups in flight
+  const int groups = (cols + 4 * kChunk<T> - 1) / (4 * kChunk<T>);
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) c[t] = f32x4{0, 0, 0, 0};
+  for (int g = part; g < groups; g += parts * U) {
+    u32x4 xv[U], wv[U][TILES];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int chunk = (g + u * parts) * 4 + (lane >> 4);
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) wv[u][t] = row_chunk<T, Aligned>(w[t], chunk, cols);
+      xv[u] = row_chunk<T, Aligned>(x, chunk, cols);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) c[t] = mma<T>(wv[u][t], xv[u], c[t]);
+  }
+}
+
+// 16 columns of h a workgroup; its four waves share the sum over k.
+template <typename T, bool Aligned>
+__global__ __launch_bounds__(256) void k_gated_few(const T *x, int64_t ldx, const T *gates, int64_t ld_gate,
+                                                   const T *values, int64_t ld_value, int rows, int width, int hidden,
+                                                   int act, T *h, int64_t ldh) {
+  __shared__ f32x4 shared[3][2][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15;
+  const int64_t n = min(int(blockIdx.x) * 16 + q, hidden - 1);
+  const T *const w[2] = {gates + n * ld_gate, values + n * ld_value};
+  f32x4 c[2];
+  few_products<T, Aligned, 2>(x + min(q, rows - 1) * ldx, w, width, wave, 4, lane, c);
+  if (wave) {
+    shared[wave - 1][0][lane] = c[0];
+    shared[wave - 1][1][lane] = c[1];
+  }
+  __syncthreads();
+  if (wave || q >= rows) return;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    c[0] += shared[i][0][lane];
+    c[1] += shared[i][1][lane];
+  }
+  const int f = int(blockIdx.x) * 16 + (lane >> 4) * 4;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    float p, dp;
+    gate(act, c[0][r], p, dp);
+    if (f + r < hidden) h[q * ldh + f + r] = T(p * c[1][r]);
+  }
+}
+
+// Each wave takes every (4 gridDim.x)-th 16 words and keeps its lanes' softmax
+// so far; part [rows][gridDim.x].
+template <typename T, bool Aligned>
+__global__ __launch_bounds__(256) void k_xent_few(const T *x, int64_t ldx, const T *weight, int64_t ldw,
+                                                  const float *bias, const int32_t *labels, int rows, int width,
+                                                  int vocab, float *label_logit, float2 *part) {
+  __shared__ float2 shared[4][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15;
+  const T *row = x + min(q, rows - 1) * ldx;
+  const int label = q < rows ? labels[q] : -1;
+  float2 so_far = make_float2(-INFINITY, 0.0f);
+  for (int n0 = (int(blockIdx.x) * 4 + wave) * 16; n0 < vocab; n0 += int(gridDim.x) * 64) {
+    const T *const w[1] = {weight + int64_t(min(n0 + q, vocab - 1)) * ldw};
+    f32x4 c[1];
+    few_products<T, Aligned, 1>(row, w, width, 0, 1, lane, c);
+    const int v = n0 + (lane >> 4) * 4;
+    float top = so_far.x;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      c[0][r] = v + r < vocab ? (bias ? c[0][r] + bias[v + r] : c[0][r]) : -INFINITY;
+      if (v + r == label && label < vocab) label_logit[q] = c[0][r];
+      top = fmaxf(top, c[0][r]);
+    }
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float sum = so_far.y * exp_diff(so_far.x, ref);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sum += exp_diff(c[0][r], ref);
+    so_far = make_float2(top, sum);
+  }
+#pragma unroll
+  for (int x_ = 16; x_ < 64; x_ <<= 1)
+    so_far = softmax_join(so_far, make_float2(__shfl_xor(so_far.x, x_), __shfl_xor(so_far.y, x_)));
+  if (lane < 16) shared[wave][lane] = so_far;
+  __syncthreads();
+  if (threadIdx.x >= rows) return;
+  for (int i = 1; i < 4; ++i) so_far = softmax_join(so_far, shared[i][threadIdx.x]);
+  part[int64_t(threadIdx.x) * gridDim.x + blockIdx.x] = so_far;
+}
+
 // ---------------------------------------------------------- small kernels ---
-// Joins the parts of a row: 16 rows a workgroup, 16 threads a row.
+// The loss of a row from its softmax (largest logit, sum).
+__device__ inline void write_loss(float2 a, int m, const float *label_logit, const int32_t *labels, int vocab,
+                                  float *loss, float *lse) {
+  const float total = a.x == -INFINITY && a.y == 0.0f ? -INFINITY : a.x + kLn2 * __builtin_amdgcn_logf(a.y);
+  lse[m] = total;
+  const int label = labels[m];
+  float out = 0.0f;
+  if (label >= 0 && label < vocab) {
+    const float z = label_logit[m];
+    out = z == -INFINITY ? INFINITY : total - z;
+  }
+  loss[m] = out;
+}
+
+// Joins the parts [ntiles][rows]: 16 rows a workgroup, 16 threads a row.
 __global__ __launch_bounds__(256) void k_lse_join(const float2 *part, int ntiles, const float *label_logit,
                                                   const int32_t *labels, int rows, int vocab, float *loss, float *lse) {
   __shared__ float2 shared[16][17];
@@ -769,16 +896,24 @@ __global__ __launch_bounds__(256) void k_lse_join(const float2 *part, int ntiles
   __syncthreads();
   if (threadIdx.x < 16 && m < rows) {
     for (int w = 1; w < 16; ++w) a = softmax_join(a, shared[w][threadIdx.x]);
-    const float total = a.x == -INFINITY && a.y == 0.0f ? -INFINITY : a.x + kLn2 * __builtin_amdgcn_logf(a.y);
-    lse[m] = total;
-    const int label = labels[m];
-    float out = 0.0f;
-    if (label >= 0 && label < vocab) {
-      const float z = label_logit[m];
-      out = z == -INFINITY ? INFINITY : total - z;
-    }
-    loss[m] = out;
+    write_loss(a, m, label_logit, labels, vocab, loss, lse);
   }
+}
+
+// Joins the parts [rows][parts] of few rows: one workgroup a row.
+__global__ __launch_bounds__(256) void k_lse_join_few(const float2 *part, int parts, const float *label_logit,
+                                                      const int32_t *labels, int vocab, float *loss, float *lse) {
+  __shared__ float2 shared[4];
+  const int m = blockIdx.x;
+  float2 a = make_float2(-INFINITY, 0.0f);
+  for (int t = threadIdx.x; t < parts; t += 256) a = softmax_join(a, part[int64_t(m) * parts + t]);
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) a = softmax_join(a, make_float2(__shfl_xor(a.x, x), __shfl_xor(a.y, x)));
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = a;
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (int w = 1; w < 4; ++w) a = softmax_join(a, shared[w]);
+  write_loss(a, m, label_logit, labels, vocab, loss, lse);
 }
 
 // The rows' gradients as factors of the products: row_factor = dloss / S for dx
@@ -1040,6 +1175,16 @@ hipError_t gated_forward_t(const lda_gated_args &a, Arena &ws, bool dry) {
   if (a.rows == 0) return hipSuccess;
   const hipStream_t s = static_cast<hipStream_t>(a.stream);
   const int rows = int(a.rows), k = int(round_up(a.width, kChunk<T>));
+  if (rows <= kFewRows) {
+    if (dry) return hipSuccess;
+    const bool aligned = in_place<T>(a.x, a.ldx, a.width) && in_place<T>(a.w_gate, a.ld_gate, a.width) &&
+                         in_place<T>(a.w_value, a.ld_value, a.width);
+    auto kernel = aligned ? k_gated_few<T, true> : k_gated_few<T, false>;
+    kernel<<<unsigned(ceil_div(a.hidden, 16)), 256, 0, s>>>(
+        static_cast<const T *>(a.x), a.ldx, static_cast<const T *>(a.w_gate), a.ld_gate,
+        static_cast<const T *>(a.w_value), a.ld_value, rows, a.width, a.hidden, a.act, static_cast<T *>(a.h), a.ldh);
+    return hipGetLastError();
+  }
   Matrix<T> x, gate, value;
   OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
   OPS_TRY(pair_operands<T>(a, false, ws, dry, s, gate, value));
@@ -1086,6 +1231,20 @@ hipError_t xent_forward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   if (a.rows == 0) return hipSuccess;
   const hipStream_t s = static_cast<hipStream_t>(a.stream);
   const int rows = int(a.rows), k = int(round_up(a.width, kChunk<T>));
+  if (rows <= kFewRows) {
+    const int64_t groups = ceil_div(a.vocab, 64);
+    const int parts = int(groups < 1024 ? groups : 1024);
+    float2 *part = ws.take<float2>(int64_t(rows) * parts);
+    float *label_logit = ws.take<float>(rows);
+    if (dry) return hipSuccess;
+    auto kernel = in_place<T>(a.x, a.ldx, a.width) && in_place<T>(a.weight, a.ld_weight, a.width) ? k_xent_few<T, true>
+                                                                                                  : k_xent_few<T, false>;
+    kernel<<<unsigned(parts), 256, 0, s>>>(static_cast<const T *>(a.x), a.ldx, static_cast<const T *>(a.weight),
+                                           a.ld_weight, a.bias, a.labels, rows, a.width, a.vocab, label_logit, part);
+    OPS_TRY(hipGetLastError());
+    k_lse_join_few<<<unsigned(rows), 256, 0, s>>>(part, parts, label_logit, a.labels, a.vocab, a.loss, a.lse);
+    return hipGetLastError();
+  }
   const Tiles tiles(a.rows, a.vocab);
   const int ntiles = int(ceil_div(a.vocab, tiles.n));
   Matrix<T> x, w;

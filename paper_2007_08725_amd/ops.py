@@ -68,7 +68,7 @@ def _call(name, args, device, workspace=True):
     if torch.cuda.current_device() != device.index:
         with torch.cuda.device(device):
             return _call(name, args, device, workspace)
-    args.stream = torch.cuda.current_stream(device).cuda_stream
+    args.stream = torch._C._cuda_getCurrentRawStream(device.index)
     scratch = None
     if workspace:
         size = _SIZE()
@@ -128,8 +128,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5):
         _vector("weight", weight, x, cols, x.dtype)
         _vector("bias", bias, x, cols, x.dtype)
     y = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
-    stats = torch.empty(2, rows, dtype=torch.float32, device=x.device)
-    mean, rstd = stats[0], stats[1]
+    mean, rstd = torch.empty(2, rows, dtype=torch.float32, device=x.device).unbind(0)
     a = NormArgs(dtype=_DTYPES[x.dtype], rows=rows, cols=cols, eps=eps, x=x.data_ptr(), ldx=x.stride(0),
                  weight=None if weight is None else weight.data_ptr(), bias=None if bias is None else bias.data_ptr(),
                  y=y.data_ptr(), ldy=cols, mean=mean.data_ptr(), rstd=rstd.data_ptr())
@@ -217,8 +216,7 @@ def softmax_xent(x, weight, labels, bias=None):
     not kept.
     """
     a = _xent_args(x, weight, labels, bias)
-    out = torch.empty(2, a.rows, dtype=torch.float32, device=x.device)
-    loss, lse = out[0], out[1]
+    loss, lse = torch.empty(2, a.rows, dtype=torch.float32, device=x.device).unbind(0)
     a.loss, a.lse = loss.data_ptr(), lse.data_ptr()
     _call("lda_softmax_xent", a, x.device)
     return loss, lse
