@@ -264,8 +264,6 @@ struct Stage {
     }                                                                                                        \
   } while (0)
 
-constexpr int kEpilogueLds = 8192;  // of the softmax epilogues: four waves' parts of 256 rows
-
 // Every wave's reads and its older loads are done; those of the last `Flying`
 // loads of each wave may be in flight.
 template <int Flying>
@@ -386,19 +384,13 @@ __device__ inline lds_char *unfolded(char *lds) {
   return (lds_char *)lds + none;
 }
 
-// Many tiles: eight waves of 128 x 64, two on each SIMD.
-template <typename T, typename L, typename R, typename Epilogue>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_product_large(Grid g, L left, R right,
-                                                                                                 Epilogue epilogue) {
+// BM x BN = 256 x 256: eight waves of 128 x 64, one workgroup a CU.  128 x 128
+// and 64 x 64, where those leave CUs without work: four waves, several
+// workgroups a CU.
+template <typename T, int BM, int BN, int WM, int WN, typename L, typename R, typename Epilogue>
+__global__ __launch_bounds__(64 * WM *WN, 2) void k_product(Grid g, L left, R right, Epilogue epilogue) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  walk_tiles<T, 256, 256, 2, 4>(g, left, right, epilogue, unfolded(lds), unfolded(lds), lds + 4 * (256 + 256) * 64);
-}
-
-// Few tiles: waves of 32 x 32, several workgroups a CU.
-template <typename T, typename L, typename R, typename Epilogue>
-__global__ __launch_bounds__(256) void k_product_small(Grid g, L left, R right, Epilogue epilogue) {
-  extern __shared__ __attribute__((aligned(1024))) char lds[];
-  walk_tiles<T, 64, 64, 2, 2>(g, left, right, epilogue, unfolded(lds), unfolded(lds), lds + 4 * (64 + 64) * 64);
+  walk_tiles<T, BM, BN, WM, WN>(g, left, right, epilogue, unfolded(lds), unfolded(lds), lds + 4 * (BM + BN) * 64);
 }
 
 // ------------------------------------------------------------- epilogues ----
@@ -501,16 +493,23 @@ struct StorePart {
   }
 };
 
-// The activation and its derivative.
+// The activation and its derivative.  The normal distribution function by
+// Abramowitz and Stegun, 7.1.26: 1 - Phi(|a|) = exp(-a^2 / 2) (a1 t + .. + a5 t^5) / 2
+// with t = 1 / (1 + p |a| / sqrt 2), within 7.5e-8, the rounding of a value of
+// order 1 in 32 bits; the exponential is the derivative's too.
 __device__ inline void gate(int act, float a, float &p, float &dp) {
   if (act == LDA_GELU) {
-    const float phi = 0.5f * erfcf(-a * 0.70710678118654752f);
+    const float bell = __builtin_amdgcn_exp2f(-0.5f * kLog2e * a * a);
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * 0.70710678118654752f * fabsf(a));
+    const float tail = 0.5f * bell * t *
+                       (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    const float phi = a >= 0.0f ? 1.0f - tail : tail;
     p = a * phi;
-    dp = phi + a * 0.3989422804014327f * __builtin_amdgcn_exp2f(-0.5f * kLog2e * a * a);
+    dp = phi + a * 0.3989422804014327f * bell;
     return;
   }
   // sigmoid(a) and 1 - sigmoid(a) from e = exp(-|a|), which does not overflow
-  const float e = __builtin_amdgcn_exp2f(-kLog2e * fabsf(a)), big = 1.0f / (1.0f + e), small = e * big;
+  const float e = __builtin_amdgcn_exp2f(-kLog2e * fabsf(a)), big = __builtin_amdgcn_rcpf(1.0f + e), small = e * big;
   const float s = a >= 0.0f ? big : small, t = a >= 0.0f ? small : big;
   if (act == LDA_SIGMOID) {
     p = s;
@@ -1061,27 +1060,35 @@ hipError_t operand(const void *p, int64_t ld, int64_t rows, int cols, Arena &ws,
   return dry ? hipSuccess : pack<T>(p, ld, rows, cols, nullptr, copy, ldd, s);
 }
 
-// Tiles of a product and the parts its sum over k is split into: large tiles
-// where they fill the device (with the splits: at least 32 steps each), else
-// small ones.  Only a product whose result is stored plainly can be split.
+// Tiles of a product and the parts its sum over k is split into.  Only a product
+// whose result is stored plainly can be split, into parts of at least 32 steps.
+// Each shape's cost is the area that the busiest CU has to multiply, over what
+// the shape reaches of the large one's rate (measured: 256 x 256 alone on a CU
+// 1, two workgroups of 128 x 128 0.75, four of 64 x 64 0.45, and about half of
+// that where a CU has only one).
 struct Tiles {
-  bool large = true;
   int m = 256, n = 256, splits = 1;
   Tiles(int64_t rows, int64_t cols, int64_t steps = 0) {
     const int64_t most = steps / 32 < 1 ? 1 : steps / 32 > 64 ? 64 : steps / 32;
-    int64_t tiles = ceil_div(rows, 256) * ceil_div(cols, 256);
-    int64_t want = 256;
-    if (tiles * most < 128) {
-      large = false;
-      m = n = 64;
-      tiles = ceil_div(rows, 64) * ceil_div(cols, 64);
-      want = 768;
+    double best = 0;
+    for (int side : {256, 128, 64}) {
+      const int64_t tiles = ceil_div(rows, side) * ceil_div(cols, side);
+      const int fit = side == 256 ? 1 : side == 128 ? 2 : 4;
+      int64_t want = kCus * fit / tiles;
+      want = want < 1 ? 1 : want > most ? most : want;
+      if (want > 1) want = ceil_div(steps, split_steps(steps, want));  // none is empty
+      const int64_t each = ceil_div(tiles * want, kCus);  // tiles of the busiest CU
+      const double rate = (side == 256 ? 1.0 : side == 128 ? 0.75 : 0.45) * (each < fit ? 0.5 + 0.5 * each / fit : 1.0);
+      const double cost = double(each) * side * side / rate / double(want);
+      if (best == 0 || cost < best) {
+        best = cost;
+        m = n = side;
+        splits = int(want);
+      }
     }
-    want = ceil_div(want, tiles);
-    if (want > most) want = most;
-    if (steps) splits = int(ceil_div(steps, split_steps(steps, want)));  // none is empty
   }
   static int64_t split_steps(int64_t steps, int64_t splits) { return round_up(ceil_div(steps, splits), 2); }
+  static constexpr int64_t kCus = 256;
 };
 
 template <typename T>
@@ -1097,7 +1104,7 @@ struct Shape {
 // Calls fn with the shape of the tiles.
 template <typename Fn>
 hipError_t with_shape(const Tiles &t, Fn fn) {
-  return t.large ? fn(Shape<256, 256, 2, 4>()) : fn(Shape<64, 64, 2, 2>());
+  return t.m == 256 ? fn(Shape<256, 256, 2, 4>()) : t.m == 128 ? fn(Shape<128, 128, 2, 2>()) : fn(Shape<64, 64, 2, 2>());
 }
 
 template <typename T, typename S, typename L, typename R, typename Epilogue>
@@ -1108,18 +1115,17 @@ hipError_t product(int64_t m, int64_t n, int64_t k, int splits, const L &left, c
   g.ntiles = int(ceil_div(n, S::BN));
   g.steps = int(steps_of<T>(k));
   g.split = int(Tiles::split_steps(g.steps, splits));
-  g.splits = splits;
-  const int64_t items = round_up(int64_t(g.mtiles) * g.ntiles * splits, 8);
-  constexpr size_t lds = 4 * (S::BM + S::BN) * 64 + kEpilogueLds;
-  if constexpr (S::BM == 256) {
-    auto kernel = k_product_large<T, L, R, Epilogue>;
+  g.splits = int(ceil_div(g.steps, g.split));  // a shorter k than the splits were chosen for leaves some out
+  const int64_t items = round_up(int64_t(g.mtiles) * g.ntiles * g.splits, 8);
+  constexpr size_t lds = 4 * (S::BM + S::BN) * 64 + S::BM * S::WN * 8;  // and the softmax parts of a tile's rows
+  auto kernel = k_product<T, S::BM, S::BN, S::WM, S::WN, L, R, Epilogue>;
+  if constexpr (lds > 65536) {
     static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                                           hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
     OPS_TRY(allowed);
-    kernel<<<unsigned(items < 256 ? items : 256), 512, lds, s>>>(g, left, right, epi);
-  } else {
-    k_product_small<T, L, R, Epilogue><<<unsigned(items < 1024 ? items : 1024), 256, lds, s>>>(g, left, right, epi);
   }
+  const int64_t most = Tiles::kCus * (S::BM == 256 ? 1 : S::BM == 128 ? 2 : 4);
+  kernel<<<unsigned(items < most ? items : most), 64 * S::WM * S::WN, lds, s>>>(g, left, right, epi);
   return hipGetLastError();
 }
 
@@ -1289,7 +1295,7 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   T *x_scaled = ws.take<T>(a.rows * k);
   T *grad = ws.take<T>(a.rows * piece);
   float *col_part = a.bias ? ws.take<float>(int64_t(mtiles) * piece) : nullptr;
-  const Tiles dx_tiles(a.rows, a.width, steps_of<T>(piece));
+  const Tiles dx_tiles(a.rows, a.width, steps_of<T>(piece < a.vocab ? piece : a.vocab));
   const int splits = dx_tiles.splits;
   const int64_t cols4 = round_up(a.width, 4);
   float *dx_part = ws.take<float>(splits * a.rows * cols4);

@@ -295,6 +295,18 @@ def test_softmax_xent(ops, dtype, rows, width, vocab):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,width,vocab", [(700, 72, 5003), (2049, 40, 20011), (1030, 257, 9001)])
+def test_softmax_xent_larger_tiles(ops, dtype, rows, width, vocab):
+    xent_case(ops, dtype, rows, width, vocab, vocab > 10000)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,width,hidden", [(1500, 136, 1100), (2100, 257, 3001), (4100, 40, 2050)])
+def test_gated_larger_tiles(ops, dtype, rows, width, hidden):
+    gated_case(ops, dtype, rows, width, hidden, "silu")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,pad,offset", [(1, 8, 8), (3, 1, 1), (50, 8, 16), (150, 5, 3)])
 @pytest.mark.parametrize("with_bias", [False, True])
 def test_softmax_xent_strides(ops, dtype, rows, pad, offset, with_bias):
@@ -313,6 +325,12 @@ def test_softmax_xent_many_pieces(ops, dtype):
     """A vocabulary of several pieces: rows and words are such that G of all words would pass 256 MiB."""
     rows, width, vocab = 3000 if dtype == torch.float32 else 6000, 16, 30011
     xent_case(ops, dtype, rows, width, vocab, True)
+
+
+@pytest.mark.parametrize("extra", [1, 70, 2500])
+def test_softmax_xent_short_last_piece(ops, extra):
+    """A last piece with fewer steps of k than dx is split into (65,536 words are a piece at 2,048 rows of 16 bits)."""
+    xent_case(ops, torch.bfloat16, 2048, 16, 65536 + extra, True)
 
 
 @pytest.mark.parametrize("dtype", TYPES)

@@ -140,7 +140,7 @@ def test_null_arguments(lib, make, backward):
 
 @pytest.mark.parametrize("make,change,backward", [
     (norm, dict(weight=A, bias=A, dweight=A, dbias=A), True), (gated, dict(), True), (xent, dict(), True),
-    (gated, dict(width=7, ldx=7, ld_gate=7, ld_value=7), False), (xent, dict(rows=700), False)])
+    (gated, dict(rows=40, width=7, ldx=7, ld_gate=7, ld_value=7), False), (xent, dict(rows=700), False)])
 def test_workspace_is_checked(lib, make, change, backward):
     """A call whose workspace is missing, too small or misaligned is refused before any launch."""
     name = NAMES[make] + ("_backward" if backward else "")
