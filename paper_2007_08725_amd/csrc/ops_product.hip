@@ -31,7 +31,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 // One 16-byte fragment of each operand per lane: row lane & 15, 16-byte chunk
 // lane >> 4 of 64 bytes of k.  The matrix instruction takes R as its first
 // operand, so lane l of the result holds C[m = l & 15][n = 4 (l >> 4) + r],
-// r = 0..3: four neighbours along the contiguous axis of C.
+// r = 0..3 (of a fragment of R's rows: Order): four neighbours along the
+// contiguous axis of C.
 template <typename T>
 __device__ inline f32x4 mma(u32x4 r, u32x4 l, f32x4 c);
 template <>
@@ -95,10 +96,11 @@ struct Columns {
   __device__ bool in(int step, int k0) const { return step * kStep<T> + k0 < k; }
 };
 
-// The rows of w_gate and w_value in turns of 16: row n of the pair is row
-// (n / 32) * 16 + n % 16 of w_gate where n & 16 is 0, else of w_value.  A lane
-// that holds a fragment of a then holds the same elements of b in the next.
-__device__ inline int pair_row(int n) { return (n >> 5) * 16 + (n & 15); }
+// The rows of w_gate and w_value in turns of four: row n of the pair is row
+// (n / 8) * 4 + n % 4 of w_gate where n & 4 is 0, else of w_value.  A lane that
+// holds four neighbours of a then holds the same four of b in its next
+// fragment.
+__device__ inline int pair_row(int n) { return (n >> 3) * 4 + (n & 3); }
 
 template <typename T>
 struct PairRows {
@@ -109,7 +111,7 @@ struct PairRows {
   __device__ int64_t ahead(int step) const { return int64_t(step) * 64; }
   __device__ const char *base(int n, int k0) const {
     const int64_t f = min(pair_row(n), hidden - 1);
-    return reinterpret_cast<const char *>((n & 16 ? value + f * ld_value : gate + f * ld_gate) + k0);
+    return reinterpret_cast<const char *>((n & 4 ? value + f * ld_value : gate + f * ld_gate) + k0);
   }
   __device__ bool in(int step, int k0) const { return step * kStep<T> + k0 < k; }
 };
@@ -121,14 +123,9 @@ struct PairColumns {
   const T *gate, *value;
   int64_t ld;  // of both
   int width, hidden;
-  // a step is one turn of the pair in 16-bit types, half of one in 32 bits
-  __device__ int64_t ahead(int step) const {
-    if (sizeof(T) == 2) return step * 32 * ld;
-    const int64_t other = reinterpret_cast<const char *>(value) - reinterpret_cast<const char *>(gate);
-    return (step >> 1) * 64 * ld + (step & 1 ? other : 0);
-  }
+  __device__ int64_t ahead(int step) const { return step * 32 * ld; }
   __device__ const char *base(int row, int k0) const {
-    return reinterpret_cast<const char *>((k0 & 16 ? value : gate) + int64_t(pair_row(k0)) * ld +
+    return reinterpret_cast<const char *>((k0 & 4 ? value : gate) + int64_t(pair_row(k0)) * ld +
                                           min(row, (width - 1) / kChunk<T> * kChunk<T>));
   }
   __device__ bool in(int step, int k0) const { return pair_row(step * kStep<T> + k0) < hidden; }
@@ -175,22 +172,38 @@ __device__ inline void tile_at(const Grid &g, int t, int &mt, int &nt) {
 // An operand's part of a stage in LDS, B rows: B/16 loads of 1 KiB, dealt to the
 // waves in turns.
 //
-// k contiguous: 64 bytes a row; chunk c of row r lies at place c ^ (r / 2 & 3),
-// so that the 16 rows that a fragment read touches spread over the banks.
+// k contiguous: 64 bytes a row; chunk c of row r lies at place c ^ chunk_turn(r).
 //
-// Rows contiguous: kStep lines of B elements, in slots of 16 rows.  Four
-// 16-bit lines of a slot are what one transposing read of 16 lanes takes
-// (8 bytes each: lane q reads line q / 4, rows 4 (q % 4) on, and gets row q of
-// the four lines), in single precision a line's slot is one read.  The slots
-// of a line are permuted by the line's number so that lines read together
-// spread over the banks.
+// Rows contiguous: kStep lines of B elements, in slots of 16 rows, a slot in
+// 16-byte parts.  Four 16-bit lines of a slot are what one transposing read of
+// 16 lanes takes (8 bytes each: lane q reads line q / 4, four rows, and gets
+// one row of the four lines); in single precision a line's slot is one read.
+// Slots and parts of a line are permuted by the line's number.
 //
-// Measured: no bank conflicts with either layout.
-__device__ inline int chunk_turn(int row) { return (row >> 1) & 3; }
+// The permutations spread what is read together over the banks, for the 16
+// neighbouring rows of a fragment of L as for the four times four rows that a
+// fragment of R may take (Order).
+__device__ inline int chunk_turn(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 2); }
 template <typename T, int B>
 __device__ inline int slot_turn(int line) {
-  return (sizeof(T) == 2 ? (line & 3) | ((line >> 1) & 4) : (line >> 2) & 3) & (B / 16 - 1);
+  return (sizeof(T) == 2 ? (line & 1) << 2 | (line & 2) | (line >> 3 & 1) : line >> 2 & 3) & (B / 16 - 1);
 }
+template <typename T>
+__device__ inline int part_turn(int line) {
+  return sizeof(T) == 2 ? line >> 1 & 1 : line >> 2 & 3;
+}
+
+// Which row of R, in the wave's part, is row q of its fragment j, and so which
+// columns of C lane group g (of 16 lanes) holds: with Runs eight neighbouring
+// ones in two fragments, which 16-bit results are stored by (16 bytes a lane,
+// 64 a row); else four of every 16, for single-precision ones.
+template <bool Runs>
+struct Order {
+  static __device__ int row(int j, int q) {
+    return Runs ? (j >> 1) * 32 + (q >> 2) * 8 + (j & 1) * 4 + (q & 3) : j * 16 + q;
+  }
+  static __device__ int col(int j, int g) { return Runs ? (j >> 1) * 32 + g * 8 + (j & 1) * 4 : j * 16 + g * 4; }
+};
 
 template <typename T, int B, int WAVES, typename Op>
 struct Stage {
@@ -207,7 +220,7 @@ struct Stage {
 
   __device__ void aim(const Op &op, int row0, int wave, int lane) {
     if (Op::kContiguous) {
-      k0 = ((lane & 3) ^ chunk_turn(lane >> 2)) * kChunk<T>;
+      k0 = ((lane & 3) ^ chunk_turn(wave * 16 + (lane >> 2))) * kChunk<T>;  // the same in every load
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) src[i] = op.base(row0 + (i * WAVES + wave) * 16 + (lane >> 2), k0);
     } else {
@@ -217,7 +230,7 @@ struct Stage {
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         const int line = k0 + i * NEXT, slot = (part / per_slot) ^ slot_turn<T, B>(line);
-        src[i] = op.base(row0 + slot * 16 + part % per_slot * kChunk<T>, line);
+        src[i] = op.base(row0 + slot * 16 + ((part % per_slot) ^ part_turn<T>(line)) * kChunk<T>, line);
       }
     }
   }
@@ -239,29 +252,31 @@ struct Stage {
         (lds_ptr)((to) + (i_ * decltype(stage)::WAVES_ + wave) * 1024), 16, 0, 0);                           \
   } while (0)
 
-#define READ_FRAGMENTS(stage, f, count, tile, row0)                                                          \
-  do {                                                                                                       \
-    typedef decltype(stage) S_;                                                                              \
-    const int q_ = lane & 15, group_ = lane >> 4;                                                            \
-    _Pragma("unroll") for (int i_ = 0; i_ < (count); ++i_) {                                                 \
-      const int slot_ = ((row0) >> 4) + i_;                                                                  \
-      if constexpr (S_::CONTIGUOUS) {                                                                        \
-        (f)[i_] = *(const lds_u32x4 *)((tile) + (slot_ * 16 + q_) * 64 + (group_ ^ chunk_turn(q_)) * 16);    \
-      } else if constexpr (sizeof(T) == 2) {                                                                 \
-        const int line_ = group_ * 8 + (q_ >> 2);                                                            \
-        const int at_ = line_ * S_::LINE + (slot_ ^ slot_turn<T, S_::ROWS>(line_)) * 32 + (q_ & 3) * 8;      \
-        const s16x4 lo_ = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((tile) + at_));              \
-        const s16x4 hi_ = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((tile) + at_ + 4 * S_::LINE)); \
-        const u32x2 l_ = __builtin_bit_cast(u32x2, lo_), h_ = __builtin_bit_cast(u32x2, hi_);                \
-        (f)[i_] = u32x4{l_[0], l_[1], h_[0], h_[1]};                                                         \
-      } else {                                                                                               \
-        _Pragma("unroll") for (int e_ = 0; e_ < 4; ++e_) {                                                   \
-          const int line_ = group_ * 4 + e_;                                                                 \
-          (f)[i_][e_] = *(const lds_u32 *)((tile) + line_ * S_::LINE +                                       \
-                                           (slot_ ^ slot_turn<T, S_::ROWS>(line_)) * 64 + q_ * 4);           \
-        }                                                                                                    \
-      }                                                                                                      \
-    }                                                                                                        \
+#define READ_FRAGMENTS(stage, order, f, count, tile, row0)                                                            \
+  do {                                                                                                                \
+    typedef decltype(stage) S_;                                                                                       \
+    const int q_ = lane & 15, group_ = lane >> 4;                                                                     \
+    _Pragma("unroll") for (int i_ = 0; i_ < (count); ++i_) {                                                          \
+      if constexpr (S_::CONTIGUOUS) {                                                                                 \
+        const int row_ = (row0) + order::row(i_, q_);                                                                 \
+        (f)[i_] = *(const lds_u32x4 *)((tile) + row_ * 64 + (group_ ^ chunk_turn(row_)) * 16);                        \
+      } else if constexpr (sizeof(T) == 2) {                                                                          \
+        /* lane q reads four rows of line q / 4: those that lanes 4 (q % 4) on get */                                 \
+        const int line_ = group_ * 8 + (q_ >> 2), row_ = (row0) + order::row(i_, (q_ & 3) * 4);                       \
+        const int at_ = line_ * S_::LINE + ((row_ >> 4) ^ slot_turn<T, S_::ROWS>(line_)) * 32 +                       \
+                        (((row_ & 15) * 2) ^ (part_turn<T>(line_) * 16));                                             \
+        const s16x4 lo_ = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((tile) + at_));                       \
+        const s16x4 hi_ = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((tile) + at_ + 4 * S_::LINE));        \
+        const u32x2 l_ = __builtin_bit_cast(u32x2, lo_), h_ = __builtin_bit_cast(u32x2, hi_);                         \
+        (f)[i_] = u32x4{l_[0], l_[1], h_[0], h_[1]};                                                                  \
+      } else {                                                                                                        \
+        _Pragma("unroll") for (int e_ = 0; e_ < 4; ++e_) {                                                            \
+          const int line_ = group_ * 4 + e_, row_ = (row0) + order::row(i_, q_);                                      \
+          (f)[i_][e_] = *(const lds_u32 *)((tile) + line_ * S_::LINE + ((row_ >> 4) ^ slot_turn<T, S_::ROWS>(line_)) * 64 +\
+                                           (((row_ >> 2 & 3) ^ part_turn<T>(line_)) * 16 + (row_ & 3) * 4));          \
+        }                                                                                                             \
+      }                                                                                                               \
+    }                                                                                                                 \
   } while (0)
 
 // Every wave's reads and its older loads are done; those of the last `Flying`
@@ -293,6 +308,8 @@ __device__ inline void walk_tiles(const Grid &g, const L &left, const R &right, 
   typedef Stage<T, BM, WAVES, L> StageL;
   typedef Stage<T, BN, WAVES, R> StageR;
   constexpr int LOADS = StageL::LOADS + StageR::LOADS;
+  typedef Order<false> OrderL;
+  typedef Order<Epilogue::kRuns> OrderR;
 
   // this workgroup's items (a tile and a split of k): every width-th of its
   // die's run of them
@@ -340,8 +357,8 @@ __device__ inline void walk_tiles(const Grid &g, const L &left, const R &right, 
   }
   stage_barrier<0>();
   u32x4 al[MI], ar[NI], bl[MI], br[NI];
-  READ_FRAGMENTS(from_l, al, MI, data, wm * TM);
-  READ_FRAGMENTS(from_r, ar, NI, data + BM * 64, wn * TN);
+  READ_FRAGMENTS(from_l, OrderL, al, MI, data, wm * TM);
+  READ_FRAGMENTS(from_r, OrderR, ar, NI, data + BM * 64, wn * TN);
   int slot = 0;  // the stage of the step that is multiplied
   for (; item < last; item += width) {
     int mt, nt;
@@ -357,15 +374,15 @@ __device__ inline void walk_tiles(const Grid &g, const L &left, const R &right, 
     for (int steps = min(g.split, g.steps - split * g.split); steps > 0; steps -= 2) {
       stage_barrier<2 * LOADS>();
       const int odd = (slot + 1) & 3, even = (slot + 2) & 3;
-      READ_FRAGMENTS(from_l, bl, MI, data + odd * STAGE, wm * TM);
-      READ_FRAGMENTS(from_r, br, NI, data + odd * STAGE + BM * 64, wn * TN);
+      READ_FRAGMENTS(from_l, OrderL, bl, MI, data + odd * STAGE, wm * TM);
+      READ_FRAGMENTS(from_r, OrderR, br, NI, data + odd * STAGE + BM * 64, wn * TN);
       LOAD_STEP(from_l, left, ahead_step, fill + slot * STAGE);
       LOAD_STEP(from_r, right, ahead_step, fill + slot * STAGE + BM * 64);
       multiply(al, ar);
       advance();
       stage_barrier<2 * LOADS>();
-      READ_FRAGMENTS(from_l, al, MI, data + even * STAGE, wm * TM);
-      READ_FRAGMENTS(from_r, ar, NI, data + even * STAGE + BM * 64, wn * TN);
+      READ_FRAGMENTS(from_l, OrderL, al, MI, data + even * STAGE, wm * TM);
+      READ_FRAGMENTS(from_r, OrderR, ar, NI, data + even * STAGE + BM * 64, wn * TN);
       LOAD_STEP(from_l, left, ahead_step, fill + odd * STAGE);
       LOAD_STEP(from_r, right, ahead_step, fill + odd * STAGE + BM * 64);
       multiply(bl, br);
@@ -426,27 +443,47 @@ __device__ inline f32x4 load4(const T *p, int count, bool whole) {
   return v;
 }
 
+// Stores the columns of C that a lane of group g holds, in a row that ends at
+// `cols`: with Runs and 16-bit types eight at a time.  `by` is how many
+// elements of the row can be stored at once: 8, 4 or 1.
+template <bool Runs, typename T, int NI, typename Value>
+__device__ inline void store_row(T *row, int n0, int g, int cols, int by, Value value) {
+#pragma unroll
+  for (int j = 0; j < NI; j += 2) {
+    const int c = n0 + Order<Runs>::col(j, g), d = n0 + Order<Runs>::col(j + 1, g);
+    const f32x4 a = value(j), b = value(j + 1);
+    if (Runs && sizeof(T) == 2 && by == 8 && c + 8 <= cols) {
+      typedef T vec __attribute__((ext_vector_type(8)));
+      *reinterpret_cast<vec *>(row + c) = vec{T(a[0]), T(a[1]), T(a[2]), T(a[3]), T(b[0]), T(b[1]), T(b[2]), T(b[3])};
+    } else {
+      if (c < cols) store4(row + c, a, cols - c, by >= 4);
+      if (d < cols) store4(row + d, b, cols - d, by >= 4);
+    }
+  }
+}
+
 // Where row m of a product's result goes: a matrix, or w_gate's and w_value's
-// gradients in turns of 16 rows (pair_row).
+// gradients in turns of four rows (pair_row).
 template <typename T>
 struct Target {
   T *p, *q;
   int64_t ld;
   int rows;  // of p (and q)
   bool pair;
-  bool whole;           // four columns can be stored at once
+  int by;               // columns that can be stored at once
   const float *factor;  // of the result, on the device: one for all (step 0) or one a row (step 1); NULL = 1
   int factor_step;
   __device__ float scale(int m) const { return factor ? factor[m * factor_step] : 1.0f; }
   __device__ T *row(int m) const {
     const int f = pair ? pair_row(m) : m;
     if (f >= rows) return nullptr;
-    return (pair && (m & 16) ? q : p) + f * ld;
+    return (pair && (m & 4) ? q : p) + f * ld;
   }
 };
 
 template <typename T>
 struct Store {
+  static constexpr bool kRuns = sizeof(T) == 2;
   Target<T> out;
   int cols;
   template <int MI, int NI>
@@ -458,11 +495,7 @@ struct Store {
       T *row = out.row(m);
       if (!row) continue;
       const float f = out.scale(m);
-#pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        const int n = at.n0 + j * 16 + (at.lane >> 4) * 4;
-        if (n < cols) store4(row + n, c[i][j] * f, cols - n, out.whole);
-      }
+      store_row<kRuns, T, NI>(row, at.n0, at.lane >> 4, cols, out.by, [&](int j) { return c[i][j] * f; });
     }
   }
 };
@@ -471,6 +504,7 @@ struct Store {
 // what an earlier launch left there if Add.
 template <bool Add>
 struct StorePart {
+  static constexpr bool kRuns = false;
   float *part;
   int rows, cols4;
   template <int MI, int NI>
@@ -483,7 +517,7 @@ struct StorePart {
       float *row = part + (int64_t(at.split) * rows + m) * cols4;
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
-        const int n = at.n0 + j * 16 + (at.lane >> 4) * 4;
+        const int n = at.n0 + Order<kRuns>::col(j, at.lane >> 4);
         if (n >= cols4) continue;
         f32x4 *p = reinterpret_cast<f32x4 *>(row + n);
         if constexpr (Add) *p += c[i][j];
@@ -522,6 +556,7 @@ __device__ inline void gate(int act, float a, float &p, float &dp) {
 
 template <typename T>
 struct GatedForward {
+  static constexpr bool kRuns = true;
   T *h;
   int64_t ld;
   int rows, hidden, act;
@@ -534,8 +569,8 @@ struct GatedForward {
       const int m = at.m0 + i * 16 + (at.lane & 15);
       if (m >= rows) continue;
 #pragma unroll
-      for (int j = 0; j < NI; j += 2) {
-        const int f = pair_row(at.n0 + j * 16) + (at.lane >> 4) * 4;
+      for (int j = 0; j < NI; j += 2) {  // a and b of the same four columns
+        const int f = pair_row(at.n0 + Order<kRuns>::col(j, at.lane >> 4));
         if (f >= hidden) continue;
         f32x4 v;
 #pragma unroll
@@ -550,10 +585,11 @@ struct GatedForward {
   }
 };
 
-// da and db in turns of 16 columns (pair_row), zero past `hidden`: operands of
+// da and db in turns of four columns (pair_row), zero past `hidden`: operands of
 // the backward products.
 template <typename T>
 struct GatedBackward {
+  static constexpr bool kRuns = true;
   const T *dh;
   int64_t ld;
   T *dab;  // [rows][pair_cols]
@@ -566,23 +602,20 @@ struct GatedBackward {
       one_row_at_a_time();
       const int m = at.m0 + i * 16 + (at.lane & 15);
       if (m >= rows) continue;
+      f32x4 d[NI];
 #pragma unroll
       for (int j = 0; j < NI; j += 2) {
-        const int n = at.n0 + j * 16 + (at.lane >> 4) * 4, f = pair_row(n);
-        if (n >= pair_cols) continue;
-        const f32x4 d = load4(dh + m * ld + f, hidden - f, whole);
-        f32x4 da, db;
+        const int f = pair_row(at.n0 + Order<kRuns>::col(j, at.lane >> 4));
+        const f32x4 dhv = load4(dh + m * ld + f, hidden - f, whole);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           float p, dp;
           gate(act, c[i][j][r], p, dp);
-          da[r] = f + r < hidden ? d[r] * c[i][j + 1][r] * dp : 0.0f;
-          db[r] = f + r < hidden ? d[r] * p : 0.0f;
+          d[j][r] = f + r < hidden ? dhv[r] * c[i][j + 1][r] * dp : 0.0f;
+          d[j + 1][r] = f + r < hidden ? dhv[r] * p : 0.0f;
         }
-        T *out = dab + int64_t(m) * pair_cols + n;
-        store4(out, da, 4, true);
-        store4(out + 16, db, 4, true);
       }
+      store_row<kRuns, T, NI>(dab + int64_t(m) * pair_cols, at.n0, at.lane >> 4, pair_cols, 8, [&](int j) { return d[j]; });
     }
   }
 };
@@ -597,30 +630,33 @@ __device__ inline float2 softmax_join(float2 a, float2 b) {
 
 // The bias of a lane's words; -inf past the vocabulary, where the products are
 // of some row of the weights that is in it.
-template <int NI>
+template <bool Runs, int NI>
 __device__ inline void word_bias(f32x4 (&b)[NI], const float *bias, int n0, int lane, int first, int vocab) {
 #pragma unroll
   for (int j = 0; j < NI; ++j)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int v = first + n0 + j * 16 + (lane >> 4) * 4 + r;
+      const int v = first + n0 + Order<Runs>::col(j, lane >> 4) + r;
       b[j][r] = bias ? bias[min(v, vocab - 1)] : 0.0f;
       if (v >= vocab) b[j][r] = -INFINITY;
     }
 }
 
-// Where a row's label is among the wave's words, if this lane holds it: the
-// word's index, else -1.
-template <int NI>
+// Where a row's label is among the wave's words, if this lane holds it: 4 j + r,
+// else -1.
+template <bool Runs, int NI>
 __device__ inline int label_at(int label, int n0, int lane, int first, int vocab) {
-  const int at = label - first - n0 - (lane >> 4) * 4;
-  return label >= 0 && label < vocab && at >= 0 && at < NI * 16 && (at & 12) == 0 ? at : -1;
+  const int at = label - first - n0;
+  if (label < 0 || label >= vocab || at < 0 || at >= NI * 16) return -1;
+  if (Runs) return (at >> 3 & 3) == lane >> 4 ? (at >> 5) * 8 + (at & 7) : -1;
+  return (at >> 2 & 3) == lane >> 4 ? (at >> 4) * 4 + (at & 3) : -1;
 }
 
 // Per row and tile of words: the largest logit and the sum of exp(z - it), and
 // the label's logit from the lane that holds it.
 template <int BM, int WN>
 struct SoftmaxPart {
+  static constexpr bool kRuns = false;
   const float *bias;
   const int32_t *labels;
   float *label_logit;  // [rows]
@@ -630,7 +666,7 @@ struct SoftmaxPart {
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
     float2 *shared = reinterpret_cast<float2 *>(at.lds);  // [WN][BM]
     f32x4 b[NI];
-    word_bias(b, bias, at.n0, at.lane, 0, vocab);
+    word_bias<kRuns>(b, bias, at.n0, at.lane, 0, vocab);
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       one_row_at_a_time();
@@ -638,13 +674,13 @@ struct SoftmaxPart {
 #pragma unroll
       for (int j = 0; j < NI; ++j) z[j] = c[i][j] + b[j];
       const int m = at.m0 + i * 16 + (at.lane & 15);
-      const int hit = label_at<NI>(m < rows ? labels[m] : -1, at.n0, at.lane, 0, vocab);
+      const int hit = label_at<kRuns, NI>(m < rows ? labels[m] : -1, at.n0, at.lane, 0, vocab);
       if (__ballot(hit >= 0)) {
 #pragma unroll
         for (int j = 0; j < NI; ++j)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (hit == j * 16 + r) label_logit[m] = z[j][r];
+            if (hit == j * 4 + r) label_logit[m] = z[j][r];
       }
       float top = -INFINITY;
 #pragma unroll
@@ -692,6 +728,7 @@ constexpr float kGradUnit<f16> = 16384.0f;
 
 template <typename T, int BN, int WM>
 struct SoftmaxGrad {
+  static constexpr bool kRuns = true;
   const float *bias;
   const int32_t *labels;
   const float *lse, *row_factor;  // row_factor: dloss / S, 0 for a row that is left out
@@ -702,7 +739,7 @@ struct SoftmaxGrad {
   template <int MI, int NI>
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
     f32x4 b[NI], sums[NI];
-    word_bias(b, bias, at.n0, at.lane, first, vocab);
+    word_bias<kRuns>(b, bias, at.n0, at.lane, first, vocab);
 #pragma unroll
     for (int j = 0; j < NI; ++j) sums[j] = f32x4{0, 0, 0, 0};
 #pragma unroll
@@ -718,20 +755,18 @@ struct SoftmaxGrad {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           z[j][r] = kept ? __builtin_amdgcn_exp2f((c[i][j][r] + b[j][r] - l) * kLog2e + kGradLog2<T>) : 0.0f;
-      const int hit = kept ? label_at<NI>(label, at.n0, at.lane, first, vocab) : -1;
+      const int hit = kept ? label_at<kRuns, NI>(label, at.n0, at.lane, first, vocab) : -1;
       if (__ballot(hit >= 0)) {
 #pragma unroll
         for (int j = 0; j < NI; ++j)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (hit == j * 16 + r) z[j][r] -= kGradUnit<T>;
+            if (hit == j * 4 + r) z[j][r] -= kGradUnit<T>;
       }
 #pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        const int n = at.n0 + j * 16 + (at.lane >> 4) * 4;
-        if (m < rows && n < ldg) store4(grad + m * ldg + n, z[j], 4, true);
-        sums[j] += z[j] * d;
-      }
+      for (int j = 0; j < NI; ++j) sums[j] += z[j] * d;
+      if (m < rows)
+        store_row<kRuns, T, NI>(grad + m * ldg, at.n0, at.lane >> 4, int(ldg), 8, [&](int j) { return z[j]; });
     }
     if (!col_part) return;
     float *shared = reinterpret_cast<float *>(at.lds);  // [WM][BN]
@@ -742,7 +777,7 @@ struct SoftmaxGrad {
         float s = sums[j][r];
 #pragma unroll
         for (int x = 1; x < 16; x <<= 1) s += __shfl_xor(s, x);
-        if ((at.lane & 15) == 0) shared[at.wm * BN + at.wn * NI * 16 + j * 16 + (at.lane >> 4) * 4 + r] = s;
+        if ((at.lane & 15) == 0) shared[at.wm * BN + at.wn * NI * 16 + Order<kRuns>::col(j, at.lane >> 4) + r] = s;
       }
     __syncthreads();
     const int n = at.nt * BN + int(threadIdx.x);
@@ -982,7 +1017,7 @@ __global__ __launch_bounds__(256) void k_join(const float *part, int splits, int
     f32x4 s = *reinterpret_cast<const f32x4 *>(part + at);
     for (int z = 1; z < splits; ++z) s += *reinterpret_cast<const f32x4 *>(part + z * all + at);
     s *= out.scale(m);
-    store4(row + n, s, cols - n, out.whole);
+    store4(row + n, s, cols - n, out.by >= 4);
   }
 }
 
@@ -1020,9 +1055,12 @@ unsigned strided(int64_t workgroups) { return unsigned(workgroups < 65536 ? work
     if (e_ != hipSuccess) return e_;       \
   } while (0)
 
+// How many elements of a row can be moved at once: 8, 4 or 1.
 template <typename T>
-bool whole4(const void *p, int64_t ld) {
-  return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0 && ld % 4 == 0;
+int at_once(const void *p, int64_t ld) {
+  for (int n : {8, 4})
+    if (reinterpret_cast<uintptr_t>(p) % (n * sizeof(T) < 16 ? n * sizeof(T) : 16) == 0 && ld % n == 0) return n;
+  return 1;
 }
 
 // Whether an operand can be read where it lies: its rows start at multiples of
@@ -1195,7 +1233,7 @@ hipError_t gated_forward_t(const lda_gated_args &a, Arena &ws, bool dry) {
   OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
   OPS_TRY(pair_operands<T>(a, false, ws, dry, s, gate, value));
   if (dry) return hipSuccess;
-  const GatedForward<T> epi{static_cast<T *>(a.h), a.ldh, rows, a.hidden, a.act, whole4<T>(a.h, a.ldh)};
+  const GatedForward<T> epi{static_cast<T *>(a.h), a.ldh, rows, a.hidden, a.act, at_once<T>(a.h, a.ldh) >= 4};
   return with_shape(Tiles(a.rows, pair_cols(a.hidden)), [&](auto shape) {
     return product<T, decltype(shape)>(a.rows, pair_cols(a.hidden), k, 1, Rows<T>{x.p, x.ld, rows, k},
                                        PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s);
@@ -1218,16 +1256,17 @@ hipError_t gated_backward_t(const lda_gated_args &a, Arena &ws, bool dry) {
   T *dab = ws.take<T>(a.rows * pc);
   if (!dry) {
     const GatedBackward<T> epi{static_cast<const T *>(a.dh), a.lddh, dab, rows, a.hidden, pc, a.act,
-                               whole4<T>(a.dh, a.lddh)};
+                               at_once<T>(a.dh, a.lddh) >= 4};
     OPS_TRY(with_shape(Tiles(a.rows, pc), [&](auto shape) {
       return product<T, decltype(shape)>(a.rows, pc, k, 1, Rows<T>{x.p, x.ld, rows, k},
                                          PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s);
     }));
   }
-  const Target<T> dx{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, whole4<T>(a.dx, a.lddx), nullptr, 0};
+  const Target<T> dx{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, at_once<T>(a.dx, a.lddx), nullptr, 0};
   OPS_TRY(product_into<T>(a.rows, a.width, pc, Rows<T>{dab, pc, rows, pc},
                           PairColumns<T>{gate.p, value.p, gate.ld, a.width, a.hidden}, dx, ws, dry, s));
-  const Target<T> dw{dwg, dwv, a.width, a.hidden, true, whole4<T>(dwg, a.width) && whole4<T>(dwv, a.width), nullptr, 0};
+  const int by_g = at_once<T>(dwg, a.width), by_v = at_once<T>(dwv, a.width);
+  const Target<T> dw{dwg, dwv, a.width, a.hidden, true, by_g < by_v ? by_g : by_v, nullptr, 0};
   return product_into<T>(pc, a.width, a.rows, Columns<T>{dab, pc, pc, rows}, Columns<T>{x.p, x.ld, a.width, rows}, dw,
                          ws, dry, s);
 }
@@ -1334,14 +1373,14 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
       }));
     }
     T *dwp = dw + int64_t(first) * a.width;
-    const Target<T> out{dwp, nullptr, a.width, words, false, whole4<T>(dwp, a.width), top, 0};
+    const Target<T> out{dwp, nullptr, a.width, words, false, at_once<T>(dwp, a.width), top, 0};
     OPS_TRY(product_into<T>(words, a.width, a.rows, Columns<T>{grad, words_k, words, rows},
                             Columns<T>{x_scaled, k, a.width, rows}, out, ws, dry, s));
     if (ws.used > most) most = ws.used;
   }
   ws.used = most;
   if (dry) return hipSuccess;
-  const Target<T> out{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, whole4<T>(a.dx, a.lddx), row_factor, 1};
+  const Target<T> out{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, at_once<T>(a.dx, a.lddx), row_factor, 1};
   k_join<T><<<strided(ceil_div(a.rows * cols4, 1024)), 256, 0, s>>>(dx_part, splits, rows, a.width, int(cols4), out);
   return hipGetLastError();
 }
