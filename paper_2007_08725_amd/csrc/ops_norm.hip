@@ -19,7 +19,6 @@ namespace {
 
 typedef __bf16 bf16;
 typedef _Float16 f16;
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 template <typename T>
 constexpr int kChunk = 16 / int(sizeof(T));
@@ -88,7 +87,6 @@ __device__ inline float2 row_sum(float2 s, float2 *shared) {
 }
 
 constexpr int threads_of(int lanes) { return lanes > 256 ? lanes : 256; }
-constexpr bool grad_in_registers(int threads, int columns) { return threads < 1024 || columns < 32; }
 
 template <typename T, int LANES, int V, bool Aligned>
 __global__ __launch_bounds__(threads_of(LANES)) void k_norm(const T *x, int64_t ldx, const T *weight, const T *bias,
@@ -152,25 +150,13 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_norm_grad(const T *dy, in
   constexpr int C = At::C, THREADS = threads_of(LANES), GROUPS = THREADS / LANES;
   __shared__ float2 shared[GROUPS > 1 ? THREADS * C : 16];
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
-  // The weight and both sums stay in registers.  With 32 columns a lane and
-  // 1,024 lanes (128 registers each) only one sum does: the weight is read from
-  // the caches and the sum of dy is kept in LDS, by the lane that owns it.
-  constexpr bool kHold = grad_in_registers(THREADS, V * C);
-  extern __shared__ f32x4 in_lds[];  // [V][C / 4][THREADS]
-  float sw[V][C], sb[kHold ? V : 1][C];
+  float sw[V][C], sb[V][C];
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
+  for (int i = 0; i < V; ++i)
 #pragma unroll
-    for (int e = 0; e < C; ++e) {
-      sw[i][e] = 0.0f;
-      if (kHold) sb[i][e] = 0.0f;
-    }
-    if (!kHold)
-#pragma unroll
-      for (int q = 0; q < C / 4; ++q) in_lds[(i * (C / 4) + q) * THREADS + threadIdx.x] = f32x4{0, 0, 0, 0};
-  }
+    for (int e = 0; e < C; ++e) sw[i][e] = sb[i][e] = 0.0f;
   Chunk<T> w[V];
-  if (kHold && weight) At::load(weight, cols, lane, w);
+  if (weight) At::load(weight, cols, lane, w);
   // every lane of a workgroup that meets at barriers has the same rows
   for (int64_t row = int64_t(blockIdx.x) * GROUPS + group; row < rows; row += int64_t(gridDim.x) * GROUPS) {
     Chunk<T> v[V], d[V];
@@ -180,7 +166,6 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_norm_grad(const T *dy, in
     float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      if (!kHold && weight) At::load_one(weight, cols, lane, i, w[i]);
 #pragma unroll
       for (int e = 0; e < C; ++e) {
         const float h = (v[i][e] - mu) * r;
@@ -189,13 +174,8 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_norm_grad(const T *dy, in
         s.x += g;
         s.y += g * h;
         sw[i][e] += d[i][e] * h;
-        if (kHold) sb[i][e] += d[i][e];
+        sb[i][e] += d[i][e];
       }
-      if (!kHold)
-#pragma unroll
-        for (int q = 0; q < C / 4; ++q)
-          in_lds[(i * (C / 4) + q) * THREADS + threadIdx.x] +=
-              f32x4{d[i][4 * q], d[i][4 * q + 1], d[i][4 * q + 2], d[i][4 * q + 3]};
     }
     s = row_sum<LANES>(s, shared);
     s.x /= cols;
@@ -203,7 +183,6 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_norm_grad(const T *dy, in
     T *out = dx + row * lddx;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      if (!kHold && weight) At::load_one(weight, cols, lane, i, w[i]);
       typename Chunk<T>::vec o;
 #pragma unroll
       for (int e = 0; e < C; ++e) {
@@ -222,7 +201,7 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_norm_grad(const T *dy, in
       // the groups' sums, in the order of the groups
       __syncthreads();
 #pragma unroll
-      for (int e = 0; e < C; ++e) shared[e * THREADS + threadIdx.x] = make_float2(sw[i][e], sb[kHold ? i : 0][e]);
+      for (int e = 0; e < C; ++e) shared[e * THREADS + threadIdx.x] = make_float2(sw[i][e], sb[i][e]);
       __syncthreads();
       for (int at = threadIdx.x; at < LANES * C; at += THREADS) {
         const int e = at % C, l = at / C, c = At::first(i, l) + e;
@@ -244,7 +223,7 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_norm_grad(const T *dy, in
         const int c = At::first(i, lane) + e;
         if (c < cols) {
           pw[c] = sw[i][e];
-          pb[c] = kHold ? sb[kHold ? i : 0][e] : in_lds[(i * (C / 4) + e / 4) * THREADS + threadIdx.x][e % 4];
+          pb[c] = sb[i][e];
         }
       }
     }
@@ -297,45 +276,81 @@ __global__ __launch_bounds__(1024) void k_norm_wide(const T *x, int64_t ldx, con
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(1024) void k_norm_wide_dx(const T *dy, int64_t lddy, const T *x, int64_t ldx,
-                                                       const T *weight, const float *mean, const float *rstd, int cols,
-                                                       T *dx, int64_t lddx) {
+// The backward pass in two kernels: the rows' two sums (sums [2][rows]: mean g,
+// mean g h), then strips of 256 chunks of the columns over `per` rows each, which
+// give dx and the parts [2][gridDim.y][cols] of dweight and dbias.  x and dy are
+// read twice, but a lane keeps one chunk's sums: all columns of such a row kept
+// by 512 or 1,024 lanes need more registers than there are (measured at 32,768
+// columns of 16 bits: 402 to 680 us in one kernel, against 290 here).
+template <typename T, bool Aligned>
+__global__ __launch_bounds__(1024) void k_norm_wide_sums(const T *dy, int64_t lddy, const T *x, int64_t ldx,
+                                                         const T *weight, const float *mean, const float *rstd,
+                                                         int64_t rows, int cols, float *sums) {
+  typedef Cols<T, 1024, 1, Aligned> At;
+  constexpr int C = At::C;
   __shared__ float2 shared[16];
-  const T *row = x + int64_t(blockIdx.x) * ldx, *grad = dy + int64_t(blockIdx.x) * lddy;
-  const float mu = mean[blockIdx.x], r = rstd[blockIdx.x];
+  const int64_t row = blockIdx.x;
+  const float mu = mean[row], r = rstd[row];
   float2 s = make_float2(0.0f, 0.0f);
-  for (int c = threadIdx.x; c < cols; c += 1024) {
-    const float g = float(grad[c]) * (weight ? float(weight[c]) : 1.0f);
-    s.x += g;
-    s.y += g * (float(row[c]) - mu) * r;
+#pragma unroll 2
+  for (int c = 0; c < cols; c += 1024 * C) {
+    Chunk<T> v, d, w;
+    At::load_one(x + row * ldx + c, cols - c, threadIdx.x, 0, v);
+    At::load_one(dy + row * lddy + c, cols - c, threadIdx.x, 0, d);
+    if (weight) At::load_one(weight + c, cols - c, threadIdx.x, 0, w);
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+      const float g = weight ? d[e] * w[e] : d[e];
+      s.x += g;
+      s.y += g * ((v[e] - mu) * r);
+    }
   }
   s = row_sum<1024>(s, shared);
-  s.x /= cols;
-  s.y /= cols;
-  T *out = dx + int64_t(blockIdx.x) * lddx;
-  for (int c = threadIdx.x; c < cols; c += 1024) {
-    const float g = float(grad[c]) * (weight ? float(weight[c]) : 1.0f);
-    out[c] = T(r * (g - s.x - (float(row[c]) - mu) * r * s.y));
+  if (threadIdx.x == 0) {
+    sums[row] = s.x / cols;
+    sums[rows + row] = s.y / cols;
   }
 }
 
-// Column sums of dy h and dy over `per` rows a workgroup: part[2][gridDim.y][cols].
-template <typename T>
-__global__ __launch_bounds__(256) void k_norm_wide_dw(const T *dy, int64_t lddy, const T *x, int64_t ldx,
-                                                      const float *mean, const float *rstd, int64_t rows, int cols,
-                                                      int64_t per, float *part) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= cols) return;
-  const int64_t first = blockIdx.y * per, last = first + per < rows ? first + per : rows;
-  float sw = 0.0f, sb = 0.0f;
-  for (int64_t r = first; r < last; ++r) {
-    const float g = float(dy[r * lddy + c]);
-    sb += g;
-    sw += g * (float(x[r * ldx + c]) - mean[r]) * rstd[r];
+template <typename T, bool Aligned>
+__global__ __launch_bounds__(256) void k_norm_wide_grad(const T *dy, int64_t lddy, const T *x, int64_t ldx,
+                                                        const T *weight, const float *mean, const float *rstd,
+                                                        const float *sums, int64_t rows, int cols, int64_t per, T *dx,
+                                                        int64_t lddx, float *part) {
+  typedef Cols<T, 256, 1, Aligned> At;
+  constexpr int C = At::C;
+  const int first = blockIdx.x * 256 * C, mine = cols - first;  // the strip's first column, and the columns from it on
+  const int lane = threadIdx.x, c = At::first(0, lane);
+  Chunk<T> w;
+  if (weight) At::load_one(weight + first, mine, lane, 0, w);
+  float sw[C], sb[C];
+#pragma unroll
+  for (int e = 0; e < C; ++e) sw[e] = sb[e] = 0.0f;
+  const int64_t from = blockIdx.y * per, to = from + per < rows ? from + per : rows;
+#pragma unroll 4
+  for (int64_t row = from; row < to; ++row) {
+    Chunk<T> v, d;
+    At::load_one(x + row * ldx + first, mine, lane, 0, v);
+    At::load_one(dy + row * lddy + first, mine, lane, 0, d);
+    const float mu = mean[row], r = rstd[row], mg = sums[row], mh = sums[rows + row];
+    typename Chunk<T>::vec o;
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+      const float h = (v[e] - mu) * r;
+      const float g = weight ? d[e] * w[e] : d[e];
+      sw[e] += d[e] * h;
+      sb[e] += d[e];
+      o[e] = T(r * (g - mg - h * mh));
+    }
+    At::store(dx + row * lddx + first, mine, c, o);
   }
-  part[int64_t(blockIdx.y) * cols + c] = sw;
-  part[(int64_t(gridDim.y) + blockIdx.y) * cols + c] = sb;
+  if (!part) return;
+#pragma unroll
+  for (int e = 0; e < C; ++e)
+    if (c + e < mine) {
+      part[int64_t(blockIdx.y) * cols + first + c + e] = sw[e];
+      part[(int64_t(gridDim.y) + blockIdx.y) * cols + first + c + e] = sb[e];
+    }
 }
 
 // ------------------------------------------------------------------- host ---
@@ -347,8 +362,10 @@ struct Shape {
 
 // Calls fn with the lanes that share a row of `chunks` 16-byte chunks and the
 // chunks that each holds; false if no lanes hold them all.  A wave a row up to
-// 256 chunks (of 8 lanes up to 8), then workgroups of 256 and of 1,024 threads.
-template <bool Aligned, typename Fn>
+// 256 chunks (of 8 lanes up to 8), then workgroups of 256 threads, then of 1,024
+// in the forward pass and of 512 in the backward pass, whose lanes need more
+// registers: two sums of each column.
+template <bool Aligned, bool Grad, typename Fn>
 bool with_lanes(int64_t chunks, Fn fn) {
   if (chunks <= 8) fn(Shape<8, 1, Aligned>());
   else if (chunks <= 64) fn(Shape<64, 1, Aligned>());
@@ -356,16 +373,22 @@ bool with_lanes(int64_t chunks, Fn fn) {
   else if (chunks <= 256) fn(Shape<64, 4, Aligned>());
   else if (chunks <= 512) fn(Shape<256, 2, Aligned>());
   else if (chunks <= 1024) fn(Shape<256, 4, Aligned>());
-  else if (chunks <= 2048) fn(Shape<1024, 2, Aligned>());
-  else if (chunks <= 4096) fn(Shape<1024, 4, Aligned>());
-  else return false;
+  else if (chunks <= 2048) fn(Shape<Grad ? 512 : 1024, Grad ? 4 : 2, Aligned>());
+  else {
+    if constexpr (!Grad)
+      if (chunks <= 4096) {
+        fn(Shape<1024, 4, Aligned>());
+        return true;
+      }
+    return false;
+  }
   return true;
 }
 
-template <typename T, typename Fn>
+template <typename T, bool Grad, typename Fn>
 bool with_shape(bool aligned, int cols, Fn fn) {
   const int64_t chunks = ceil_div(cols, kChunk<T>);
-  return aligned ? with_lanes<true>(chunks, fn) : with_lanes<false>(chunks, fn);
+  return aligned ? with_lanes<true, Grad>(chunks, fn) : with_lanes<false, Grad>(chunks, fn);
 }
 
 template <typename T>
@@ -381,7 +404,7 @@ hipError_t norm_forward_t(const lda_norm_args &a) {
   T *y = static_cast<T *>(a.y);
   const bool aligned = a.cols % kChunk<T> == 0 && aligned16<T>(x, a.ldx) && aligned16<T>(y, a.ldy) &&
                        aligned16<T>(w, 0) && aligned16<T>(b, 0);
-  const bool done = with_shape<T>(aligned, a.cols, [&](auto shape) {
+  const bool done = with_shape<T, false>(aligned, a.cols, [&](auto shape) {
     typedef decltype(shape) S;
     constexpr int threads = threads_of(S::LANES);
     k_norm<T, S::LANES, S::V, S::Aligned><<<unsigned(ceil_div(a.rows, threads / S::LANES)), threads, 0, s>>>(
@@ -402,38 +425,37 @@ hipError_t norm_backward_t(const lda_norm_args &a, Arena &ws, bool dry) {
   hipError_t e = hipSuccess;
   int64_t parts = 0;
   float *part = nullptr;
-  const bool done = with_shape<T>(aligned, a.cols, [&](auto shape) {
+  const bool done = with_shape<T, true>(aligned, a.cols, [&](auto shape) {
     typedef decltype(shape) S;
     constexpr int threads = threads_of(S::LANES), groups = threads / S::LANES;
     // workgroups: enough to fill the device, each with several rows, so that
     // the parts stay small beside x and dy
-    const int64_t most = threads == 1024 ? 256 : 1024;
+    const int64_t most = threads == 512 ? 256 : 1024;
     parts = ceil_div(a.rows, groups * 4);
     parts = parts > most ? most : parts < 1 ? 1 : parts;
     part = a.dweight ? ws.take<float>(2 * parts * a.cols) : nullptr;
     if (dry) return;
-    auto kernel = k_norm_grad<T, S::LANES, S::V, S::Aligned>;
-    constexpr size_t lds = grad_in_registers(threads, S::V * kChunk<T>) ? 0 : threads * S::V * kChunk<T> * sizeof(float);
-    if (lds) {
-      static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
-                                                            hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
-      e = allowed;
-      if (e != hipSuccess) return;
-    }
-    kernel<<<unsigned(parts), threads, lds, s>>>(dy, a.lddy, x, a.ldx, w, a.mean, a.rstd, a.rows, a.cols, dx, a.lddx,
-                                                 part);
+    k_norm_grad<T, S::LANES, S::V, S::Aligned><<<unsigned(parts), threads, 0, s>>>(
+        dy, a.lddy, x, a.ldx, w, a.mean, a.rstd, a.rows, a.cols, dx, a.lddx, part);
     e = hipGetLastError();
   });
   if (!done) {
-    parts = a.rows < 64 ? (a.rows ? a.rows : 1) : 64;
+    const int64_t strips = ceil_div(a.cols, 256 * kChunk<T>);
+    // about 2,048 workgroups, each with at least eight rows
+    const int64_t per = a.rows * strips > 16384 ? ceil_div(a.rows * strips, 2048) : 8;
+    parts = a.rows ? ceil_div(a.rows, per) : 1;
     part = a.dweight ? ws.take<float>(2 * parts * a.cols) : nullptr;
-    if (!dry && a.rows) {
-      k_norm_wide_dx<T><<<unsigned(a.rows), 1024, 0, s>>>(dy, a.lddy, x, a.ldx, w, a.mean, a.rstd, a.cols, dx, a.lddx);
-      e = hipGetLastError();
-    }
-    if (!dry && part && e == hipSuccess) {
-      k_norm_wide_dw<T><<<dim3(unsigned(ceil_div(a.cols, 256)), unsigned(parts)), 256, 0, s>>>(
-          dy, a.lddy, x, a.ldx, a.mean, a.rstd, a.rows, a.cols, ceil_div(a.rows, parts), part);
+    float *sums = ws.take<float>(2 * a.rows);
+    if (!dry) {
+      if (a.rows) {
+        auto kernel = aligned ? k_norm_wide_sums<T, true> : k_norm_wide_sums<T, false>;
+        kernel<<<unsigned(a.rows), 1024, 0, s>>>(dy, a.lddy, x, a.ldx, w, a.mean, a.rstd, a.rows, a.cols, sums);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+      }
+      auto kernel = aligned ? k_norm_wide_grad<T, true> : k_norm_wide_grad<T, false>;
+      kernel<<<dim3(unsigned(strips), unsigned(parts)), 256, 0, s>>>(dy, a.lddy, x, a.ldx, w, a.mean, a.rstd, sums,
+                                                                    a.rows, a.cols, per, dx, a.lddx, part);
       e = hipGetLastError();
     }
   }

@@ -47,11 +47,14 @@ __device__ inline f32x4 mma<f16>(u32x4 r, u32x4 l, f32x4 c) {
 }
 // single precision: the four values of a chunk go to four instructions; the
 // sum over k does not care that k is dealt out by fours
+__device__ inline f32x4 mma_one(u32x4 r, u32x4 l, int e, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(f32x4, r)[e], __builtin_bit_cast(f32x4, l)[e], c, 0, 0,
+                                              0);
+}
 template <>
 __device__ inline f32x4 mma<float>(u32x4 r, u32x4 l, f32x4 c) {
-  const f32x4 a = __builtin_bit_cast(f32x4, r), b = __builtin_bit_cast(f32x4, l);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+  for (int e = 0; e < 4; ++e) c = mma_one(r, l, e, c);
   return c;
 }
 
@@ -341,11 +344,17 @@ __device__ inline void walk_tiles(const Grid &g, const L &left, const R &right, 
     }
   };
   f32x4 acc[MI][NI];
+  // an instruction never follows one with the same accumulators
   auto multiply = [&](const u32x4(&l)[MI], const u32x4(&r)[NI]) {
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
+    for (int e = 0; e < (sizeof(T) == 4 ? 4 : 1); ++e)
 #pragma unroll
-      for (int j = 0; j < NI; ++j) acc[i][j] = mma<T>(r[j], l[i], acc[i][j]);
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          if constexpr (sizeof(T) == 4) acc[i][j] = mma_one(r[j], l[i], e, acc[i][j]);
+          else acc[i][j] = mma<T>(r[j], l[i], acc[i][j]);
+        }
   };
 
   aim();
@@ -996,13 +1005,19 @@ __global__ __launch_bounds__(1024) void k_grad_factors(const float *dloss, const
   }
 }
 
-// out[n] = sum over t of part[t][n]
+// out[n] = sum over t of part[t][n]: 64 columns a workgroup, a wave for every
+// fourth part.
 __global__ __launch_bounds__(256) void k_sum_parts(const float *part, int count, int n_all, float *out) {
-  const int n = blockIdx.x * 256 + threadIdx.x;
-  if (n >= n_all) return;
+  __shared__ float shared[4][64];
+  const int n = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
   float s = 0.0f;
-  for (int t = 0; t < count; ++t) s += part[int64_t(t) * n_all + n];
-  out[n] = s;
+  if (n < n_all) {
+#pragma unroll 4
+    for (int t = wave; t < count; t += 4) s += part[int64_t(t) * n_all + n];
+  }
+  shared[wave][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (wave == 0 && n < n_all) out[n] = s + shared[1][threadIdx.x] + shared[2][threadIdx.x] + shared[3][threadIdx.x];
 }
 
 // Joins the splits of a product.
@@ -1359,7 +1374,7 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
         return product<T, S>(a.rows, words_k, k, 1, Rows<T>{x.p, x.ld, rows, k}, Rows<T>{wp, w.ld, words, k}, epi, s);
       }));
       if (a.dbias) {
-        k_sum_parts<<<unsigned(ceil_div(words, 256)), 256, 0, s>>>(col_part, mtiles, words, a.dbias + first);
+        k_sum_parts<<<unsigned(ceil_div(words, 64)), 256, 0, s>>>(col_part, mtiles, words, a.dbias + first);
         OPS_TRY(hipGetLastError());
       }
       OPS_TRY(with_shape(dx_tiles, [&](auto shape) {
