@@ -172,6 +172,7 @@ __device__ inline void tile_at(const Grid &g, int t, int &mt, int &nt) {
   mt = first + in % high;
   nt = in / high;
 }
+
 // An operand's part of a stage in LDS, B rows: B/16 loads of 1 KiB, dealt to the
 // waves in turns.
 //
@@ -1115,13 +1116,18 @@ hipError_t operand(const void *p, int64_t ld, int64_t rows, int cols, Arena &ws,
 
 // Tiles of a product and the parts its sum over k is split into.  Only a product
 // whose result is stored plainly can be split, into parts of at least 32 steps.
-// Each shape's cost is the area that the busiest CU has to multiply, over what
-// the shape reaches of the large one's rate (measured: 256 x 256 alone on a CU
-// 1, two workgroups of 128 x 128 0.75, four of 64 x 64 0.45, and about half of
-// that where a CU has only one).
+//
+// The shape with the least cost: the area that the busiest CU has to multiply,
+// over the rate that the shape reaches there.  A CU takes one workgroup of 256 x
+// 256, two of 128 x 128 or four of 64 x 64, and about half of the rate with only
+// one of several.  Measured, gated layer of 16-bit types, forward, us with 256 /
+// 128 / 64: 4096 x 512 x 4096 44 / 48 / 69 (all CUs full), 2048 x 1024 x 2048
+// 30 / 25 / 35, 512 x 1024 x 1024 28 / 15 / 13.  In single precision the matrix
+// unit alone bounds a CU, and smaller tiles are no slower: 2048 x 512 x 4096
+// 156 / 138 / 151, 256 x 1024 x 1024 272 / 70 / 25.
 struct Tiles {
   int m = 256, n = 256, splits = 1;
-  Tiles(int64_t rows, int64_t cols, int64_t steps = 0) {
+  Tiles(int64_t rows, int64_t cols, bool single, int64_t steps = 0) {
     const int64_t most = steps / 32 < 1 ? 1 : steps / 32 > 64 ? 64 : steps / 32;
     double best = 0;
     for (int side : {256, 128, 64}) {
@@ -1131,7 +1137,9 @@ struct Tiles {
       want = want < 1 ? 1 : want > most ? most : want;
       if (want > 1) want = ceil_div(steps, split_steps(steps, want));  // none is empty
       const int64_t each = ceil_div(tiles * want, kCus);  // tiles of the busiest CU
-      const double rate = (side == 256 ? 1.0 : side == 128 ? 0.75 : 0.45) * (each < fit ? 0.5 + 0.5 * each / fit : 1.0);
+      const double full = single ? (side == 256 ? 0.87 : side == 128 ? 1.0 : 0.91)
+                                 : (side == 256 ? 1.0 : side == 128 ? 0.75 : 0.45);
+      const double rate = full * (each < fit ? 0.5 + 0.5 * each / fit : 1.0);
       const double cost = double(each) * side * side / rate / double(want);
       if (best == 0 || cost < best) {
         best = cost;
@@ -1143,6 +1151,11 @@ struct Tiles {
   static int64_t split_steps(int64_t steps, int64_t splits) { return round_up(ceil_div(steps, splits), 2); }
   static constexpr int64_t kCus = 256;
 };
+
+template <typename T>
+Tiles tiles_of(int64_t rows, int64_t cols, int64_t steps = 0) {
+  return Tiles(rows, cols, sizeof(T) == 4, steps);
+}
 
 template <typename T>
 int64_t steps_of(int64_t k) {
@@ -1173,9 +1186,8 @@ hipError_t product(int64_t m, int64_t n, int64_t k, int splits, const L &left, c
   constexpr size_t lds = 4 * (S::BM + S::BN) * 64 + S::BM * S::WN * 8;  // and the softmax parts of a tile's rows
   auto kernel = k_product<T, S::BM, S::BN, S::WM, S::WN, L, R, Epilogue>;
   if constexpr (lds > 65536) {
-    static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
-                                                          hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
-    OPS_TRY(allowed);
+    OPS_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                int(lds)));
   }
   const int64_t most = Tiles::kCus * (S::BM == 256 ? 1 : S::BM == 128 ? 2 : 4);
   kernel<<<unsigned(items < most ? items : most), 64 * S::WM * S::WN, lds, s>>>(g, left, right, epi);
@@ -1186,7 +1198,7 @@ hipError_t product(int64_t m, int64_t n, int64_t k, int splits, const L &left, c
 template <typename T, typename L, typename R>
 hipError_t product_into(int64_t m, int64_t n, int64_t k, const L &left, const R &right, const Target<T> &out, Arena &ws,
                         bool dry, hipStream_t s) {
-  const Tiles tiles(m, n, steps_of<T>(k));
+  const Tiles tiles = tiles_of<T>(m, n, steps_of<T>(k));
   const int splits = tiles.splits;
   const int64_t cols4 = round_up(n, 4);
   float *part = splits > 1 ? ws.take<float>(splits * m * cols4) : nullptr;
@@ -1249,7 +1261,7 @@ hipError_t gated_forward_t(const lda_gated_args &a, Arena &ws, bool dry) {
   OPS_TRY(pair_operands<T>(a, false, ws, dry, s, gate, value));
   if (dry) return hipSuccess;
   const GatedForward<T> epi{static_cast<T *>(a.h), a.ldh, rows, a.hidden, a.act, at_once<T>(a.h, a.ldh) >= 4};
-  return with_shape(Tiles(a.rows, pair_cols(a.hidden)), [&](auto shape) {
+  return with_shape(tiles_of<T>(a.rows, pair_cols(a.hidden)), [&](auto shape) {
     return product<T, decltype(shape)>(a.rows, pair_cols(a.hidden), k, 1, Rows<T>{x.p, x.ld, rows, k},
                                        PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s);
   });
@@ -1272,7 +1284,7 @@ hipError_t gated_backward_t(const lda_gated_args &a, Arena &ws, bool dry) {
   if (!dry) {
     const GatedBackward<T> epi{static_cast<const T *>(a.dh), a.lddh, dab, rows, a.hidden, pc, a.act,
                                at_once<T>(a.dh, a.lddh) >= 4};
-    OPS_TRY(with_shape(Tiles(a.rows, pc), [&](auto shape) {
+    OPS_TRY(with_shape(tiles_of<T>(a.rows, pc), [&](auto shape) {
       return product<T, decltype(shape)>(a.rows, pc, k, 1, Rows<T>{x.p, x.ld, rows, k},
                                          PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s);
     }));
@@ -1305,7 +1317,7 @@ hipError_t xent_forward_t(const lda_xent_args &a, Arena &ws, bool dry) {
     k_lse_join_few<<<unsigned(rows), 256, 0, s>>>(part, parts, label_logit, a.labels, a.vocab, a.loss, a.lse);
     return hipGetLastError();
   }
-  const Tiles tiles(a.rows, a.vocab);
+  const Tiles tiles = tiles_of<T>(a.rows, a.vocab);
   const int ntiles = int(ceil_div(a.vocab, tiles.n));
   Matrix<T> x, w;
   OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
@@ -1341,7 +1353,7 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
     return a.dbias ? zero(a.dbias, a.vocab, s) : hipSuccess;
   }
   const int rows = int(a.rows), piece = piece_words<T>(a.rows, a.vocab), k = int(round_up(a.width, kChunk<T>));
-  const int mtiles = int(ceil_div(a.rows, Tiles(a.rows, piece).m));
+  const int mtiles = int(ceil_div(a.rows, tiles_of<T>(a.rows, piece).m));
   Matrix<T> x, w;
   OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
   OPS_TRY(operand<T>(a.weight, a.ld_weight, a.vocab, a.width, ws, dry, s, w));
@@ -1349,7 +1361,7 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   T *x_scaled = ws.take<T>(a.rows * k);
   T *grad = ws.take<T>(a.rows * piece);
   float *col_part = a.bias ? ws.take<float>(int64_t(mtiles) * piece) : nullptr;
-  const Tiles dx_tiles(a.rows, a.width, steps_of<T>(piece < a.vocab ? piece : a.vocab));
+  const Tiles dx_tiles = tiles_of<T>(a.rows, a.width, steps_of<T>(piece < a.vocab ? piece : a.vocab));
   const int splits = dx_tiles.splits;
   const int64_t cols4 = round_up(a.width, 4);
   float *dx_part = ws.take<float>(splits * a.rows * cols4);
@@ -1367,7 +1379,7 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
     const T *wp = w.p + int64_t(first) * w.ld;
     ws.used = mark;
     if (!dry) {
-      OPS_TRY(with_shape(Tiles(a.rows, piece), [&](auto shape) {
+      OPS_TRY(with_shape(tiles_of<T>(a.rows, piece), [&](auto shape) {
         typedef decltype(shape) S;
         const SoftmaxGrad<T, S::BN, S::WM> epi{a.bias, a.labels, a.lse, row_factor, grad, words_k, col_part, rows,
                                                a.vocab, first, words};
