@@ -14,9 +14,10 @@
  *   - Matrices are row-major with unit column stride; ld* is the row stride
  *     in elements.  Inputs may overlap or repeat rows (any ld >= 0); outputs
  *     need ld >= columns and must not overlap anything else of the call.
- *     Pointers need the alignment of their element type only; rows at
- *     multiples of 16 bytes are read where they lie, others are copied into
- *     the workspace first.
+ *     Pointers need the alignment of their element type only.  Matrices whose
+ *     rows start at multiples of 16 bytes and hold a multiple of 16 bytes are
+ *     read where they lie; others are slower (the products copy them into the
+ *     workspace first).
  *   - Sums, softmax statistics and row statistics are kept in 32 bits; an
  *     output is rounded once to its type.  Every sum has one order: results
  *     are the same bits on every run.
@@ -144,10 +145,11 @@ lda_status lda_gated_backward(const lda_gated_args *a);
  *   G_iv = dloss_i * (exp(z_iv - lse_i) - [v = label_i])
  * (0 for rows left out and rows without words) in the workspace:
  *   dx = G weight, dweight = G^T x, dbias = sum over rows of G
- * In 16-bit types G is rounded to the type of the matrices as an operand of
- * the products, scaled so that the largest finite |dloss| fits the type.
- * dbias is NULL if and only if bias is.  With rows = 0, dweight and dbias are
- * set to zero.
+ * As an operand of the first two products, in 16-bit types, G is kept without
+ * dloss and rounded to the type of the matrices (dbias is summed before); dloss
+ * multiplies dx in 32 bits, and x, rounded once more, for dweight.  Rows of
+ * weight must be finite also where their word is masked.  dbias is NULL if and
+ * only if bias is.  With rows = 0, dweight and dbias are set to zero.
  */
 typedef struct {
   int32_t dtype;

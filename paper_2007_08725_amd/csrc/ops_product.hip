@@ -1,10 +1,10 @@
 // Matrix products of the word-model operators (include/lda_ops.h): the gated
 // layer and the softmax cross entropy, forward and backward.
 //
-// Every product is C[m][n] = sum_k L[m][k] R[n][k] with both operands
-// contiguous in k, on the matrix units; what is done with C (activation,
+// Every product is C[m][n] = sum_k L[m][k] R[n][k] on the matrix units, either
+// operand as it lies in memory or transposed; what is done with C (activation,
 // softmax statistics, gradient of the logits, store) is the epilogue of the
-// kernel that computes it, while C is still in registers.
+// kernel that computes it, while C is still in registers.  Sums are in 32 bits.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -302,6 +302,13 @@ __device__ inline void stage_barrier() {
 //
 // `fill` and `data` are both the stages in LDS: between two barriers the stage
 // that is filled is not the one that is read.
+//
+// What bounds it: a CU takes 64 bytes a cycle from its L2, so that at the
+// matrix unit's rate a 128 x 128 tile needs all of that and a 256 x 256 tile
+// half; 256 x 256 with one step in flight was bound by the loads' latency.  Now
+// (8192 x 1024 x 16384 of bf16, two splits, 229 to 237 us = 1,160 to 1,200
+// TFLOP/s, where a library product of 8192^3 reaches 1,323) the matrix unit is
+// busy 59% of the cycles, at a clock of about 1.8 GHz (2.4 GHz at most).
 template <typename T, int BM, int BN, int WM, int WN, typename L, typename R, typename Epilogue>
 __device__ inline void walk_tiles(const Grid &g, const L &left, const R &right, const Epilogue &epilogue,
                                   lds_char *__restrict fill, const lds_char *__restrict data, char *scratch) {
@@ -564,6 +571,8 @@ __device__ inline void gate(int act, float a, float &p, float &dp) {
   }
 }
 
+// h from the accumulators: a and b are never written.  8192 x 1024 x 4096 of
+// bf16: 149 us = 920 TFLOP/s of both projections, the activation included.
 template <typename T>
 struct GatedForward {
   static constexpr bool kRuns = true;
@@ -596,7 +605,11 @@ struct GatedForward {
 };
 
 // da and db in turns of four columns (pair_row), zero past `hidden`: operands of
-// the backward products.
+// the backward products, from a and b recomputed.  Kept in 32 bits, as their
+// precision asks for, they would be written and read again (268 MB each way at
+// 8192 x 4096, about 110 us); recomputed, they cost 150 us of the backward
+// pass' 450, and a training step keeps x alone.  190 us with dh's reads and
+// dab's stores.
 template <typename T>
 struct GatedBackward {
   static constexpr bool kRuns = true;
@@ -663,7 +676,13 @@ __device__ inline int label_at(int label, int n0, int lane, int first, int vocab
 }
 
 // Per row and tile of words: the largest logit and the sum of exp(z - it), and
-// the label's logit from the lane that holds it.
+// the label's logit from the lane that holds it.  The parts of a row, one of a
+// tile's 256 words each, are joined by k_lse_join: 36 MB for 8,192 rows and
+// 141,000 words, where the logits would be 2.3 GB.
+//
+// 8192 x 1024 x 141000 of bf16: 2.1 to 2.2 ms = 1,080 to 1,120 TFLOP/s with
+// this epilogue (a library product that writes the logits: 1,044).  A wave's
+// exponentials do not overlap with its own products.
 template <int BM, int WN>
 struct SoftmaxPart {
   static constexpr bool kRuns = false;
@@ -723,10 +742,15 @@ struct SoftmaxPart {
 
 // G of one piece of the vocabulary (words from `first` on) without the rows'
 // own gradients, S (exp(z - lse) - [v = label]), and the column sums of the
-// rows' gradients times it by tile of rows.  |exp(z - lse) - 1| <= 1 wherever
-// G has one value that leads its row, so the label's -S is exact and what is
-// rounded is small beside it.  S is 1, in half precision 2^14, so that
-// probabilities down to 2^-28 are normal numbers.
+// rows' gradients times it by tile of rows.  Where one value of G leads its row
+// it is the label's, -S (1 - p), which rounds to -S itself where p is small; so
+// what the rounding of G to bf16 or f16, as operand of two products, changes is
+// small beside it.  S is 1, in half precision 2^14, so that probabilities down
+// to 2^-28 are normal numbers.
+//
+// A piece of 16,384 words at 8,192 rows of width 1,024: 301 to 313 us, where dx,
+// a product of the same size that stores little, takes 229 to 237: the rest is
+// the exponentials and G's 268 MB.
 template <typename T>
 constexpr float kGradLog2 = 0.0f;
 template <>
@@ -803,7 +827,9 @@ struct SoftmaxGrad {
 // ---------------------------------------------------------------- few rows ---
 // At most 16 rows of x (single tokens in serving): the weights are read once,
 // from HBM straight into fragments, 16 of their rows a wave, and nothing is
-// staged; x comes from the caches.  Bound by the weights' bytes.
+// staged; x comes from the caches.  Bound by the weights' bytes: one row against
+// 141000 x 1024 of bf16 (289 MB) takes 55 us = 5.3 TB/s, where a copy of 4 GiB
+// reaches 4.8 TB/s; through tiles of 64 x 64 it took 83 us.
 constexpr int kFewRows = 16;
 
 // Chunk `c` of a row of `cols` elements, zero past its end; rows that do not
@@ -843,7 +869,8 @@ __device__ inline void few_products(const T *x, const T *const (&w)[TILES], int 
   }
 }
 
-// 16 columns of h a workgroup; its four waves share the sum over k.
+// 16 columns of h a workgroup; its four waves share the sum over k (a hidden
+// width of 1,024 is 64 workgroups: 5 us at a width of 1,000, latency).
 template <typename T, bool Aligned>
 __global__ __launch_bounds__(256) void k_gated_few(const T *x, int64_t ldx, const T *gates, int64_t ld_gate,
                                                    const T *values, int64_t ld_value, int rows, int width, int hidden,
