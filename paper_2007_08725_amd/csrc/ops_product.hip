@@ -990,10 +990,11 @@ __global__ __launch_bounds__(256) void k_lse_join_few(const float2 *part, int pa
 // The rows' gradients as factors of the products: row_factor = dloss / S for dx
 // and dbias, and x_factor = dloss / unit for the rows of x in dweight, whose
 // result is then multiplied by out[0] = unit / S.  The unit is the smallest
-// finite |dloss| above 0, by the power of two that brings it to the largest's
-// magnitude: equal gradients, and power-of-two multiples of one (a word that
-// counts once, twice, four times), then leave the rows of x unrounded.  The
-// factors are 0 for rows that are left out.
+// finite |dloss| above 0, by the power of two that brings it to the largest or
+// just above: equal gradients, and power-of-two multiples of one (a word that
+// counts once, twice, four times), then leave the rows of x unrounded, and no
+// factor is above 1, so that none takes x out of its type's range.  The factors
+// are 0 for rows that are left out.
 __global__ __launch_bounds__(1024) void k_grad_factors(const float *dloss, const float *lse, const int32_t *labels,
                                                        int rows, int vocab, float s, float *out, float *row_factor,
                                                        float *x_factor) {
@@ -1024,6 +1025,7 @@ __global__ __launch_bounds__(1024) void k_grad_factors(const float *dloss, const
     int e_top, e_low;
     frexpf(top, &e_top);
     unit = ldexpf(frexpf(low, &e_low), e_top);
+    if (unit < top) unit = fminf(2.0f * unit, 0x1.fffffep127f);
   }
   if (threadIdx.x == 0) out[0] = unit / s;
   for (int m = threadIdx.x; m < rows; m += 1024) {

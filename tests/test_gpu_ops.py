@@ -357,6 +357,26 @@ def _xent_all(ops, x, w, labels, bias, dloss):
     return loss, dx, dw, db
 
 
+@pytest.mark.parametrize("rows", [5, 40])
+def test_softmax_xent_unequal_gradients_at_the_types_range(ops, rows):
+    """Half-precision x near its largest value: the rows' factors must not take it past it."""
+    width, vocab = 64, 300
+    x, w = rand(1, rows, width, dtype=torch.float16), rand(2, vocab, width, scale=0.1, dtype=torch.float16)
+    x[:, 0], w[:, 0] = 50000.0, 0.0  # no part in the logits
+    labels = torch.arange(rows, dtype=torch.int32, device="cuda") * 7 % vocab
+    dloss = torch.linspace(1.05e-3, 1.9e-3, rows, device="cuda")
+    _, dx, dw, _ = _xent_all(ops, x, w, labels, None, dloss)
+    x8, w8 = x.to(F8), w.to(F8)
+    z = x8 @ w8.t()
+    p = torch.exp(z - torch.logsumexp(z, 1)[:, None])
+    p[torch.arange(rows, device="cuda"), labels.long()] -= 1
+    grad = p * dloss.to(F8)[:, None]
+    # G and the scaled x are rounded once each, the logits are off by g of their magnitude
+    eg = (3 * U[torch.float16] + 4 * g(width) * float((x8[:, 1:].abs() @ w8[:, 1:].abs().t()).max())) * grad.abs()
+    check("dweight", dw, grad.t() @ x8, (eg + g(rows) * grad.abs()).t() @ x8.abs())
+    assert bool(dx.isfinite().all())
+
+
 @pytest.mark.parametrize("rows", [3, 40])
 def test_softmax_xent_no_row_kept(ops, rows):
     x, w = rand(1, rows, 40), rand(2, 90, 40)
