@@ -1071,22 +1071,47 @@ __global__ __launch_bounds__(256) void k_zero(T *p, int64_t n) {
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) p[i] = T(0.0f);
 }
 
-// A copy of a matrix for the products: its rows at multiples of 16 bytes, zero
+// Copies of matrices for the products, up to three a launch (a launch takes
+// longer than the copy of a small matrix): rows at multiples of 16 bytes, zero
 // past their end; each row times its factor, a row of factor 0 zero whatever it
-// holds (factor NULL = 1).
+// holds (factor NULL = 1).  A lane reads a chunk element by element and writes
+// it at once; divisions in 32 bits where the count of chunks allows it.
 template <typename T>
-__global__ __launch_bounds__(256) void k_pack(const T *src, int64_t ld, int64_t rows, int cols, const float *factor,
-                                              T *dst, int ldd) {
-  const int64_t all = rows * ldd, step = int64_t(gridDim.x) * 256;
+struct Copy {
+  const T *src;
+  int64_t ld, rows;
+  int cols, chunks;  // of a row of dst
+  const float *factor;
+  T *dst;
+};
+constexpr int kCopies = 3;
+template <typename T>
+struct Copies {
+  Copy<T> copy[kCopies];
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_pack(const Copies<T> copies) {
+  const Copy<T> &c = copies.copy[blockIdx.y];
+  const int64_t all = c.rows * c.chunks, step = int64_t(gridDim.x) * 256;
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += step) {
-    const int64_t r = i / ldd;
-    const int c = int(i % ldd);
-    T v = T(0.0f);
-    if (c < cols) {
-      v = src[r * ld + c];
-      if (factor) v = factor[r] == 0.0f ? T(0.0f) : T(float(v) * factor[r]);
+    const int64_t r = all <= 0xffffffffll ? uint32_t(i) / uint32_t(c.chunks) : i / c.chunks;
+    const int first = int(i - r * c.chunks) * kChunk<T>;
+    const float f = c.factor ? c.factor[r] : 1.0f;
+    union {
+      T v[kChunk<T>];
+      uint4 all;
+    } u;
+#pragma unroll
+    for (int e = 0; e < kChunk<T>; ++e) {
+      T v = T(0.0f);
+      if (first + e < c.cols && f != 0.0f) {
+        v = c.src[r * c.ld + first + e];
+        if (c.factor) v = T(float(v) * f);
+      }
+      u.v[e] = v;
     }
-    dst[i] = v;
+    reinterpret_cast<uint4 *>(c.dst)[i] = u.all;
   }
 }
 
@@ -1121,26 +1146,33 @@ struct Matrix {
   int64_t ld;
 };
 
+// The copies that a call needs before its first product.
 template <typename T>
-hipError_t pack(const void *p, int64_t ld, int64_t rows, int cols, const float *factor, T *copy, int64_t ldd,
-                hipStream_t s) {
-  k_pack<T><<<strided(ceil_div(rows * ldd, 256)), 256, 0, s>>>(static_cast<const T *>(p), ld, rows, cols, factor, copy,
-                                                              int(ldd));
-  return hipGetLastError();
-}
+struct Packs {
+  Copies<T> copies = {};
+  int count = 0;
+  int64_t most = 0;  // chunks of the largest
+
+  void add(const void *p, int64_t ld, int64_t rows, int cols, const float *factor, T *dst, int64_t ldd) {
+    const int chunks = int(ldd / kChunk<T>);
+    copies.copy[count++] = Copy<T>{static_cast<const T *>(p), ld, rows, cols, chunks, factor, dst};
+    if (rows * chunks > most) most = rows * chunks;
+  }
+  hipError_t run(hipStream_t s) {
+    if (count == 0) return hipSuccess;
+    k_pack<T><<<dim3(strided(ceil_div(most, 256)), unsigned(count)), 256, 0, s>>>(copies);
+    return hipGetLastError();
+  }
+};
 
 // A matrix as the products read it, copied where it has to be.
 template <typename T>
-hipError_t operand(const void *p, int64_t ld, int64_t rows, int cols, Arena &ws, bool dry, hipStream_t s,
-                   Matrix<T> &out) {
-  if (in_place<T>(p, ld, cols)) {
-    out = Matrix<T>{static_cast<const T *>(p), ld};
-    return hipSuccess;
-  }
+Matrix<T> operand(const void *p, int64_t ld, int64_t rows, int cols, Arena &ws, Packs<T> &packs) {
+  if (in_place<T>(p, ld, cols)) return Matrix<T>{static_cast<const T *>(p), ld};
   const int64_t ldd = round_up(cols, kChunk<T>);
   T *copy = ws.take<T>(rows * ldd);
-  out = Matrix<T>{copy, ldd};
-  return dry ? hipSuccess : pack<T>(p, ld, rows, cols, nullptr, copy, ldd, s);
+  packs.add(p, ld, rows, cols, nullptr, copy, ldd);
+  return Matrix<T>{copy, ldd};
 }
 
 // Tiles of a product and the parts its sum over k is split into.  Only a product
@@ -1255,19 +1287,18 @@ int64_t pair_cols(int hidden) { return 2 * round_up(hidden, 64); }
 // Both weights as the products read them, with one row stride if `same` (they
 // are copied for that where they have two).
 template <typename T>
-hipError_t pair_operands(const lda_gated_args &a, bool same, Arena &ws, bool dry, hipStream_t s, Matrix<T> &gate,
-                         Matrix<T> &value) {
-  OPS_TRY(operand<T>(a.w_gate, a.ld_gate, a.hidden, a.width, ws, dry, s, gate));
-  OPS_TRY(operand<T>(a.w_value, a.ld_value, a.hidden, a.width, ws, dry, s, value));
-  if (!same || gate.ld == value.ld) return hipSuccess;
+void pair_operands(const lda_gated_args &a, bool same, Arena &ws, Packs<T> &packs, Matrix<T> &gate, Matrix<T> &value) {
+  gate = operand<T>(a.w_gate, a.ld_gate, a.hidden, a.width, ws, packs);
+  value = operand<T>(a.w_value, a.ld_value, a.hidden, a.width, ws, packs);
+  if (!same || gate.ld == value.ld) return;
+  // a copy has this stride, so that no weight is copied twice
   const int64_t ldd = round_up(a.width, kChunk<T>);
   for (Matrix<T> *m : {&gate, &value}) {
     if (m->ld == ldd) continue;
     T *copy = ws.take<T>(a.hidden * ldd);
-    if (!dry) OPS_TRY(pack<T>(m->p, m->ld, a.hidden, a.width, nullptr, copy, ldd, s));
+    packs.add(m->p, m->ld, a.hidden, a.width, nullptr, copy, ldd);
     *m = Matrix<T>{copy, ldd};
   }
-  return hipSuccess;
 }
 
 template <typename T>
@@ -1285,10 +1316,12 @@ hipError_t gated_forward_t(const lda_gated_args &a, Arena &ws, bool dry) {
         static_cast<const T *>(a.w_value), a.ld_value, rows, a.width, a.hidden, a.act, static_cast<T *>(a.h), a.ldh);
     return hipGetLastError();
   }
-  Matrix<T> x, gate, value;
-  OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
-  OPS_TRY(pair_operands<T>(a, false, ws, dry, s, gate, value));
+  Packs<T> packs;
+  const Matrix<T> x = operand<T>(a.x, a.ldx, a.rows, a.width, ws, packs);
+  Matrix<T> gate, value;
+  pair_operands<T>(a, false, ws, packs, gate, value);
   if (dry) return hipSuccess;
+  OPS_TRY(packs.run(s));
   const GatedForward<T> epi{static_cast<T *>(a.h), a.ldh, rows, a.hidden, a.act, at_once<T>(a.h, a.ldh) >= 4};
   return with_shape(tiles_of<T>(a.rows, pair_cols(a.hidden)), [&](auto shape) {
     return product<T, decltype(shape)>(a.rows, pair_cols(a.hidden), k, 1, Rows<T>{x.p, x.ld, rows, k},
@@ -1306,11 +1339,13 @@ hipError_t gated_backward_t(const lda_gated_args &a, Arena &ws, bool dry) {
     return zero(dwv, int64_t(a.hidden) * a.width, s);
   }
   const int rows = int(a.rows), pc = int(pair_cols(a.hidden)), k = int(round_up(a.width, kChunk<T>));
-  Matrix<T> x, gate, value;
-  OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
-  OPS_TRY(pair_operands<T>(a, true, ws, dry, s, gate, value));
+  Packs<T> packs;
+  const Matrix<T> x = operand<T>(a.x, a.ldx, a.rows, a.width, ws, packs);
+  Matrix<T> gate, value;
+  pair_operands<T>(a, true, ws, packs, gate, value);
   T *dab = ws.take<T>(a.rows * pc);
   if (!dry) {
+    OPS_TRY(packs.run(s));
     const GatedBackward<T> epi{static_cast<const T *>(a.dh), a.lddh, dab, rows, a.hidden, pc, a.act,
                                at_once<T>(a.dh, a.lddh) >= 4};
     OPS_TRY(with_shape(tiles_of<T>(a.rows, pc), [&](auto shape) {
@@ -1348,12 +1383,13 @@ hipError_t xent_forward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   }
   const Tiles tiles = tiles_of<T>(a.rows, a.vocab);
   const int ntiles = int(ceil_div(a.vocab, tiles.n));
-  Matrix<T> x, w;
-  OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
-  OPS_TRY(operand<T>(a.weight, a.ld_weight, a.vocab, a.width, ws, dry, s, w));
+  Packs<T> packs;
+  const Matrix<T> x = operand<T>(a.x, a.ldx, a.rows, a.width, ws, packs);
+  const Matrix<T> w = operand<T>(a.weight, a.ld_weight, a.vocab, a.width, ws, packs);
   float2 *part = ws.take<float2>(int64_t(ntiles) * rows);
   float *label_logit = ws.take<float>(rows);
   if (dry) return hipSuccess;
+  OPS_TRY(packs.run(s));
   OPS_TRY(with_shape(tiles, [&](auto shape) {
     typedef decltype(shape) S;
     const SoftmaxPart<S::BM, S::WN> epi{a.bias, a.labels, label_logit, part, rows, a.vocab};
@@ -1383,9 +1419,9 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   }
   const int rows = int(a.rows), piece = piece_words<T>(a.rows, a.vocab), k = int(round_up(a.width, kChunk<T>));
   const int mtiles = int(ceil_div(a.rows, tiles_of<T>(a.rows, piece).m));
-  Matrix<T> x, w;
-  OPS_TRY(operand<T>(a.x, a.ldx, a.rows, a.width, ws, dry, s, x));
-  OPS_TRY(operand<T>(a.weight, a.ld_weight, a.vocab, a.width, ws, dry, s, w));
+  Packs<T> packs;
+  const Matrix<T> x = operand<T>(a.x, a.ldx, a.rows, a.width, ws, packs);
+  const Matrix<T> w = operand<T>(a.weight, a.ld_weight, a.vocab, a.width, ws, packs);
   float *top = ws.take<float>(1), *row_factor = ws.take<float>(rows), *x_factor = ws.take<float>(rows);
   T *x_scaled = ws.take<T>(a.rows * k);
   T *grad = ws.take<T>(a.rows * piece);
@@ -1397,7 +1433,8 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   if (!dry) {
     k_grad_factors<<<1, 1024, 0, s>>>(a.dloss, a.lse, a.labels, rows, a.vocab, kGradUnit<T>, top, row_factor, x_factor);
     OPS_TRY(hipGetLastError());
-    OPS_TRY(pack<T>(a.x, a.ldx, a.rows, a.width, x_factor, x_scaled, k, s));
+    packs.add(a.x, a.ldx, a.rows, a.width, x_factor, x_scaled, k);
+    OPS_TRY(packs.run(s));
   }
   // the pieces' products share the scratch of their parts
   const size_t mark = ws.used;
