@@ -1176,36 +1176,45 @@ Matrix<T> operand(const void *p, int64_t ld, int64_t rows, int cols, Arena &ws, 
 }
 
 // Tiles of a product and the parts its sum over k is split into.  Only a product
-// whose result is stored plainly can be split, into parts of at least 32 steps.
+// whose result is stored plainly can be split (`steps` given), into parts of at
+// least 8 steps.
 //
-// The shape with the least cost: the area that the busiest CU has to multiply,
-// over the rate that the shape reaches there.  A CU takes one workgroup of 256 x
+// The shape and the parts with the least time: the area that the busiest CU has
+// to multiply, over the rate that the shape reaches there, and for parts a
+// launch that joins them and their bytes.  A CU takes one workgroup of 256 x
 // 256, two of 128 x 128 or four of 64 x 64, and about half of the rate with only
 // one of several.  Measured, gated layer of 16-bit types, forward, us with 256 /
 // 128 / 64: 4096 x 512 x 4096 44 / 48 / 69 (all CUs full), 2048 x 1024 x 2048
 // 30 / 25 / 35, 512 x 1024 x 1024 28 / 15 / 13.  In single precision the matrix
-// unit alone bounds a CU, and smaller tiles are no slower: 2048 x 512 x 4096
-// 156 / 138 / 151, 256 x 1024 x 1024 272 / 70 / 25.
+// unit alone bounds a CU, 256 accumulators spill, and smaller tiles are no
+// slower: 2048 x 512 x 4096 156 / 138 / 151, 256 x 1024 x 1024 272 / 70 / 25.
 struct Tiles {
-  int m = 256, n = 256, splits = 1;
+  int m = 0, n = 0, splits = 1;
   Tiles(int64_t rows, int64_t cols, bool single, int64_t steps = 0) {
-    const int64_t most = steps / 32 < 1 ? 1 : steps / 32 > 64 ? 64 : steps / 32;
+    const int64_t most = steps / 8 < 1 ? 1 : steps / 8 > 64 ? 64 : steps / 8;
+    // us of a CU for a step of 256 x 256 at a rate of 1
+    const double step_us = single ? 4.3 : 0.9;
     double best = 0;
     for (int side : {256, 128, 64}) {
+      if (single && side == 256) continue;
       const int64_t tiles = ceil_div(rows, side) * ceil_div(cols, side);
       const int fit = side == 256 ? 1 : side == 128 ? 2 : 4;
-      int64_t want = kCus * fit / tiles;
-      want = want < 1 ? 1 : want > most ? most : want;
-      if (want > 1) want = ceil_div(steps, split_steps(steps, want));  // none is empty
-      const int64_t each = ceil_div(tiles * want, kCus);  // tiles of the busiest CU
-      const double full = single ? (side == 256 ? 0.87 : side == 128 ? 1.0 : 0.91)
-                                 : (side == 256 ? 1.0 : side == 128 ? 0.75 : 0.45);
-      const double rate = full * (each < fit ? 0.5 + 0.5 * each / fit : 1.0);
-      const double cost = double(each) * side * side / rate / double(want);
-      if (best == 0 || cost < best) {
-        best = cost;
-        m = n = side;
-        splits = int(want);
+      const double full = single ? (side == 128 ? 1.0 : 0.91) : (side == 256 ? 1.0 : side == 128 ? 0.75 : 0.45);
+      // whole, or parts that give every CU one, two or four workgroups
+      for (int64_t fill = 0; fill <= fit; fill = fill ? 2 * fill : 1) {
+        int64_t want = fill * kCus / tiles;
+        want = want < 1 ? 1 : want > most ? most : want;
+        if (fill && want == 1) continue;
+        if (want > 1) want = ceil_div(steps, split_steps(steps, want));  // none is empty
+        const int64_t each = ceil_div(tiles * want, kCus);  // tiles of the busiest CU
+        const double rate = full * (each < fit ? 0.5 + 0.5 * each / fit : 1.0);
+        double us = double(each) * side * side / 65536 * step_us * (steps ? steps : 1) / rate / double(want);
+        if (want > 1) us += 4.0 + double(rows) * double(cols) * want * 1e-6;
+        if (best == 0 || us < best) {
+          best = us;
+          m = n = side;
+          splits = int(want);
+        }
       }
     }
   }
@@ -1229,9 +1238,12 @@ struct Shape {
 };
 
 // Calls fn with the shape of the tiles.
-template <typename Fn>
+template <typename T, typename Fn>
 hipError_t with_shape(const Tiles &t, Fn fn) {
-  return t.m == 256 ? fn(Shape<256, 256, 2, 4>()) : t.m == 128 ? fn(Shape<128, 128, 2, 2>()) : fn(Shape<64, 64, 2, 2>());
+  if constexpr (sizeof(T) == 2) {
+    if (t.m == 256) return fn(Shape<256, 256, 2, 4>());
+  }
+  return t.m == 128 ? fn(Shape<128, 128, 2, 2>()) : fn(Shape<64, 64, 2, 2>());
 }
 
 template <typename T, typename S, typename L, typename R, typename Epilogue>
@@ -1265,10 +1277,10 @@ hipError_t product_into(int64_t m, int64_t n, int64_t k, const L &left, const R 
   float *part = splits > 1 ? ws.take<float>(splits * m * cols4) : nullptr;
   if (dry) return hipSuccess;
   if (splits == 1)
-    return with_shape(tiles, [&](auto shape) {
+    return with_shape<T>(tiles, [&](auto shape) {
       return product<T, decltype(shape)>(m, n, k, 1, left, right, Store<T>{out, int(n)}, s);
     });
-  OPS_TRY(with_shape(tiles, [&](auto shape) {
+  OPS_TRY(with_shape<T>(tiles, [&](auto shape) {
     return product<T, decltype(shape)>(m, n, k, splits, left, right, StorePart<false>{part, int(m), int(cols4)}, s);
   }));
   k_join<T><<<strided(ceil_div(m * cols4, 1024)), 256, 0, s>>>(part, splits, int(m), int(n), int(cols4), out);
@@ -1323,7 +1335,7 @@ hipError_t gated_forward_t(const lda_gated_args &a, Arena &ws, bool dry) {
   if (dry) return hipSuccess;
   OPS_TRY(packs.run(s));
   const GatedForward<T> epi{static_cast<T *>(a.h), a.ldh, rows, a.hidden, a.act, at_once<T>(a.h, a.ldh) >= 4};
-  return with_shape(tiles_of<T>(a.rows, pair_cols(a.hidden)), [&](auto shape) {
+  return with_shape<T>(tiles_of<T>(a.rows, pair_cols(a.hidden)), [&](auto shape) {
     return product<T, decltype(shape)>(a.rows, pair_cols(a.hidden), k, 1, Rows<T>{x.p, x.ld, rows, k},
                                        PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s);
   });
@@ -1348,7 +1360,7 @@ hipError_t gated_backward_t(const lda_gated_args &a, Arena &ws, bool dry) {
     OPS_TRY(packs.run(s));
     const GatedBackward<T> epi{static_cast<const T *>(a.dh), a.lddh, dab, rows, a.hidden, pc, a.act,
                                at_once<T>(a.dh, a.lddh) >= 4};
-    OPS_TRY(with_shape(tiles_of<T>(a.rows, pc), [&](auto shape) {
+    OPS_TRY(with_shape<T>(tiles_of<T>(a.rows, pc), [&](auto shape) {
       return product<T, decltype(shape)>(a.rows, pc, k, 1, Rows<T>{x.p, x.ld, rows, k},
                                          PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s);
     }));
@@ -1390,7 +1402,7 @@ hipError_t xent_forward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   float *label_logit = ws.take<float>(rows);
   if (dry) return hipSuccess;
   OPS_TRY(packs.run(s));
-  OPS_TRY(with_shape(tiles, [&](auto shape) {
+  OPS_TRY(with_shape<T>(tiles, [&](auto shape) {
     typedef decltype(shape) S;
     const SoftmaxPart<S::BM, S::WN> epi{a.bias, a.labels, label_logit, part, rows, a.vocab};
     return product<T, S>(a.rows, a.vocab, k, 1, Rows<T>{x.p, x.ld, rows, k}, Rows<T>{w.p, w.ld, a.vocab, k}, epi, s);
@@ -1445,7 +1457,7 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
     const T *wp = w.p + int64_t(first) * w.ld;
     ws.used = mark;
     if (!dry) {
-      OPS_TRY(with_shape(tiles_of<T>(a.rows, piece), [&](auto shape) {
+      OPS_TRY(with_shape<T>(tiles_of<T>(a.rows, piece), [&](auto shape) {
         typedef decltype(shape) S;
         const SoftmaxGrad<T, S::BN, S::WM> epi{a.bias, a.labels, a.lse, row_factor, grad, words_k, col_part, rows,
                                                a.vocab, first, words};
@@ -1455,7 +1467,7 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
         k_sum_parts<<<unsigned(ceil_div(words, 64)), 256, 0, s>>>(col_part, mtiles, words, a.dbias + first);
         OPS_TRY(hipGetLastError());
       }
-      OPS_TRY(with_shape(dx_tiles, [&](auto shape) {
+      OPS_TRY(with_shape<T>(dx_tiles, [&](auto shape) {
         const Rows<T> gr{grad, words_k, rows, words_k};
         const Columns<T> wc{wp, w.ld, a.width, words};
         if (first == 0)
