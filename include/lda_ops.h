@@ -101,7 +101,11 @@ lda_status lda_layer_norm_backward(const lda_norm_args *a);
  *   da = dh * b * act'(a), db = dh * act(a)
  *   dx = da w_gate + db w_value, dw_gate = da^T x, dw_value = db^T x
  * da and db are rounded to the type of the matrices, as operands of the three
- * products.  With rows = 0 the weights' gradients are set to zero.
+ * products; in half precision times a power of two for each row, so that they
+ * may pass the type's range where the gradients do not (a row's part of the
+ * weights' gradients loses bits where max |dh| max |x| |x|, |x| the row's length,
+ * is more than some 2^29 below the largest row's).  With rows = 0 the weights'
+ * gradients are set to zero.
  */
 typedef struct {
   int32_t dtype, act; /* lda_dtype, lda_act */

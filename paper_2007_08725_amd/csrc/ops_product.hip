@@ -610,12 +610,22 @@ struct GatedForward {
 // 8192 x 4096, about 110 us); recomputed, they cost 150 us of the backward
 // pass' 450, and a training step keeps x alone.  190 us with dh's reads and
 // dab's stores.
+//
+// In half precision da and db go past the type's range, or below it, long before
+// the gradients that are made of them: each row is multiplied by a power of two
+// (k_gated_scales), which the products' results or operands take back.
+template <typename T>
+constexpr bool kScaledRows = false;
+template <>
+constexpr bool kScaledRows<f16> = true;
+
 template <typename T>
 struct GatedBackward {
   static constexpr bool kRuns = true;
   const T *dh;
   int64_t ld;
-  T *dab;  // [rows][pair_cols]
+  const float *scale;  // of each row, with kScaledRows
+  T *dab;              // [rows][pair_cols]
   int rows, hidden, pair_cols, act;
   bool whole;
   template <int MI, int NI>
@@ -625,11 +635,14 @@ struct GatedBackward {
       one_row_at_a_time();
       const int m = at.m0 + i * 16 + (at.lane & 15);
       if (m >= rows) continue;
+      float s = 1.0f;
+      if constexpr (kScaledRows<T>) s = scale[m];
       f32x4 d[NI];
 #pragma unroll
       for (int j = 0; j < NI; j += 2) {
         const int f = pair_row(at.n0 + Order<kRuns>::col(j, at.lane >> 4));
-        const f32x4 dhv = load4(dh + m * ld + f, hidden - f, whole);
+        f32x4 dhv = load4(dh + m * ld + f, hidden - f, whole);
+        if constexpr (kScaledRows<T>) dhv *= s;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           float p, dp;
@@ -1071,7 +1084,7 @@ __global__ __launch_bounds__(256) void k_zero(T *p, int64_t n) {
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) p[i] = T(0.0f);
 }
 
-// Copies of matrices for the products, up to three a launch (a launch takes
+// Copies of matrices for the products, up to four a launch (a launch takes
 // longer than the copy of a small matrix): rows at multiples of 16 bytes, zero
 // past their end; each row times its factor, a row of factor 0 zero whatever it
 // holds (factor NULL = 1).  A lane reads a chunk element by element and writes
@@ -1084,7 +1097,7 @@ struct Copy {
   const float *factor;
   T *dst;
 };
-constexpr int kCopies = 3;
+constexpr int kCopies = 4;
 template <typename T>
 struct Copies {
   Copy<T> copy[kCopies];
@@ -1113,6 +1126,113 @@ __global__ __launch_bounds__(256) void k_pack(const Copies<T> copies) {
     }
     reinterpret_cast<uint4 *>(c.dst)[i] = u.all;
   }
+}
+
+// The largest magnitude and the length (root of the sum of squares) of each row
+// of up to four matrices, of the finite values: a wave a row.
+template <typename T>
+struct Sized {
+  const T *p;
+  int64_t ld, rows;
+  int cols;
+  bool aligned;  // row_chunk's
+  float2 *out;
+};
+constexpr int kSized = 4;
+template <typename T>
+struct SizedRows {
+  Sized<T> of[kSized];
+};
+
+template <typename T, bool Aligned>
+__device__ inline float2 row_size(const T *row, int cols, int lane) {
+  float2 s = make_float2(0.0f, 0.0f);
+  for (int c = lane; c * kChunk<T> < cols; c += 64) {
+    typedef T vec __attribute__((ext_vector_type(kChunk<T>)));
+    const vec v = __builtin_bit_cast(vec, row_chunk<T, Aligned>(row, c, cols));
+#pragma unroll
+    for (int e = 0; e < kChunk<T>; ++e) {
+      const float x = fabsf(float(v[e]));
+      if (x < INFINITY) {
+        s.x = fmaxf(s.x, x);
+        s.y += x * x;
+      }
+    }
+  }
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) {
+    s.x = fmaxf(s.x, __shfl_xor(s.x, x));
+    s.y += __shfl_xor(s.y, x);
+  }
+  return make_float2(s.x, sqrtf(s.y));
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_row_sizes(const SizedRows<T> all) {
+  const Sized<T> &a = all.of[blockIdx.y];
+  const int lane = threadIdx.x & 63;
+  for (int64_t r = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6); r < a.rows; r += int64_t(gridDim.x) * 4) {
+    const T *row = a.p + r * a.ld;
+    const float2 s = a.aligned ? row_size<T, true>(row, a.cols, lane) : row_size<T, false>(row, a.cols, lane);
+    if (lane == 0) a.out[r] = s;
+  }
+}
+
+// The largest of the threads' values, for every thread of 1,024.
+__device__ inline float group_max(float v, float (&shared)[16]) {
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) v = fmaxf(v, __shfl_xor(v, x));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 16; ++w) v = fmaxf(v, shared[w]);
+  return v;
+}
+
+// Powers of two that bring the rows of da and db below 2^15 in magnitude, by
+//   |a|, |b| <= |x_i| |w|, |act'| <= 1.2, |act(a)| <= |a| (sigmoid: 1),
+//   |da|, |db| <= max |dh_i| (1.2 |x_i| |w| (+ 1)),  |w| the longest row of both weights:
+// row i is kept times scale[i] = 2^k_i, so that what lies more than some 2^29
+// below that bound is subnormal, and dx_factor[i] = 2^-k_i takes it back from
+// dx.  x_factor is the same for k_gated_units, which also gets the largest |x|
+// 2^-k_i by workgroup, tops [gridDim.x].  A row without a gradient has scale 1
+// and x_factor 0.
+__global__ __launch_bounds__(1024) void k_gated_scales(const float2 *x, const float2 *dh, const float2 *gate,
+                                                       const float2 *value, int rows, int hidden, int act, float *scale,
+                                                       float *dx_factor, float *x_factor, float *tops) {
+  __shared__ float shared[16];
+  float longest = 0.0f;
+  for (int f = threadIdx.x; f < hidden; f += 1024) longest = fmaxf(longest, fmaxf(gate[f].y, value[f].y));
+  longest = group_max(longest, shared);
+  float top = 0.0f;
+  for (int m = int(blockIdx.x) * 1024 + int(threadIdx.x); m < rows; m += int(gridDim.x) * 1024) {
+    const float bound = dh[m].x * (1.2f * x[m].y * longest + (act == LDA_SIGMOID ? 1.0f : 0.0f));
+    int e = 15;
+    if (bound > 0.0f) frexpf(bound, &e);  // bound < 2^e
+    scale[m] = ldexpf(1.0f, 15 - e);
+    dx_factor[m] = ldexpf(1.0f, e - 15);
+    x_factor[m] = bound > 0.0f ? dx_factor[m] : 0.0f;
+    top = fmaxf(top, x[m].x * x_factor[m]);
+  }
+  top = group_max(top, shared);
+  if (threadIdx.x == 0) tops[blockIdx.x] = top;
+}
+
+// dw = sum over rows of (2^k_i da_i) (2^-k_i x_i): the second factor, an operand
+// too, is brought below 2^15 by a power of two for all rows, which out[0] takes
+// back.  A row's part loses bits where its largest |x| times its bound is more
+// than some 2^29 below the largest.
+__global__ __launch_bounds__(1024) void k_gated_units(const float *tops, int count, int rows, float *x_factor,
+                                                      float *out) {
+  __shared__ float shared[16];
+  const float top = group_max(int(threadIdx.x) < count ? tops[threadIdx.x] : 0.0f, shared);
+  int e = 15;
+  if (top > 0.0f) frexpf(top, &e);
+  if (blockIdx.x == 0 && threadIdx.x == 0) out[0] = ldexpf(1.0f, e - 15);
+  const float unit = ldexpf(1.0f, 15 - e);
+  for (int m = int(blockIdx.x) * 1024 + int(threadIdx.x); m < rows; m += int(gridDim.x) * 1024)
+    x_factor[m] *= unit;
 }
 
 // ------------------------------------------------------------------- host ---
@@ -1144,6 +1264,25 @@ template <typename T>
 struct Matrix {
   const T *p;
   int64_t ld;
+};
+
+// The matrices whose rows' sizes a call needs.
+template <typename T>
+struct Sizes {
+  SizedRows<T> rows_of = {};
+  int count = 0;
+  int64_t most = 0;  // rows
+
+  float2 *add(const void *p, int64_t ld, int64_t rows, int cols, Arena &ws) {
+    float2 *out = ws.take<float2>(rows);
+    rows_of.of[count++] = Sized<T>{static_cast<const T *>(p), ld, rows, cols, in_place<T>(p, ld, cols), out};
+    if (rows > most) most = rows;
+    return out;
+  }
+  hipError_t run(hipStream_t s) {
+    k_row_sizes<T><<<dim3(strided(ceil_div(most, 4)), unsigned(count)), 256, 0, s>>>(rows_of);
+    return hipGetLastError();
+  }
 };
 
 // The copies that a call needs before its first product.
@@ -1356,22 +1495,47 @@ hipError_t gated_backward_t(const lda_gated_args &a, Arena &ws, bool dry) {
   Matrix<T> gate, value;
   pair_operands<T>(a, true, ws, packs, gate, value);
   T *dab = ws.take<T>(a.rows * pc);
+  float *scale = nullptr, *dx_factor = nullptr, *dw_factor = nullptr;
+  Matrix<T> x_scaled = x;
+  if constexpr (kScaledRows<T>) {
+    Sizes<T> sizes;
+    const float2 *sx = sizes.add(a.x, a.ldx, a.rows, a.width, ws), *sd = sizes.add(a.dh, a.lddh, a.rows, a.hidden, ws);
+    const float2 *sg = sizes.add(a.w_gate, a.ld_gate, a.hidden, a.width, ws);
+    const float2 *sv = sizes.add(a.w_value, a.ld_value, a.hidden, a.width, ws);
+    const int64_t needed = ceil_div(a.rows, 1024);
+    const int groups = int(needed < 256 ? needed : 256);  // k_gated_units: at most 1,024
+    float *tops = ws.take<float>(groups), *x_factor = ws.take<float>(rows);
+    scale = ws.take<float>(rows);
+    dx_factor = ws.take<float>(rows);
+    dw_factor = ws.take<float>(1);
+    T *copy = ws.take<T>(a.rows * k);
+    packs.add(a.x, a.ldx, a.rows, a.width, x_factor, copy, k);
+    x_scaled = Matrix<T>{copy, k};
+    if (!dry) {
+      OPS_TRY(sizes.run(s));
+      k_gated_scales<<<unsigned(groups), 1024, 0, s>>>(sx, sd, sg, sv, rows, a.hidden, a.act, scale, dx_factor,
+                                                    x_factor, tops);
+      OPS_TRY(hipGetLastError());
+      k_gated_units<<<unsigned(groups), 1024, 0, s>>>(tops, groups, rows, x_factor, dw_factor);
+      OPS_TRY(hipGetLastError());
+    }
+  }
   if (!dry) {
     OPS_TRY(packs.run(s));
-    const GatedBackward<T> epi{static_cast<const T *>(a.dh), a.lddh, dab, rows, a.hidden, pc, a.act,
+    const GatedBackward<T> epi{static_cast<const T *>(a.dh), a.lddh, scale, dab, rows, a.hidden, pc, a.act,
                                at_once<T>(a.dh, a.lddh) >= 4};
     OPS_TRY(with_shape<T>(tiles_of<T>(a.rows, pc), [&](auto shape) {
       return product<T, decltype(shape)>(a.rows, pc, k, 1, Rows<T>{x.p, x.ld, rows, k},
                                          PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s);
     }));
   }
-  const Target<T> dx{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, at_once<T>(a.dx, a.lddx), nullptr, 0};
+  const Target<T> dx{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, at_once<T>(a.dx, a.lddx), dx_factor, 1};
   OPS_TRY(product_into<T>(a.rows, a.width, pc, Rows<T>{dab, pc, rows, pc},
                           PairColumns<T>{gate.p, value.p, gate.ld, a.width, a.hidden}, dx, ws, dry, s));
   const int by_g = at_once<T>(dwg, a.width), by_v = at_once<T>(dwv, a.width);
-  const Target<T> dw{dwg, dwv, a.width, a.hidden, true, by_g < by_v ? by_g : by_v, nullptr, 0};
-  return product_into<T>(pc, a.width, a.rows, Columns<T>{dab, pc, pc, rows}, Columns<T>{x.p, x.ld, a.width, rows}, dw,
-                         ws, dry, s);
+  const Target<T> dw{dwg, dwv, a.width, a.hidden, true, by_g < by_v ? by_g : by_v, dw_factor, 0};
+  return product_into<T>(pc, a.width, a.rows, Columns<T>{dab, pc, pc, rows},
+                         Columns<T>{x_scaled.p, x_scaled.ld, a.width, rows}, dw, ws, dry, s);
 }
 
 template <typename T>
