@@ -152,8 +152,8 @@ lda_status lda_gated_backward(const lda_gated_args *a);
  * As an operand of the first two products, in 16-bit types, G is kept without
  * dloss and rounded to the type of the matrices (dbias is summed before); dloss
  * multiplies dx in 32 bits, and x, rounded once more, for dweight (in half
- * precision a row's part of dweight loses bits where its |dloss| is more than
- * some 2^10 times below the largest).  Rows of weight must be finite also where
+ * precision a row's part of dweight loses bits where its |x dloss| is more than
+ * some 2^28 times below the largest).  Rows of weight must be finite also where
  * their word is masked.  dbias is NULL if and only if bias is.  With rows = 0,
  * dweight and dbias are set to zero.
  */

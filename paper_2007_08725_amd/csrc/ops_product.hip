@@ -544,6 +544,13 @@ struct StorePart {
   }
 };
 
+// In half precision operands of gradients are brought into the type's range, by
+// powers of two from the sizes of the rows that they are made of.
+template <typename T>
+constexpr bool kScaledRows = false;
+template <>
+constexpr bool kScaledRows<f16> = true;
+
 // The activation and its derivative.  The normal distribution function by
 // Abramowitz and Stegun, 7.1.26: 1 - Phi(|a|) = exp(-a^2 / 2) (a1 t + .. + a5 t^5) / 2
 // with t = 1 / (1 + p |a| / sqrt 2), within 7.5e-8, the rounding of a value of
@@ -614,11 +621,6 @@ struct GatedForward {
 // In half precision da and db go past the type's range, or below it, long before
 // the gradients that are made of them: each row is multiplied by a power of two
 // (k_gated_scales), which the products' results or operands take back.
-template <typename T>
-constexpr bool kScaledRows = false;
-template <>
-constexpr bool kScaledRows<f16> = true;
-
 template <typename T>
 struct GatedBackward {
   static constexpr bool kRuns = true;
@@ -1000,6 +1002,18 @@ __global__ __launch_bounds__(256) void k_lse_join_few(const float2 *part, int pa
   write_loss(a, m, label_logit, labels, vocab, loss, lse);
 }
 
+// The largest of the threads' values, for every thread of 1,024.
+__device__ inline float group_max(float v, float (&shared)[16]) {
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) v = fmaxf(v, __shfl_xor(v, x));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 16; ++w) v = fmaxf(v, shared[w]);
+  return v;
+}
+
 // The rows' gradients as factors of the products: row_factor = dloss / S for dx
 // and dbias, and x_factor = dloss / unit for the rows of x in dweight, whose
 // result is then multiplied by out[0] = unit / S.  The unit is the smallest
@@ -1008,43 +1022,50 @@ __global__ __launch_bounds__(256) void k_lse_join_few(const float2 *part, int pa
 // counts once, twice, four times), then leave the rows of x unrounded, and no
 // factor is above 1, so that none takes x out of its type's range.  The factors
 // are 0 for rows that are left out.
+//
+// In half precision (x_size: the rows' sizes) another power of two brings
+// the largest |x| |dloss| to 2^14 or above, below 2^15: rows lose bits only where
+// theirs is more than some 2^28 below, instead of where |dloss| is 2^10 to 2^14
+// below the largest.
 __global__ __launch_bounds__(1024) void k_grad_factors(const float *dloss, const float *lse, const int32_t *labels,
-                                                       int rows, int vocab, float s, float *out, float *row_factor,
-                                                       float *x_factor) {
-  __shared__ float tops[16], lows[16];
+                                                       const float2 *x_size, int rows, int vocab, float s, float *out,
+                                                       float *row_factor, float *x_factor) {
+  __shared__ float shared[16];
+  auto in = [&](int m) { return labels[m] >= 0 && labels[m] < vocab; };
   float top = 0.0f, low = INFINITY;
   for (int m = threadIdx.x; m < rows; m += 1024) {
     const float d = fabsf(dloss[m]);
-    if (labels[m] >= 0 && labels[m] < vocab && d < INFINITY && d > 0.0f) {
+    if (in(m) && d < INFINITY && d > 0.0f) {
       top = fmaxf(top, d);
       low = fminf(low, d);
     }
   }
-  for (int x = 1; x < 64; x <<= 1) {
-    top = fmaxf(top, __shfl_xor(top, x));
-    low = fminf(low, __shfl_xor(low, x));
-  }
-  if ((threadIdx.x & 63) == 0) {
-    tops[threadIdx.x >> 6] = top;
-    lows[threadIdx.x >> 6] = low;
-  }
-  __syncthreads();
-  for (int w = 0; w < 16; ++w) {
-    top = fmaxf(top, tops[w]);
-    low = fminf(low, lows[w]);
-  }
-  float unit = 0x1p-100f;  // at least: below, the quotients would leave the range
+  top = group_max(top, shared);
+  low = -group_max(-low, shared);
+  float unit = x_size ? 0x1p-70f : 0x1p-100f;  // at least: below, the quotients would leave the range
   if (top > unit) {
     int e_top, e_low;
     frexpf(top, &e_top);
     unit = ldexpf(frexpf(low, &e_low), e_top);
     if (unit < top) unit = fminf(2.0f * unit, 0x1.fffffep127f);
   }
-  if (threadIdx.x == 0) out[0] = unit / s;
+  float shift = 1.0f;
+  if (x_size) {
+    float most = 0.0f;
+    for (int m = threadIdx.x; m < rows; m += 1024) {
+      const float d = fabsf(dloss[m]);
+      if (in(m) && lse[m] != -INFINITY && d < INFINITY) most = fmaxf(most, x_size[m].x * (d / unit));
+    }
+    most = group_max(most, shared);
+    int e = 15;
+    if (most > 0.0f) frexpf(most, &e);  // most < 2^e
+    shift = ldexpf(1.0f, 15 - (e < -25 ? -25 : e));
+  }
+  if (threadIdx.x == 0) out[0] = unit / s / shift;
   for (int m = threadIdx.x; m < rows; m += 1024) {
-    const bool kept = labels[m] >= 0 && labels[m] < vocab && lse[m] != -INFINITY;
+    const bool kept = in(m) && lse[m] != -INFINITY;
     row_factor[m] = kept ? dloss[m] / s : 0.0f;
-    x_factor[m] = kept ? dloss[m] / unit : 0.0f;
+    x_factor[m] = kept ? dloss[m] / unit * shift : 0.0f;
   }
 }
 
@@ -1176,18 +1197,6 @@ __global__ __launch_bounds__(256) void k_row_sizes(const SizedRows<T> all) {
     const float2 s = a.aligned ? row_size<T, true>(row, a.cols, lane) : row_size<T, false>(row, a.cols, lane);
     if (lane == 0) a.out[r] = s;
   }
-}
-
-// The largest of the threads' values, for every thread of 1,024.
-__device__ inline float group_max(float v, float (&shared)[16]) {
-#pragma unroll
-  for (int x = 1; x < 64; x <<= 1) v = fmaxf(v, __shfl_xor(v, x));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < 16; ++w) v = fmaxf(v, shared[w]);
-  return v;
 }
 
 // Powers of two that bring the rows of da and db below 2^15 in magnitude, by
@@ -1599,6 +1608,8 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   const Matrix<T> x = operand<T>(a.x, a.ldx, a.rows, a.width, ws, packs);
   const Matrix<T> w = operand<T>(a.weight, a.ld_weight, a.vocab, a.width, ws, packs);
   float *top = ws.take<float>(1), *row_factor = ws.take<float>(rows), *x_factor = ws.take<float>(rows);
+  Sizes<T> sizes;
+  const float2 *x_size = kScaledRows<T> ? sizes.add(a.x, a.ldx, a.rows, a.width, ws) : nullptr;
   T *x_scaled = ws.take<T>(a.rows * k);
   T *grad = ws.take<T>(a.rows * piece);
   float *col_part = a.bias ? ws.take<float>(int64_t(mtiles) * piece) : nullptr;
@@ -1607,7 +1618,9 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   const int64_t cols4 = round_up(a.width, 4);
   float *dx_part = ws.take<float>(splits * a.rows * cols4);
   if (!dry) {
-    k_grad_factors<<<1, 1024, 0, s>>>(a.dloss, a.lse, a.labels, rows, a.vocab, kGradUnit<T>, top, row_factor, x_factor);
+    if constexpr (kScaledRows<T>) OPS_TRY(sizes.run(s));
+    k_grad_factors<<<1, 1024, 0, s>>>(a.dloss, a.lse, a.labels, x_size, rows, a.vocab, kGradUnit<T>, top, row_factor,
+                                      x_factor);
     OPS_TRY(hipGetLastError());
     packs.add(a.x, a.ldx, a.rows, a.width, x_factor, x_scaled, k);
     OPS_TRY(packs.run(s));

@@ -97,3 +97,70 @@ def test_gated_half_precision_rows_without_gradient(ops):  # noqa: F811
     x[7, 3] = float("nan")
     dx = ops.gated_backward(dh, x, wg, wv)[0]
     assert bool(dx[7].isnan().all()) and torch.equal(dx[[i for i in keep if i != 7]], got[0][[i for i in keep if i != 7]])
+
+
+# ---------------------------------------------------- softmax cross entropy ---
+def xent_gradients(ops, x, w, labels, bias, dloss):  # noqa: F811
+    """The operator's dx and dweight, the formulas' in 64 bits, and bounds on what is off.
+
+    G = p - [label] is off by the logits' errors times p, by its rounding u, and
+    in half precision, where it is kept times 2^14, by half a step of the
+    subnormal numbers, 2^-39.  x dloss is off by its rounding u, and by 2^-39 of
+    the largest, which is kept at 2^14 at least.
+    """
+    dtype, rows, width, vocab = x.dtype, x.shape[0], x.shape[1], w.shape[0]
+    _, lse = ops.softmax_xent(x, w, labels, bias)
+    dx, dw, _ = ops.softmax_xent_backward(dloss, lse, x, w, labels, bias)
+    x8, w8, d8 = x.to(F8), w.to(F8), dloss.to(F8)[:, None]
+    z, mag = x8 @ w8.t(), x8.abs() @ w8.abs().t()
+    if bias is not None:
+        z, mag = z + bias.to(F8), mag + bias.to(F8).abs()
+    top = torch.logsumexp(z, 1, keepdim=True)
+    p = torch.exp(z - top)
+    # a logit's error, that of the lse (the largest logit's, the sum's, its own
+    # rounding), and of the exponential's argument, of at most 64 where p is not 0
+    ez = g(width) * mag
+    ep = p * (2 * (ez + ez.amax(1, keepdim=True) + g(vocab) + 2 * E * top.abs()) + 8 * E * 64)
+    grad = p.clone()
+    grad[torch.arange(rows, device="cuda"), labels.long()] -= 1
+    u = (U[dtype] if dtype != torch.float32 else 0.0) + 4 * E
+    eg = ep + u * grad.abs() + 2.0 ** -39
+    xd = (x8 * d8).abs()
+    exd = u * xd + 2.0 ** -39 * xd.max()
+    refs = ((grad * d8) @ w8, (grad * d8).t() @ x8)
+    bounds = (((eg + g(vocab) * grad.abs()) * d8.abs()) @ w8.abs(),
+              (eg + g(rows) * grad.abs()).t() @ xd + grad.abs().t() @ exd)
+    return dict(dx=(dx, refs[0], bounds[0]), dweight=(dw, refs[1], bounds[1]))
+
+
+@pytest.mark.parametrize("rows,width,vocab", [(12, 64, 200), (96, 40, 400)])
+@pytest.mark.parametrize("below", [8, 14, 20, 24])
+def test_softmax_xent_half_precision_rows_of_unlike_gradients(ops, rows, width, vocab, below):  # noqa: F811
+    """Rows whose gradient is 2^-below of the largest, with words of their own: their part of dweight keeps its bits."""
+    x, w = rand(1, rows, width, dtype=F16), rand(2, vocab, width, scale=0.3 * width ** -0.5, dtype=F16)
+    small = torch.arange(rows, device="cuda") % 2 == 1
+    # the small rows' words are all but impossible for the others
+    labels = torch.arange(rows, dtype=torch.int32, device="cuda")
+    bias = rand(3, vocab)
+    bias[:rows][small] = -40.0
+    dloss = torch.full((rows,), 2.0 ** 12, device="cuda")
+    dloss[small] = torch.linspace(1.0, 1.9, int(small.sum()), device="cuda") * 2.0 ** (12 - below)
+    got, ref, bound = xent_gradients(ops, x, w, labels, bias, dloss)["dweight"]
+    telling("dweight", ref[:rows], bound[:rows], F16)
+    check("dweight", got, ref, bound)
+
+
+@pytest.mark.parametrize("x_scale,w_scale,name", [(2e4, 1e-4, "dweight"), (1e-4, 2e4, "dx")])
+@pytest.mark.parametrize("dloss_scale", [2.0 ** -26, 2.0 ** -20])
+@pytest.mark.parametrize("rows", [12, 200])
+def test_softmax_xent_half_precision_small_gradients(ops, x_scale, w_scale, name, dloss_scale, rows):  # noqa: F811
+    """Gradients far below half precision's range, of results that are in it."""
+    x, w = rand(1, rows, 64, scale=0.5 * x_scale, dtype=F16), rand(2, 300, 64, scale=w_scale / 8, dtype=F16)
+    if name == "dx":
+        w = rand(2, 300, 64, scale=0.5 * w_scale, dtype=F16)
+        x = rand(1, rows, 64, scale=x_scale / 8, dtype=F16)
+    labels = (torch.arange(rows, device="cuda") * 7 % 300).to(torch.int32)
+    got, ref, bound = xent_gradients(ops, x, w, labels, None, rand(4, rows, scale=dloss_scale))[name]
+    shown = ref[labels.long().unique()] if name == "dweight" else ref
+    telling(name, shown, bound[labels.long().unique()] if name == "dweight" else bound, F16)
+    check(name, got, ref, bound)
