@@ -551,12 +551,22 @@ constexpr bool kScaledRows = false;
 template <>
 constexpr bool kScaledRows<f16> = true;
 
-// The activation and its derivative.  The normal distribution function by
-// Abramowitz and Stegun, 7.1.26: 1 - Phi(|a|) = exp(-a^2 / 2) (a1 t + .. + a5 t^5) / 2
-// with t = 1 / (1 + p |a| / sqrt 2), within 7.5e-8, the rounding of a value of
-// order 1 in 32 bits; the exponential is the derivative's too.
+// The activation and its derivative, for matrices of type T.  In 16-bit types the
+// normal distribution function by Abramowitz and Stegun, 7.1.26:
+// 1 - Phi(|a|) = exp(-a^2 / 2) (a1 t + .. + a5 t^5) / 2 with t = 1 / (1 + p |a| / sqrt 2),
+// within 7.5e-8 (not of itself: of 1), and the exponential is the derivative's
+// too.  In single precision that is more than Phi's rounding where it is small:
+// the complementary error function.
+template <typename T>
 __device__ inline void gate(int act, float a, float &p, float &dp) {
-  if (act == LDA_GELU) {
+  if constexpr (sizeof(T) == 4) {
+    if (act == LDA_GELU) {
+      const float phi = 0.5f * erfcf(-0.70710678118654752f * a);
+      p = a * phi;
+      dp = phi + a * 0.3989422804014327f * expf(-0.5f * a * a);
+      return;
+    }
+  } else if (act == LDA_GELU) {
     const float bell = __builtin_amdgcn_exp2f(-0.5f * kLog2e * a * a);
     const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * 0.70710678118654752f * fabsf(a));
     const float tail = 0.5f * bell * t *
@@ -602,7 +612,7 @@ struct GatedForward {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           float p, dp;
-          gate(act, c[i][j][r], p, dp);
+          gate<T>(act, c[i][j][r], p, dp);
           v[r] = p * c[i][j + 1][r];
         }
         store4(h + m * ld + f, v, hidden - f, whole);
@@ -648,7 +658,7 @@ struct GatedBackward {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           float p, dp;
-          gate(act, c[i][j][r], p, dp);
+          gate<T>(act, c[i][j][r], p, dp);
           d[j][r] = f + r < hidden ? dhv[r] * c[i][j + 1][r] * dp : 0.0f;
           d[j + 1][r] = f + r < hidden ? dhv[r] * p : 0.0f;
         }
@@ -911,7 +921,7 @@ __global__ __launch_bounds__(256) void k_gated_few(const T *x, int64_t ldx, cons
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     float p, dp;
-    gate(act, c[0][r], p, dp);
+    gate<T>(act, c[0][r], p, dp);
     if (f + r < hidden) h[q * ldh + f + r] = T(p * c[1][r]);
   }
 }

@@ -99,6 +99,26 @@ def test_gated_half_precision_rows_without_gradient(ops):  # noqa: F811
     assert bool(dx[7].isnan().all()) and torch.equal(dx[[i for i in keep if i != 7]], got[0][[i for i in keep if i != 7]])
 
 
+@pytest.mark.parametrize("rows", [13, 4001])
+def test_gelu_in_single_precision(ops, rows):  # noqa: F811
+    """gelu and its derivative relative to themselves, on both sides of 0.
+
+    Phi(a) = erfc(-a / sqrt 2) / 2: the argument is off by 2 e of itself, which
+    changes Phi by up to a^2 + 1 times that; erfc by 8 e of itself.  The bell
+    exp(-a^2 / 2) is off by a^2 e, and 6 e of itself.
+    """
+    x = torch.linspace(-6, 6, rows, device="cuda")[:, None].contiguous()
+    one = torch.ones(1, 1, device="cuda")
+    a = x.to(F8)
+    p, dp = gate("gelu", a)
+    phi, bell = torch.special.ndtr(a), a.abs() * torch.exp(-0.5 * a * a) / math.sqrt(2 * math.pi)
+    rel = (2 * (a * a + 1) + 8) * E
+    check("h", ops.gated(x, one, one, "gelu"), p * a, (rel + 2 * E) * (p * a).abs())
+    dx, _, _ = ops.gated_backward(torch.ones_like(x), x, one, one, "gelu")
+    edp = rel * phi + (a * a + 6) * E * bell
+    check("dx", dx, a * dp + p, a.abs() * edp + (rel + 4 * E) * p.abs() + 4 * E * (a * dp).abs())
+
+
 # ---------------------------------------------------- softmax cross entropy ---
 def xent_gradients(ops, x, w, labels, bias, dloss):  # noqa: F811
     """The operator's dx and dweight, the formulas' in 64 bits, and bounds on what is off.
