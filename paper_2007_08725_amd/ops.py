@@ -8,6 +8,10 @@ operator runs in the library's HIP kernels; there is no CPU fallback.
 
 Matrices are float32, bfloat16 or float16, one type per call, with unit column
 stride; rows may be strided.  Results are the same bits on every run.
+
+The operators are no part of torch's autograd graph: gradients come from the
+``_backward`` calls.  Tensors that require a gradient are refused while autograd
+records (``ValueError``); call under ``torch.no_grad()`` or on detached tensors.
 """
 from __future__ import annotations
 
@@ -86,6 +90,12 @@ def _check(status):
         raise LDAError(status, load_library().lda_last_error(None).decode())
 
 
+def _refuse_autograd(name, t):
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError("%s requires a gradient, which torch would not get: call the operator under torch.no_grad() "
+                         "and its _backward" % name)
+
+
 def _matrix(name, t, like=None, shape=None):
     """A device matrix with unit column stride, of the type and device of ``like``."""
     if not isinstance(t, torch.Tensor) or t.dim() != 2:
@@ -102,6 +112,7 @@ def _matrix(name, t, like=None, shape=None):
         raise ValueError("%s must have columns" % name)
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError("%s must have unit column stride" % name)
+    _refuse_autograd(name, t)
     return t
 
 
@@ -112,6 +123,7 @@ def _vector(name, t, like, length, dtype):
         raise ValueError("%s must be %s on the device of x" % (name, dtype))
     if length > 1 and t.stride(0) != 1:
         raise ValueError("%s must be contiguous" % name)
+    _refuse_autograd(name, t)
     return t
 
 
