@@ -53,6 +53,9 @@ class WordModel:
         self.params = dict(norm_weight=torch.ones(K, device=device), norm_bias=torch.zeros(K, device=device),
                            w_gate=normal(hidden, K, scale=K ** -0.5), w_value=normal(hidden, K, scale=K ** -0.5),
                            weight=normal(V, hidden, scale=0.1 * hidden ** -0.5), bias=torch.log(freq / freq.sum()))
+        # half precision takes the gradients of this many times the mean loss: those of the mean over a batch of
+        # thousands are below its normal numbers
+        self._loss_scale = 1024.0 if dtype == torch.float16 else 1.0
         self._moments = {n: (torch.zeros_like(p), torch.zeros_like(p)) for n, p in self.params.items()}
         self._steps = 0
 
@@ -81,11 +84,13 @@ class WordModel:
     def step(self, theta, words, lr: float = 1e-2):
         """One Adam step on a batch of tokens; returns the batch's mean loss, on the device."""
         loss, kept = self.loss(theta, words)
-        grads = self.gradients(kept, torch.full_like(loss, 1.0 / loss.shape[0]))
+        grads = self.gradients(kept, torch.full_like(loss, self._loss_scale / loss.shape[0]))
         self._steps += 1
         c1, c2 = 1 - 0.9 ** self._steps, 1 - 0.999 ** self._steps
         for name, param in self.params.items():
             g = grads[name].float()
+            if self._loss_scale != 1.0:
+                g = g / self._loss_scale
             m, v = self._moments[name]
             m.mul_(0.9).add_(g, alpha=0.1)
             v.mul_(0.999).addcmul_(g, g, value=0.001)
