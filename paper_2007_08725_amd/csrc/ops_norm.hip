@@ -400,6 +400,19 @@ bool aligned16(const void *p, int64_t ld) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % kChunk<T> == 0;
 }
 
+// Launches fn(first row, rows) for all rows, `groups` of them to a workgroup of
+// `threads`: in more than one launch where one would have 2^32 threads.
+template <typename Fn>
+hipError_t by_rows(int64_t rows, int64_t threads, int64_t groups, Fn fn) {
+  const int64_t most = 0xffffffffll / threads * groups;
+  for (int64_t first = 0; first < rows; first += most) {
+    fn(first, rows - first < most ? rows - first : most);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <typename T>
 hipError_t norm_forward_t(const lda_norm_args &a) {
   if (a.rows == 0) return hipSuccess;
@@ -408,15 +421,20 @@ hipError_t norm_forward_t(const lda_norm_args &a) {
   T *y = static_cast<T *>(a.y);
   const bool aligned = a.cols % kChunk<T> == 0 && aligned16<T>(x, a.ldx) && aligned16<T>(y, a.ldy) &&
                        aligned16<T>(w, 0) && aligned16<T>(b, 0);
+  hipError_t e = hipSuccess;
   const bool done = with_shape<T, false>(aligned, a.cols, [&](auto shape) {
     typedef decltype(shape) S;
-    constexpr int threads = threads_of(S::LANES);
-    k_norm<T, S::LANES, S::V, S::Aligned><<<unsigned(ceil_div(a.rows, threads / S::LANES)), threads, 0, s>>>(
-        x, a.ldx, w, b, a.rows, a.cols, a.eps, y, a.ldy, a.mean, a.rstd);
+    constexpr int threads = threads_of(S::LANES), groups = threads / S::LANES;
+    e = by_rows(a.rows, threads, groups, [&](int64_t m, int64_t rows) {
+      k_norm<T, S::LANES, S::V, S::Aligned><<<unsigned(ceil_div(rows, groups)), threads, 0, s>>>(
+          x + m * a.ldx, a.ldx, w, b, rows, a.cols, a.eps, y + m * a.ldy, a.ldy, a.mean + m, a.rstd + m);
+    });
   });
-  if (!done)
-    k_norm_wide<T><<<unsigned(a.rows), 1024, 0, s>>>(x, a.ldx, w, b, a.cols, a.eps, y, a.ldy, a.mean, a.rstd);
-  return hipGetLastError();
+  if (done) return e;
+  return by_rows(a.rows, 1024, 1, [&](int64_t m, int64_t rows) {
+    k_norm_wide<T><<<unsigned(rows), 1024, 0, s>>>(x + m * a.ldx, a.ldx, w, b, a.cols, a.eps, y + m * a.ldy, a.ldy,
+                                                   a.mean + m, a.rstd + m);
+  });
 }
 
 template <typename T>
@@ -451,12 +469,12 @@ hipError_t norm_backward_t(const lda_norm_args &a, Arena &ws, bool dry) {
     part = a.dweight ? ws.take<float>(2 * parts * a.cols) : nullptr;
     float *sums = ws.take<float>(2 * a.rows);
     if (!dry) {
-      if (a.rows) {
-        auto kernel = aligned ? k_norm_wide_sums<T, true> : k_norm_wide_sums<T, false>;
-        kernel<<<unsigned(a.rows), 1024, 0, s>>>(dy, a.lddy, x, a.ldx, w, a.mean, a.rstd, a.rows, a.cols, sums);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-      }
+      auto sum = aligned ? k_norm_wide_sums<T, true> : k_norm_wide_sums<T, false>;
+      e = by_rows(a.rows, 1024, 1, [&](int64_t m, int64_t rows) {
+        sum<<<unsigned(rows), 1024, 0, s>>>(dy + m * a.lddy, a.lddy, x + m * a.ldx, a.ldx, w, a.mean + m, a.rstd + m,
+                                            a.rows, a.cols, sums + m);
+      });
+      if (e != hipSuccess) return e;
       auto kernel = aligned ? k_norm_wide_grad<T, true> : k_norm_wide_grad<T, false>;
       kernel<<<dim3(unsigned(strips), unsigned(parts)), 256, 0, s>>>(dy, a.lddy, x, a.ldx, w, a.mean, a.rstd, sums,
                                                                     a.rows, a.cols, per, dx, a.lddx, part);
