@@ -153,8 +153,6 @@ struct Grid {
 // what a lane whose chunk lies past the end of k reads instead
 __device__ const u32x4 kZeroChunk = {0, 0, 0, 0};
 
-typedef const __attribute__((address_space(1))) void *global_ptr;
-typedef __attribute__((address_space(3))) void *lds_ptr;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
@@ -244,44 +242,57 @@ struct Stage {
   }
 };
 
-// The loads of a step into LDS and the reads of a step's fragments.  Macros,
-// because the compiler has to see both in one function whose restricted
-// arguments say that they touch different stages: else it waits for every load
-// in flight before it reads.
-#define LOAD_STEP(stage, op, step, to)                                                                       \
-  do {                                                                                                       \
-    const int64_t ahead_ = (op).ahead(step);                                                                 \
-    _Pragma("unroll") for (int i_ = 0; i_ < decltype(stage)::LOADS; ++i_) __builtin_amdgcn_global_load_lds(  \
-        (global_ptr)(stage).from(op, step, ahead_, i_),                                                      \
-        (lds_ptr)((to) + (i_ * decltype(stage)::WAVES_ + wave) * 1024), 16, 0, 0);                           \
-  } while (0)
+// 1 KiB into LDS at `to` (the same for all lanes), 16 bytes from each lane's
+// `from`.  In assembly, since the compiler waits for every load into LDS that it
+// knows to be in flight before it reads LDS, whichever stage either is of: here
+// stage_barrier waits, and the clobbered memory keeps reads on their side of it.
+// No register is written; `s_nop` is the state between M0 and its use.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // M0 in the clobbers: reserved, so the compiler sets it where it uses it
+__device__ inline void load_to_lds(const char *from, lds_char *to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(uint32_t(uintptr_t(to))), "v"(from)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
 
-#define READ_FRAGMENTS(stage, order, f, count, tile, row0)                                                            \
-  do {                                                                                                                \
-    typedef decltype(stage) S_;                                                                                       \
-    const int q_ = lane & 15, group_ = lane >> 4;                                                                     \
-    _Pragma("unroll") for (int i_ = 0; i_ < (count); ++i_) {                                                          \
-      if constexpr (S_::CONTIGUOUS) {                                                                                 \
-        const int row_ = (row0) + order::row(i_, q_);                                                                 \
-        (f)[i_] = *(const lds_u32x4 *)((tile) + row_ * 64 + (group_ ^ chunk_turn(row_)) * 16);                        \
-      } else if constexpr (sizeof(T) == 2) {                                                                          \
-        /* lane q reads four rows of line q / 4: those that lanes 4 (q % 4) on get */                                 \
-        const int line_ = group_ * 8 + (q_ >> 2), row_ = (row0) + order::row(i_, (q_ & 3) * 4);                       \
-        const int at_ = line_ * S_::LINE + ((row_ >> 4) ^ slot_turn<T, S_::ROWS>(line_)) * 32 +                       \
-                        (((row_ & 15) * 2) ^ (part_turn<T>(line_) * 16));                                             \
-        const s16x4 lo_ = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((tile) + at_));                       \
-        const s16x4 hi_ = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((tile) + at_ + 4 * S_::LINE));        \
-        const u32x2 l_ = __builtin_bit_cast(u32x2, lo_), h_ = __builtin_bit_cast(u32x2, hi_);                         \
-        (f)[i_] = u32x4{l_[0], l_[1], h_[0], h_[1]};                                                                  \
-      } else {                                                                                                        \
-        _Pragma("unroll") for (int e_ = 0; e_ < 4; ++e_) {                                                            \
-          const int line_ = group_ * 4 + e_, row_ = (row0) + order::row(i_, q_);                                      \
-          (f)[i_][e_] = *(const lds_u32 *)((tile) + line_ * S_::LINE + ((row_ >> 4) ^ slot_turn<T, S_::ROWS>(line_)) * 64 +\
-                                           (((row_ >> 2 & 3) ^ part_turn<T>(line_)) * 16 + (row_ & 3) * 4));          \
-        }                                                                                                             \
-      }                                                                                                               \
-    }                                                                                                                 \
-  } while (0)
+// The loads of an operand's part of a step into its stage.
+template <typename S, typename Op>
+__device__ inline void load_step(const S &stage, const Op &op, int step, int wave, lds_char *to) {
+  const int64_t ahead = op.ahead(step);
+#pragma unroll
+  for (int i = 0; i < S::LOADS; ++i) load_to_lds(stage.from(op, step, ahead, i), to + (i * S::WAVES_ + wave) * 1024);
+}
+
+// A wave's fragments of a step, from row `row0` of the operand's part on.
+template <typename T, typename S, typename Order, int N>
+__device__ inline void read_fragments(u32x4 (&f)[N], const lds_char *tile, int row0, int lane) {
+  const int q = lane & 15, group = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if constexpr (S::CONTIGUOUS) {
+      const int row = row0 + Order::row(i, q);
+      f[i] = *(const lds_u32x4 *)(tile + row * 64 + (group ^ chunk_turn(row)) * 16);
+    } else if constexpr (sizeof(T) == 2) {
+      // lane q reads four rows of line q / 4: those that lanes 4 (q % 4) on get
+      const int line = group * 8 + (q >> 2), row = row0 + Order::row(i, (q & 3) * 4);
+      const int at = line * S::LINE + ((row >> 4) ^ slot_turn<T, S::ROWS>(line)) * 32 +
+                     (((row & 15) * 2) ^ (part_turn<T>(line) * 16));
+      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + at)));
+      const u32x2 hi =
+          __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + at + 4 * S::LINE)));
+      f[i] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int line = group * 4 + e, row = row0 + Order::row(i, q);
+        f[i][e] = *(const lds_u32 *)(tile + line * S::LINE + ((row >> 4) ^ slot_turn<T, S::ROWS>(line)) * 64 +
+                                     (((row >> 2 & 3) ^ part_turn<T>(line)) * 16 + (row & 3) * 4));
+      }
+    }
+  }
+}
 
 // Every wave's reads and its older loads are done; those of the last `Flying`
 // loads of each wave may be in flight.
@@ -299,9 +310,7 @@ __device__ inline void stage_barrier() {
 // multiplied, the next step's are read and three steps' loads are in flight.
 // The loads run over the ends of tiles, so that a tile's first steps are there
 // when the epilogue of the tile before is done.
-//
-// `fill` and `data` are both the stages in LDS: between two barriers the stage
-// that is filled is not the one that is read.
+// Between two barriers the stage that is filled is not the one that is read.
 //
 // What bounds it: a CU takes 64 bytes a cycle from its L2, so that at the
 // matrix unit's rate a 128 x 128 tile needs all of that and a 256 x 256 tile
@@ -311,7 +320,7 @@ __device__ inline void stage_barrier() {
 // busy 59% of the cycles, at a clock of about 1.8 GHz (2.4 GHz at most).
 template <typename T, int BM, int BN, int WM, int WN, typename L, typename R, typename Epilogue>
 __device__ inline void walk_tiles(const Grid &g, const L &left, const R &right, const Epilogue &epilogue,
-                                  lds_char *__restrict fill, const lds_char *__restrict data, char *scratch) {
+                                  lds_char *stages, char *scratch) {
   constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16, WAVES = WM * WN;
   constexpr int STAGE = (BM + BN) * 64;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -368,14 +377,14 @@ __device__ inline void walk_tiles(const Grid &g, const L &left, const R &right, 
   aim();
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    LOAD_STEP(from_l, left, ahead_step, fill + i * STAGE);
-    LOAD_STEP(from_r, right, ahead_step, fill + i * STAGE + BM * 64);
+    load_step(from_l, left, ahead_step, wave, stages + i * STAGE);
+    load_step(from_r, right, ahead_step, wave, stages + i * STAGE + BM * 64);
     advance();
   }
   stage_barrier<0>();
   u32x4 al[MI], ar[NI], bl[MI], br[NI];
-  READ_FRAGMENTS(from_l, OrderL, al, MI, data, wm * TM);
-  READ_FRAGMENTS(from_r, OrderR, ar, NI, data + BM * 64, wn * TN);
+  read_fragments<T, StageL, OrderL>(al, stages, wm * TM, lane);
+  read_fragments<T, StageR, OrderR>(ar, stages + BM * 64, wn * TN, lane);
   int slot = 0;  // the stage of the step that is multiplied
   for (; item < last; item += width) {
     int mt, nt;
@@ -391,17 +400,17 @@ __device__ inline void walk_tiles(const Grid &g, const L &left, const R &right, 
     for (int steps = min(g.split, g.steps - split * g.split); steps > 0; steps -= 2) {
       stage_barrier<2 * LOADS>();
       const int odd = (slot + 1) & 3, even = (slot + 2) & 3;
-      READ_FRAGMENTS(from_l, OrderL, bl, MI, data + odd * STAGE, wm * TM);
-      READ_FRAGMENTS(from_r, OrderR, br, NI, data + odd * STAGE + BM * 64, wn * TN);
-      LOAD_STEP(from_l, left, ahead_step, fill + slot * STAGE);
-      LOAD_STEP(from_r, right, ahead_step, fill + slot * STAGE + BM * 64);
+      load_step(from_l, left, ahead_step, wave, stages + slot * STAGE);
+      load_step(from_r, right, ahead_step, wave, stages + slot * STAGE + BM * 64);
+      read_fragments<T, StageL, OrderL>(bl, stages + odd * STAGE, wm * TM, lane);
+      read_fragments<T, StageR, OrderR>(br, stages + odd * STAGE + BM * 64, wn * TN, lane);
       multiply(al, ar);
       advance();
       stage_barrier<2 * LOADS>();
-      READ_FRAGMENTS(from_l, OrderL, al, MI, data + even * STAGE, wm * TM);
-      READ_FRAGMENTS(from_r, OrderR, ar, NI, data + even * STAGE + BM * 64, wn * TN);
-      LOAD_STEP(from_l, left, ahead_step, fill + odd * STAGE);
-      LOAD_STEP(from_r, right, ahead_step, fill + odd * STAGE + BM * 64);
+      load_step(from_l, left, ahead_step, wave, stages + odd * STAGE);
+      load_step(from_r, right, ahead_step, wave, stages + odd * STAGE + BM * 64);
+      read_fragments<T, StageL, OrderL>(al, stages + even * STAGE, wm * TM, lane);
+      read_fragments<T, StageR, OrderR>(ar, stages + even * STAGE + BM * 64, wn * TN, lane);
       multiply(bl, br);
       advance();
       slot = even;
@@ -410,21 +419,13 @@ __device__ inline void walk_tiles(const Grid &g, const L &left, const R &right, 
   }
 }
 
-// The LDS address, as one that the compiler does not know: two arguments that
-// it can prove equal lose their `restrict`.
-__device__ inline lds_char *unfolded(char *lds) {
-  uint32_t none = 0;
-  asm volatile("" : "+s"(none));
-  return (lds_char *)lds + none;
-}
-
 // BM x BN = 256 x 256: eight waves of 128 x 64, one workgroup a CU.  128 x 128
 // and 64 x 64, where those leave CUs without work: four waves, several
 // workgroups a CU.
 template <typename T, int BM, int BN, int WM, int WN, typename L, typename R, typename Epilogue>
 __global__ __launch_bounds__(64 * WM *WN, 2) void k_product(Grid g, L left, R right, Epilogue epilogue) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  walk_tiles<T, BM, BN, WM, WN>(g, left, right, epilogue, unfolded(lds), unfolded(lds), lds + 4 * (BM + BN) * 64);
+  walk_tiles<T, BM, BN, WM, WN>(g, left, right, epilogue, (lds_char *)lds, lds + 4 * (BM + BN) * 64);
 }
 
 // ------------------------------------------------------------- epilogues ----
