@@ -21,6 +21,14 @@ WALK_GATED = [(SHORT, 8197, 129, 1637), ([F32], 1500, 71, 3767), ([F32], 36, 143
 WALK_XENT = [(SHORT, 130, 1312, 34067), (SHORT, 4305, 68, 4033), (SHORT, 3784, 138, 42168), (SHORT, 21, 443, 40688),
              ([F32], 23, 608, 17785), ([F32], 8197, 1374, 264), ([F32], 8197, 477, 8667)]
 
+# The tiles of the gradients' products (operands read transposed, whole or in
+# parts, added to an earlier piece's) at the sizes that the shapes above leave
+# out; vocabularies of several pieces in each type, with a short last one.
+GRADIENT_GATED = [(SHORT, 4100, 1032, 2050), (SHORT, 1500, 1368, 718), (SHORT, 4950, 1688, 2329),
+                  ([F32], 2049, 1000, 1500), ([F32], 2639, 1602, 1354)]
+GRADIENT_XENT = [(SHORT, 1500, 1000, 8200), (SHORT, 4100, 520, 35000), (SHORT, 4100, 264, 35000),
+                 (SHORT, 6817, 69, 19772), ([F32], 1989, 70, 42247), ([F32], 2688, 1565, 219)]
+
 
 def each(shapes):
     return [(t, *s) for types, *s in shapes for t in types]
@@ -52,3 +60,20 @@ def test_several_tiles_a_workgroup_same_bits(ops, dtype):  # noqa: F811
     for _ in range(4):
         for a, b in zip(first, run()):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,rows,width,hidden", each(GRADIENT_GATED))
+def test_gated_gradient_tiles(ops, dtype, rows, width, hidden):  # noqa: F811
+    gated_case(ops, dtype, rows, width, hidden, "gelu" if hidden % 2 else "sigmoid")
+
+
+@pytest.mark.parametrize("dtype,rows,width,vocab", each(GRADIENT_XENT))
+def test_softmax_xent_gradient_tiles(ops, dtype, rows, width, vocab):  # noqa: F811
+    xent_case(ops, dtype, rows, width, vocab, rows % 2 == 1)
+
+
+@pytest.mark.parametrize("dtype", SHORT + [F32])
+@pytest.mark.parametrize("width,pad,offset", [(1000, 8, 8), (1001, 3, 1)])
+def test_gradient_tiles_of_strided_matrices(ops, dtype, width, pad, offset):  # noqa: F811
+    gated_case(ops, dtype, 2049, width, 1503, "silu", pad, offset)
+    xent_case(ops, dtype, 2049, width, 9001, True, pad, offset)
