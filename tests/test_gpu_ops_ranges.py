@@ -77,6 +77,12 @@ def test_gated_half_precision_gradients_of_any_size(ops, act, rows, width, hidde
         check(name, got[name], refs[name], bounds[name])
 
 
+@pytest.mark.parametrize("scales", SCALES)
+def test_gated_half_precision_gradients_of_many_rows(ops, scales):  # noqa: F811
+    """More rows than one workgroup finds the scales of."""
+    test_gated_half_precision_gradients_of_any_size(ops, "silu", 2500, 40, 72, True, scales)
+
+
 def test_gated_half_precision_rows_without_gradient(ops):  # noqa: F811
     """A row whose gradient is 0 takes no part, whatever its size, and one with NaN stays in its row of dx."""
     rows, width, hidden = 40, 48, 24
