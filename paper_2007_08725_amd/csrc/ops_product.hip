@@ -374,17 +374,32 @@ __device__ inline void walk_tiles(const Grid &g, const L &left, const R &right, 
         }
   };
 
+  auto load = [&](int stage) {
+    load_step(from_l, left, ahead_step, wave, stages + stage * STAGE);
+    load_step(from_r, right, ahead_step, wave, stages + stage * STAGE + BM * 64);
+  };
+  auto read = [&](int stage, u32x4(&l)[MI], u32x4(&r)[NI]) {
+    read_fragments<T, StageL, OrderL>(l, stages + stage * STAGE, wm * TM, lane);
+    read_fragments<T, StageR, OrderR>(r, stages + stage * STAGE + BM * 64, wn * TN, lane);
+  };
+  // the loads' addresses of two transposed operands do not fit beside the
+  // fragments that are read
+  constexpr bool kLoadsFirst = !L::kContiguous && !R::kContiguous;
+  auto read_or_load = [&](int from, u32x4(&l)[MI], u32x4(&r)[NI], int to) {
+    if constexpr (kLoadsFirst) load(to);
+    read(from, l, r);
+    if constexpr (!kLoadsFirst) load(to);
+  };
+
   aim();
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    load_step(from_l, left, ahead_step, wave, stages + i * STAGE);
-    load_step(from_r, right, ahead_step, wave, stages + i * STAGE + BM * 64);
+    load(i);
     advance();
   }
   stage_barrier<0>();
   u32x4 al[MI], ar[NI], bl[MI], br[NI];
-  read_fragments<T, StageL, OrderL>(al, stages, wm * TM, lane);
-  read_fragments<T, StageR, OrderR>(ar, stages + BM * 64, wn * TN, lane);
+  read(0, al, ar);
   int slot = 0;  // the stage of the step that is multiplied
   for (; item < last; item += width) {
     int mt, nt;
@@ -400,17 +415,11 @@ __device__ inline void walk_tiles(const Grid &g, const L &left, const R &right, 
     for (int steps = min(g.split, g.steps - split * g.split); steps > 0; steps -= 2) {
       stage_barrier<2 * LOADS>();
       const int odd = (slot + 1) & 3, even = (slot + 2) & 3;
-      load_step(from_l, left, ahead_step, wave, stages + slot * STAGE);
-      load_step(from_r, right, ahead_step, wave, stages + slot * STAGE + BM * 64);
-      read_fragments<T, StageL, OrderL>(bl, stages + odd * STAGE, wm * TM, lane);
-      read_fragments<T, StageR, OrderR>(br, stages + odd * STAGE + BM * 64, wn * TN, lane);
+      read_or_load(odd, bl, br, slot);
       multiply(al, ar);
       advance();
       stage_barrier<2 * LOADS>();
-      load_step(from_l, left, ahead_step, wave, stages + odd * STAGE);
-      load_step(from_r, right, ahead_step, wave, stages + odd * STAGE + BM * 64);
-      read_fragments<T, StageL, OrderL>(al, stages + even * STAGE, wm * TM, lane);
-      read_fragments<T, StageR, OrderR>(ar, stages + even * STAGE + BM * 64, wn * TN, lane);
+      read_or_load(even, al, ar, odd);
       multiply(bl, br);
       advance();
       slot = even;
