@@ -145,7 +145,8 @@ lda_status lda_gated_backward(const lda_gated_args *a);
  * loss of a masked label is +inf.
  *
  * The backward pass takes dloss [rows] and the forward's lse, recomputes the
- * logits in pieces of the vocabulary and keeps one piece of
+ * logits in pieces of the vocabulary (as many words as take 256 MiB, but at
+ * least 1,024) and keeps one piece of
  *   G_iv = dloss_i * (exp(z_iv - lse_i) - [v = label_i])
  * (0 for rows left out and rows without words) in the workspace:
  *   dx = G weight, dweight = G^T x, dbias = sum over rows of G

@@ -59,7 +59,8 @@ lda_status check_cols(int64_t cols) {
   return LDA_OK;
 }
 
-// Of a product's result: the grid of its tiles has 32 bits of threads.
+// Of a product's result: its tiles (the smallest are 64 x 64, four times as many)
+// are counted in 32 bits.
 lda_status check_product(int64_t rows, int64_t cols) {
   REQUIRE(ceil_div(rows, 128) * ceil_div(cols, 128) <= LDA_OPS_MAX_TILES, LDA_E_RANGE,
           "a product has more than LDA_OPS_MAX_TILES tiles of 128 x 128");

@@ -13,7 +13,6 @@ namespace ops {
 
 inline int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline size_t elem_size(int dtype) { return dtype == LDA_F32 ? 4 : 2; }
 
 // Scratch of one call, cut from the caller's workspace in 256-byte steps.
 // With a null base it only counts: the *_workspace calls and the launches

@@ -315,7 +315,7 @@ __device__ inline void stage_barrier() {
 // What bounds it: a CU takes 64 bytes a cycle from its L2, so that at the
 // matrix unit's rate a 128 x 128 tile needs all of that and a 256 x 256 tile
 // half; 256 x 256 with one step in flight was bound by the loads' latency.  Now
-// (8192 x 1024 x 16384 of bf16, two splits, 229 to 237 us = 1,160 to 1,200
+// (8192 x 1024 x 16384 of bf16, two splits, 229 to 242 us = 1,140 to 1,200
 // TFLOP/s, where a library product of 8192^3 reaches 1,323) the matrix unit is
 // busy 59% of the cycles, at a clock of about 1.8 GHz (2.4 GHz at most).
 template <typename T, int BM, int BN, int WM, int WN, typename L, typename R, typename Epilogue>
@@ -599,7 +599,8 @@ __device__ inline void gate(int act, float a, float &p, float &dp) {
 }
 
 // h from the accumulators: a and b are never written.  8192 x 1024 x 4096 of
-// bf16: 149 us = 920 TFLOP/s of both projections, the activation included.
+// bf16: 149 to 157 us = 875 to 920 TFLOP/s of both projections, the activation
+// included.
 template <typename T>
 struct GatedForward {
   static constexpr bool kRuns = true;
@@ -635,7 +636,7 @@ struct GatedForward {
 // the backward products, from a and b recomputed.  Kept in 32 bits, as their
 // precision asks for, they would be written and read again (268 MB each way at
 // 8192 x 4096, about 110 us); recomputed, they cost 150 us of the backward
-// pass' 450, and a training step keeps x alone.  190 us with dh's reads and
+// pass' 500, and a training step keeps x alone.  192 us with dh's reads and
 // dab's stores.
 //
 // In half precision da and db go past the type's range, or below it, long before
@@ -715,7 +716,7 @@ __device__ inline int label_at(int label, int n0, int lane, int first, int vocab
 // tile's 256 words each, are joined by k_lse_join: 36 MB for 8,192 rows and
 // 141,000 words, where the logits would be 2.3 GB.
 //
-// 8192 x 1024 x 141000 of bf16: 2.1 to 2.2 ms = 1,080 to 1,120 TFLOP/s with
+// 8192 x 1024 x 141000 of bf16: 2.1 to 2.25 ms = 1,050 to 1,120 TFLOP/s with
 // this epilogue (a library product that writes the logits: 1,044).  A wave's
 // exponentials do not overlap with its own products.
 template <int BM, int WN>
@@ -783,8 +784,8 @@ struct SoftmaxPart {
 // small beside it.  S is 1, in half precision 2^14, so that probabilities down
 // to 2^-28 are normal numbers.
 //
-// A piece of 16,384 words at 8,192 rows of width 1,024: 301 to 313 us, where dx,
-// a product of the same size that stores little, takes 229 to 237: the rest is
+// A piece of 16,384 words at 8,192 rows of width 1,024: 301 to 317 us, where dx,
+// a product of the same size that stores little, takes 229 to 242: the rest is
 // the exponentials and G's 268 MB.
 template <typename T>
 constexpr float kGradLog2 = 0.0f;
@@ -1611,7 +1612,8 @@ hipError_t xent_forward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   return hipGetLastError();
 }
 
-// Words of one piece: G of a piece takes at most 256 MiB.
+// Words of one piece: as many as G takes 256 MiB for, but at least 1,024, so that
+// its products stay large (from 131,073 rows of 16 bits on G is larger for that).
 template <typename T>
 int piece_words(int64_t rows, int vocab) {
   const int64_t most = (int64_t(256) << 20) / (rows * int64_t(sizeof(T))) / 256 * 256;
