@@ -4,8 +4,10 @@
  * A word model predicts the words of a document from a vector of its topics:
  * layer norm, a gated layer, and a softmax over the whole vocabulary, whose
  * loss is the negative log-likelihood per token that lda_loglik reports for
- * the fitted counts (there in base 2).  Each operator has its forward and its
- * backward pass.
+ * the fitted counts (there in base 2).  A model that reads the words themselves
+ * in order embeds them and runs a gated recurrence over each document, and may
+ * learn from a teacher's most likely words.  Each operator has its forward and
+ * its backward pass.
  *
  * Conventions for every call:
  *   - All data pointers are device memory of the current device, owned by the
@@ -53,6 +55,12 @@ typedef enum { LDA_SILU = 0, LDA_GELU = 1, LDA_SIGMOID = 2 } lda_act;
 /* Most tiles of 128 x 128 of a product's result (logits, gated layer, weight
  * gradient): a call on more rows is made in parts. */
 #define LDA_OPS_MAX_TILES 8388608
+/* Most words that a teacher lists for a row, and most of all rows of a call
+ * (rows times top). */
+#define LDA_OPS_MAX_TOP 256
+#define LDA_OPS_MAX_LISTED 268435456
+/* Rows from one kept state of a recurrence to the next. */
+#define LDA_OPS_RECUR_ROWS 32
 
 /*
  * Layer norm of each row of x [rows][cols]:
@@ -184,6 +192,152 @@ lda_status lda_softmax_xent_workspace(const lda_xent_args *a, size_t *bytes);
 lda_status lda_softmax_xent(const lda_xent_args *a);
 lda_status lda_softmax_xent_backward_workspace(const lda_xent_args *a, size_t *bytes);
 lda_status lda_softmax_xent_backward(const lda_xent_args *a);
+
+/*
+ * Word embedding: words [rows], weight [vocab][width],
+ *   y_i = scale * weight[word_i]
+ * and 0 for a word outside [0, vocab).  The backward pass takes dy:
+ *   dweight_v = scale * sum of dy_i over the rows with word_i = v
+ * (0 for a word that no row has; rows outside the vocabulary have no part in
+ * it, whatever their dy holds).  The rows are sorted by word and a word's are
+ * summed in 32 bits in their order, in pieces of a fixed length.  scale must be
+ * finite.
+ */
+typedef struct {
+  int32_t dtype; /* of weight, y, dy, dweight */
+  int64_t rows;
+  int32_t width, vocab; /* >= 1 */
+  float scale;
+  const int32_t *words;
+  const void *weight; /* forward */
+  int64_t ld_weight;
+  void *y;
+  int64_t ldy;
+  const void *dy; /* backward */
+  int64_t lddy;
+  void *dweight; /* row stride width */
+  void *workspace; /* backward */
+  size_t workspace_bytes;
+  void *stream;
+} lda_embed_args;
+
+lda_status lda_embedding(const lda_embed_args *a);
+lda_status lda_embedding_backward_workspace(const lda_embed_args *a, size_t *bytes);
+lda_status lda_embedding_backward(const lda_embed_args *a);
+
+/*
+ * Gated linear recurrence over documents: x and gate [rows][cols]; document s
+ * has the rows offsets[s] .. offsets[s + 1] - 1, and begins with its row of
+ * state [docs][cols] (32 bits; NULL = 0):
+ *   f_t = sigmoid(gate_t), h_t = f_t h_{t-1} + (1 - f_t) x_t
+ *   last_s = h of its last row, of an empty document its state
+ * in each column by itself; h is rounded to the type of the matrices, the state
+ * that goes on is not.  Rows of no document are 0 in h and in the gradients,
+ * whatever x, gate and dh hold there, and no document's values, infinities and
+ * NaN included, reach another one.  offsets [docs + 1] are device memory and not
+ * checked: they must not decrease (values are unspecified if they do, no access
+ * is out of range) and what lies outside [0, rows] is cut off.  A call has at most
+ * LDA_OPS_MAX_TILES / 2 parts of 256 rows by 64 columns.
+ *
+ * kept [ceil(rows / LDA_OPS_RECUR_ROWS)][cols] are the states before every
+ * LDA_OPS_RECUR_ROWS-th row, for the backward pass.  It takes dh and dlast
+ * [docs][cols] (NULL = 0):
+ *   g_t = dh_t + f_{t+1} g_{t+1}; the last row's is dh + dlast
+ *   dx_t = (1 - f_t) g_t, dgate_t = g_t (h_{t-1} - x_t) f_t (1 - f_t)
+ *   dstate_s = f g of its first row, of an empty document dlast_s
+ * dstate is NULL if and only if state is.
+ *
+ * The step is one row more of each of `rows` documents: x, gate and h
+ * [rows][cols], state and last [rows][cols], which may be the same memory.  It
+ * has no offsets, kept and workspace; docs must be rows.
+ */
+typedef struct {
+  int32_t dtype; /* of x, gate, h, dh, dx, dgate */
+  int64_t rows;
+  int32_t cols; /* >= 1 */
+  int64_t docs; /* at most LDA_OPS_MAX_ROWS */
+  const int64_t *offsets;
+  const void *x;
+  int64_t ldx;
+  const void *gate;
+  int64_t ld_gate;
+  const float *state;
+  void *h; /* forward and step */
+  int64_t ldh;
+  float *last;
+  float *kept;    /* written by the forward, read by the backward pass */
+  const void *dh; /* backward */
+  int64_t lddh;
+  const float *dlast;
+  void *dx;
+  int64_t lddx;
+  void *dgate;
+  int64_t ld_dgate;
+  float *dstate;
+  void *workspace;
+  size_t workspace_bytes;
+  void *stream;
+} lda_recur_args;
+
+lda_status lda_recurrence_workspace(const lda_recur_args *a, size_t *bytes);
+lda_status lda_recurrence(const lda_recur_args *a);
+lda_status lda_recurrence_backward_workspace(const lda_recur_args *a, size_t *bytes);
+lda_status lda_recurrence_backward(const lda_recur_args *a);
+lda_status lda_recurrence_step(const lda_recur_args *a);
+
+/*
+ * Distillation over a vocabulary: how far the softmax over x weight^T + bias is
+ * from a teacher that lists up to `top` words and their scores (logits, or
+ * logarithms of probabilities) for each row, both softened by the temperature,
+ * without keeping the logits:
+ *   z = (x weight^T + bias) / temperature, lse_i = log sum_v exp z_iv
+ *   p_i = softmax of the row's scores / temperature over its listed words
+ *   loss_i = sum_j p_ij (log p_ij - (z[i][word_ij] - lse_i))
+ * words and scores are [rows][top]; a word outside [0, vocab) is an empty place,
+ * whatever its score.  A word listed twice counts with both places.  A row
+ * without listed words, or whose scores are all -inf, is left out: loss 0, no
+ * gradient, whatever its x holds.  A score of -inf has p = 0 and no part in the
+ * loss; a listed word with p > 0 that the bias masks (-inf) makes it +inf.
+ * logits [rows][top] are the z of the listed words (0 at empty places), kept for
+ * the backward pass:
+ *   G_iv = dloss_i / temperature * (exp(z_iv - lse_i) - p_iv)
+ *   dx = G weight, dweight = G^T x, dbias = sum over rows of G
+ * p_iv being the p of the row's places with word v.  As for the softmax cross
+ * entropy the logits are recomputed in pieces of the vocabulary, one piece of G
+ * is kept without dloss, and rows of weight must be finite.  dbias is NULL if
+ * and only if bias is.  temperature and its reciprocal must be finite and positive.
+ */
+typedef struct {
+  int32_t dtype;
+  int64_t rows;
+  int32_t width, vocab, top; /* >= 1 */
+  float temperature;
+  const void *x;
+  int64_t ldx;
+  const void *weight;
+  int64_t ld_weight;
+  const float *bias;
+  const int32_t *words;
+  int64_t ld_words;
+  const float *scores;
+  int64_t ld_scores;
+  float *loss;        /* forward */
+  float *lse;         /* written by the forward, read by the backward pass */
+  float *logits;      /* the same; row stride top */
+  const float *dloss; /* backward */
+  void *dx;
+  int64_t lddx;
+  void *dweight; /* row stride width */
+  float *dbias;
+  void *workspace;
+  size_t workspace_bytes;
+  void *stream;
+} lda_distill_args;
+
+lda_status lda_softmax_distill_workspace(const lda_distill_args *a, size_t *bytes);
+lda_status lda_softmax_distill(const lda_distill_args *a);
+lda_status lda_softmax_distill_backward_workspace(const lda_distill_args *a, size_t *bytes);
+lda_status lda_softmax_distill_backward(const lda_distill_args *a);
 
 #ifdef __cplusplus
 }

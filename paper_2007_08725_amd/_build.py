@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "liblda.so")
 SOURCES = ["kernels.hip", "layout_gpu.hip", "lda_api.cpp", "layout.cpp", "chunks.cpp", "readback.cpp", "ops_norm.hip",
-           "ops_product.hip", "ops_api.cpp"]
+           "ops_product.hip", "ops_embed.hip", "ops_recurrence.hip", "ops_api.cpp"]
 ARCH = "gfx950"
 
 

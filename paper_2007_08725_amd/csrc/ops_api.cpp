@@ -1,5 +1,6 @@
 // C ABI of the word-model operators (include/lda_ops.h): argument checks and
-// error reporting around the launchers of ops_norm.hip and ops_product.hip.
+// error reporting around the launchers of ops_norm.hip, ops_product.hip,
+// ops_embed.hip and ops_recurrence.hip.
 #include <cmath>
 #include <string>
 
@@ -124,6 +125,85 @@ lda_status check_xent(const lda_xent_args *a, bool backward) {
   return check_out(a->dx, a->lddx, a->rows, a->width, "dx is NULL");
 }
 
+lda_status check_vocab(int64_t vocab) {
+  REQUIRE(vocab >= 1, LDA_E_ARG, "vocab must be positive");
+  REQUIRE(vocab <= LDA_OPS_MAX_VOCAB, LDA_E_RANGE, "more words than LDA_OPS_MAX_VOCAB");
+  return LDA_OK;
+}
+
+lda_status check_embed(const lda_embed_args *a, bool backward) {
+  REQUIRE(a, LDA_E_ARG, "args is NULL");
+  LDA_TRY(check_rows(a->dtype, a->rows));
+  LDA_TRY(check_cols(a->width));
+  LDA_TRY(check_vocab(a->vocab));
+  REQUIRE(std::isfinite(a->scale), LDA_E_ARG, "scale must be finite");
+  REQUIRE(a->words || a->rows == 0, LDA_E_ARG, "words is NULL");
+  if (backward) {
+    REQUIRE(a->dweight, LDA_E_ARG, "dweight is NULL");
+    return check_in(a->dy, a->lddy, a->rows, "dy is NULL");
+  }
+  LDA_TRY(check_in(a->weight, a->ld_weight, a->rows, "weight is NULL"));
+  return check_out(a->y, a->ldy, a->rows, a->width, "y is NULL");
+}
+
+enum class Pass { kForward, kBackward, kStep };
+
+lda_status check_recur(const lda_recur_args *a, Pass pass) {
+  REQUIRE(a, LDA_E_ARG, "args is NULL");
+  LDA_TRY(check_rows(a->dtype, a->rows));
+  LDA_TRY(check_cols(a->cols));
+  REQUIRE(a->docs >= 0, LDA_E_ARG, "docs must not be negative");
+  REQUIRE(a->docs <= LDA_OPS_MAX_ROWS, LDA_E_RANGE, "more documents than LDA_OPS_MAX_ROWS");
+  REQUIRE(ceil_div(a->rows, 256) * ceil_div(a->cols, 64) <= LDA_OPS_MAX_TILES / 2, LDA_E_RANGE,
+          "a recurrence has more than LDA_OPS_MAX_TILES / 2 parts of 256 rows by 64 columns");
+  LDA_TRY(check_in(a->x, a->ldx, a->rows, "x is NULL"));
+  LDA_TRY(check_in(a->gate, a->ld_gate, a->rows, "gate is NULL"));
+  if (pass == Pass::kStep) {
+    REQUIRE(a->docs == a->rows, LDA_E_ARG, "a step takes one row of each document");
+    REQUIRE(a->state || a->rows == 0, LDA_E_ARG, "state is NULL");
+  } else {
+    REQUIRE(a->offsets, LDA_E_ARG, "offsets is NULL");
+    REQUIRE(a->kept || a->rows == 0, LDA_E_ARG, "kept is NULL");
+  }
+  if (pass != Pass::kBackward) {
+    REQUIRE(a->last || a->docs == 0, LDA_E_ARG, "last is NULL");
+    return check_out(a->h, a->ldh, a->rows, a->cols, "h is NULL");
+  }
+  LDA_TRY(check_in(a->dh, a->lddh, a->rows, "dh is NULL"));
+  REQUIRE((a->state == nullptr) == (a->dstate == nullptr), LDA_E_ARG, "dstate must be given if and only if state is");
+  LDA_TRY(check_out(a->dx, a->lddx, a->rows, a->cols, "dx is NULL"));
+  return check_out(a->dgate, a->ld_dgate, a->rows, a->cols, "dgate is NULL");
+}
+
+lda_status check_distill(const lda_distill_args *a, bool backward) {
+  REQUIRE(a, LDA_E_ARG, "args is NULL");
+  LDA_TRY(check_rows(a->dtype, a->rows));
+  LDA_TRY(check_cols(a->width));
+  LDA_TRY(check_vocab(a->vocab));
+  REQUIRE(a->top >= 1, LDA_E_ARG, "top must be positive");
+  REQUIRE(a->top <= LDA_OPS_MAX_TOP, LDA_E_RANGE, "more words a row than LDA_OPS_MAX_TOP");
+  REQUIRE(a->rows * a->top <= LDA_OPS_MAX_LISTED, LDA_E_RANGE, "more listed words than LDA_OPS_MAX_LISTED");
+  REQUIRE(std::isfinite(a->temperature) && a->temperature > 0.0f && std::isfinite(1.0f / a->temperature), LDA_E_ARG,
+          "temperature and its reciprocal must be finite and positive");
+  LDA_TRY(check_product(a->rows, a->vocab));
+  LDA_TRY(check_product(a->vocab, a->width));
+  LDA_TRY(check_product(a->rows, a->width));
+  LDA_TRY(check_in(a->x, a->ldx, a->rows, "x is NULL"));
+  LDA_TRY(check_in(a->weight, a->ld_weight, 1, "weight is NULL"));
+  LDA_TRY(check_in(a->words, a->ld_words, a->rows, "words is NULL"));
+  LDA_TRY(check_in(a->scores, a->ld_scores, a->rows, "scores is NULL"));
+  REQUIRE(a->lse || a->rows == 0, LDA_E_ARG, "lse is NULL");
+  REQUIRE(a->logits || a->rows == 0, LDA_E_ARG, "logits is NULL");
+  if (!backward) {
+    REQUIRE(a->loss || a->rows == 0, LDA_E_ARG, "loss is NULL");
+    return LDA_OK;
+  }
+  REQUIRE(a->dloss || a->rows == 0, LDA_E_ARG, "dloss is NULL");
+  REQUIRE(a->dweight, LDA_E_ARG, "dweight is NULL");
+  REQUIRE((a->bias == nullptr) == (a->dbias == nullptr), LDA_E_ARG, "dbias must be given if and only if bias is");
+  return check_out(a->dx, a->lddx, a->rows, a->width, "dx is NULL");
+}
+
 // Counts the workspace of `fn` for `a`, and with `bytes` NULL runs it in the
 // caller's.
 template <typename Args, typename Fn>
@@ -203,6 +283,71 @@ lda_status lda_softmax_xent_backward_workspace(const lda_xent_args *a, size_t *b
 lda_status lda_softmax_xent_backward(const lda_xent_args *a) {
   LDA_TRY(check_xent(a, true));
   return with_workspace(a, xent_backward, nullptr);
+}
+
+lda_status lda_embedding(const lda_embed_args *a) {
+  LDA_TRY(check_embed(a, false));
+  return launched(embed_forward(*a));
+}
+
+lda_status lda_embedding_backward_workspace(const lda_embed_args *a, size_t *bytes) {
+  REQUIRE(bytes, LDA_E_ARG, "bytes is NULL");
+  LDA_TRY(check_embed(a, true));
+  return with_workspace(a, embed_backward, bytes);
+}
+
+lda_status lda_embedding_backward(const lda_embed_args *a) {
+  LDA_TRY(check_embed(a, true));
+  return with_workspace(a, embed_backward, nullptr);
+}
+
+lda_status lda_recurrence_workspace(const lda_recur_args *a, size_t *bytes) {
+  REQUIRE(bytes, LDA_E_ARG, "bytes is NULL");
+  LDA_TRY(check_recur(a, Pass::kForward));
+  return with_workspace(a, recur_forward, bytes);
+}
+
+lda_status lda_recurrence(const lda_recur_args *a) {
+  LDA_TRY(check_recur(a, Pass::kForward));
+  return with_workspace(a, recur_forward, nullptr);
+}
+
+lda_status lda_recurrence_backward_workspace(const lda_recur_args *a, size_t *bytes) {
+  REQUIRE(bytes, LDA_E_ARG, "bytes is NULL");
+  LDA_TRY(check_recur(a, Pass::kBackward));
+  return with_workspace(a, recur_backward, bytes);
+}
+
+lda_status lda_recurrence_backward(const lda_recur_args *a) {
+  LDA_TRY(check_recur(a, Pass::kBackward));
+  return with_workspace(a, recur_backward, nullptr);
+}
+
+lda_status lda_recurrence_step(const lda_recur_args *a) {
+  LDA_TRY(check_recur(a, Pass::kStep));
+  return launched(recur_step(*a));
+}
+
+lda_status lda_softmax_distill_workspace(const lda_distill_args *a, size_t *bytes) {
+  REQUIRE(bytes, LDA_E_ARG, "bytes is NULL");
+  LDA_TRY(check_distill(a, false));
+  return with_workspace(a, distill_forward, bytes);
+}
+
+lda_status lda_softmax_distill(const lda_distill_args *a) {
+  LDA_TRY(check_distill(a, false));
+  return with_workspace(a, distill_forward, nullptr);
+}
+
+lda_status lda_softmax_distill_backward_workspace(const lda_distill_args *a, size_t *bytes) {
+  REQUIRE(bytes, LDA_E_ARG, "bytes is NULL");
+  LDA_TRY(check_distill(a, true));
+  return with_workspace(a, distill_backward, bytes);
+}
+
+lda_status lda_softmax_distill_backward(const lda_distill_args *a) {
+  LDA_TRY(check_distill(a, true));
+  return with_workspace(a, distill_backward, nullptr);
 }
 
 }  // extern "C"

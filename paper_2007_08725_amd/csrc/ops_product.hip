@@ -1,5 +1,5 @@
 // Matrix products of the word-model operators (include/lda_ops.h): the gated
-// layer and the softmax cross entropy, forward and backward.
+// layer, the softmax cross entropy and distillation, forward and backward.
 //
 // Every product is C[m][n] = sum_k L[m][k] R[n][k] on the matrix units, either
 // operand as it lies in memory or transposed; what is done with C (activation,
@@ -719,7 +719,10 @@ __device__ inline int label_at(int label, int n0, int lane, int first, int vocab
 // 8192 x 1024 x 141000 of bf16: 2.1 to 2.25 ms = 1,050 to 1,120 TFLOP/s with
 // this epilogue (a library product that writes the logits: 1,044).  A wave's
 // exponentials do not overlap with its own products.
-template <int BM, int WN>
+//
+// With a Teacher the logits are multiplied by `unit` (1 / temperature) and there
+// is no label.
+template <int BM, int WN, bool Teacher = false>
 struct SoftmaxPart {
   static constexpr bool kRuns = false;
   const float *bias;
@@ -727,6 +730,7 @@ struct SoftmaxPart {
   float *label_logit;  // [rows]
   float2 *part;        // [ntiles][rows]
   int rows, vocab;
+  float unit;
   template <int MI, int NI>
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
     float2 *shared = reinterpret_cast<float2 *>(at.lds);  // [WN][BM]
@@ -737,15 +741,20 @@ struct SoftmaxPart {
       one_row_at_a_time();
       f32x4 z[NI];
 #pragma unroll
-      for (int j = 0; j < NI; ++j) z[j] = c[i][j] + b[j];
-      const int m = at.m0 + i * 16 + (at.lane & 15);
-      const int hit = label_at<kRuns, NI>(m < rows ? labels[m] : -1, at.n0, at.lane, 0, vocab);
-      if (__ballot(hit >= 0)) {
+      for (int j = 0; j < NI; ++j) {
+        z[j] = c[i][j] + b[j];
+        if constexpr (Teacher) z[j] *= unit;
+      }
+      if constexpr (!Teacher) {
+        const int m = at.m0 + i * 16 + (at.lane & 15);
+        const int hit = label_at<kRuns, NI>(m < rows ? labels[m] : -1, at.n0, at.lane, 0, vocab);
+        if (__ballot(hit >= 0)) {
 #pragma unroll
-        for (int j = 0; j < NI; ++j)
+          for (int j = 0; j < NI; ++j)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (hit == j * 4 + r) label_logit[m] = z[j][r];
+            for (int r = 0; r < 4; ++r)
+              if (hit == j * 4 + r) label_logit[m] = z[j][r];
+        }
       }
       float top = -INFINITY;
 #pragma unroll
@@ -796,7 +805,11 @@ constexpr float kGradUnit = 1.0f;
 template <>
 constexpr float kGradUnit<f16> = 16384.0f;
 
-template <typename T, int BN, int WM>
+//
+// With a Teacher the logits are multiplied by `unit`, `labels` says only which
+// rows are kept (0) or left out (-1), and G lacks what the teacher gives its
+// words, which k_teacher_words puts right.
+template <typename T, int BN, int WM, bool Teacher = false>
 struct SoftmaxGrad {
   static constexpr bool kRuns = true;
   const float *bias;
@@ -806,6 +819,7 @@ struct SoftmaxGrad {
   int64_t ldg;
   float *col_part;  // [mtiles][piece], NULL without a bias
   int rows, vocab, first, piece;
+  float unit;
   template <int MI, int NI>
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
     f32x4 b[NI], sums[NI];
@@ -823,15 +837,20 @@ struct SoftmaxGrad {
 #pragma unroll
       for (int j = 0; j < NI; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          z[j][r] = kept ? __builtin_amdgcn_exp2f((c[i][j][r] + b[j][r] - l) * kLog2e + kGradLog2<T>) : 0.0f;
-      const int hit = kept ? label_at<kRuns, NI>(label, at.n0, at.lane, first, vocab) : -1;
-      if (__ballot(hit >= 0)) {
+        for (int r = 0; r < 4; ++r) {
+          float logit = c[i][j][r] + b[j][r];
+          if constexpr (Teacher) logit *= unit;
+          z[j][r] = kept ? __builtin_amdgcn_exp2f((logit - l) * kLog2e + kGradLog2<T>) : 0.0f;
+        }
+      if constexpr (!Teacher) {
+        const int hit = kept ? label_at<kRuns, NI>(label, at.n0, at.lane, first, vocab) : -1;
+        if (__ballot(hit >= 0)) {
 #pragma unroll
-        for (int j = 0; j < NI; ++j)
+          for (int j = 0; j < NI; ++j)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (hit == j * 4 + r) z[j][r] -= kGradUnit<T>;
+            for (int r = 0; r < 4; ++r)
+              if (hit == j * 4 + r) z[j][r] -= kGradUnit<T>;
+        }
       }
 #pragma unroll
       for (int j = 0; j < NI; ++j) sums[j] += z[j] * d;
@@ -938,15 +957,16 @@ __global__ __launch_bounds__(256) void k_gated_few(const T *x, int64_t ldx, cons
 }
 
 // Each wave takes every (4 gridDim.x)-th 16 words and keeps its lanes' softmax
-// so far; part [rows][gridDim.x].
-template <typename T, bool Aligned>
+// so far; part [rows][gridDim.x].  With a Teacher as SoftmaxPart.
+template <typename T, bool Aligned, bool Teacher>
 __global__ __launch_bounds__(256) void k_xent_few(const T *x, int64_t ldx, const T *weight, int64_t ldw,
                                                   const float *bias, const int32_t *labels, int rows, int width,
-                                                  int vocab, float *label_logit, float2 *part) {
+                                                  int vocab, float unit, float *label_logit, float2 *part) {
   __shared__ float2 shared[4][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15;
   const T *row = x + min(q, rows - 1) * ldx;
-  const int label = q < rows ? labels[q] : -1;
+  int label = -1;
+  if constexpr (!Teacher) label = q < rows ? labels[q] : -1;
   float2 so_far = make_float2(-INFINITY, 0.0f);
   for (int n0 = (int(blockIdx.x) * 4 + wave) * 16; n0 < vocab; n0 += int(gridDim.x) * 64) {
     const T *const w[1] = {weight + int64_t(min(n0 + q, vocab - 1)) * ldw};
@@ -957,7 +977,8 @@ __global__ __launch_bounds__(256) void k_xent_few(const T *x, int64_t ldx, const
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       c[0][r] = v + r < vocab ? (bias ? c[0][r] + bias[v + r] : c[0][r]) : -INFINITY;
-      if (v + r == label && label < vocab) label_logit[q] = c[0][r];
+      if constexpr (Teacher) c[0][r] *= unit;
+      else if (v + r == label && label < vocab) label_logit[q] = c[0][r];
       top = fmaxf(top, c[0][r]);
     }
     const float ref = top == -INFINITY ? 0.0f : top;
@@ -977,11 +998,13 @@ __global__ __launch_bounds__(256) void k_xent_few(const T *x, int64_t ldx, const
 }
 
 // ---------------------------------------------------------- small kernels ---
-// The loss of a row from its softmax (largest logit, sum).
+// The loss of a row from its softmax (largest logit, sum); without labels only
+// the logarithm.
 __device__ inline void write_loss(float2 a, int m, const float *label_logit, const int32_t *labels, int vocab,
                                   float *loss, float *lse) {
   const float total = a.x == -INFINITY && a.y == 0.0f ? -INFINITY : a.x + kLn2 * __builtin_amdgcn_logf(a.y);
   lse[m] = total;
+  if (!labels) return;
   const int label = labels[m];
   float out = 0.0f;
   if (label >= 0 && label < vocab) {
@@ -1090,9 +1113,10 @@ __global__ __launch_bounds__(1024) void k_grad_factors(const float *dloss, const
   }
 }
 
-// out[n] = sum over t of part[t][n]: 64 columns a workgroup, a wave for every
-// fourth part.
-__global__ __launch_bounds__(256) void k_sum_parts(const float *part, int count, int n_all, float *out) {
+// out[n] = sum over t of part[t][n], less what `less` has there (NULL = 0): 64
+// columns a workgroup, a wave for every fourth part.
+__global__ __launch_bounds__(256) void k_sum_parts(const float *part, int count, int n_all, const float *less,
+                                                   float *out) {
   __shared__ float shared[4][64];
   const int n = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
   float s = 0.0f;
@@ -1102,7 +1126,10 @@ __global__ __launch_bounds__(256) void k_sum_parts(const float *part, int count,
   }
   shared[wave][threadIdx.x & 63] = s;
   __syncthreads();
-  if (wave == 0 && n < n_all) out[n] = s + shared[1][threadIdx.x] + shared[2][threadIdx.x] + shared[3][threadIdx.x];
+  if (wave == 0 && n < n_all) {
+    s = s + shared[1][threadIdx.x] + shared[2][threadIdx.x] + shared[3][threadIdx.x];
+    out[n] = less ? s - less[n] : s;
+  }
 }
 
 // Joins the splits of a product.
@@ -1269,16 +1296,174 @@ __global__ __launch_bounds__(1024) void k_gated_units(const float *tops, int row
   gated_units(group_max(threadIdx.x < gridDim.x ? tops[threadIdx.x] : 0.0f, shared), rows, x_factor, out);
 }
 
+// --------------------------------------------------------------- teacher ----
+// The words that a teacher lists for a row, kPlaces to a lane (place lane + 64 i),
+// and its softmax over them: p, its logarithm, and whether the row is kept.  A
+// word of -1 is an empty place.
+constexpr int kPlaces = LDA_OPS_MAX_TOP / 64;
+struct Listed {
+  int word[kPlaces];
+  float p[kPlaces], log_p[kPlaces];
+  bool kept;
+};
+
+__device__ inline Listed teacher_row(const int32_t *words, const float *scores, int top, int vocab, float unit,
+                                     int lane) {
+  Listed t;
+  float score[kPlaces], high = -INFINITY, sum = 0.0f;
+  bool some = false;
+#pragma unroll
+  for (int i = 0; i < kPlaces; ++i) {
+    const int j = lane + 64 * i;
+    t.word[i] = -1;
+    score[i] = -INFINITY;
+    if (j < top) {
+      const int word = words[j];
+      if (word >= 0 && word < vocab) {
+        t.word[i] = word;
+        score[i] = scores[j] * unit;
+      }
+    }
+    some |= score[i] != -INFINITY;  // NaN is no reason to leave a row out
+    high = fmaxf(high, score[i]);
+  }
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) high = fmaxf(high, __shfl_xor(high, x));
+  if (high == -INFINITY) high = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kPlaces; ++i) {
+    t.log_p[i] = score[i] - high;
+    t.p[i] = __builtin_amdgcn_exp2f(t.log_p[i] * kLog2e);
+    sum += t.p[i];
+  }
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+  t.kept = __ballot(some);
+  const float log_sum = kLn2 * __builtin_amdgcn_logf(sum), part = 1.0f / sum;
+#pragma unroll
+  for (int i = 0; i < kPlaces; ++i) {
+    t.log_p[i] -= log_sum;
+    t.p[i] = t.kept ? t.p[i] * part : 0.0f;
+  }
+  return t;
+}
+
+// The logits of a row's listed words and its loss: a workgroup a row, four words
+// of a wave at a time.  Reads a row of the weights for each place: 8192 x 32 of
+// 1024 bf16, 537 MB that mostly lie in the caches.
+template <typename T, bool Aligned>
+__global__ __launch_bounds__(256) void k_distill_loss(const T *x, int64_t ldx, const T *weight, int64_t ldw,
+                                                      const float *bias, const int32_t *words, int64_t ld_words,
+                                                      const float *scores, int64_t ld_scores, int width, int vocab,
+                                                      int top, float unit, const float *lse, float *logits,
+                                                      float *loss) {
+  constexpr int U = 4;
+  typedef T vec __attribute__((ext_vector_type(kChunk<T>)));
+  __shared__ float z[LDA_OPS_MAX_TOP];
+  const int64_t m = blockIdx.x;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int32_t *list = words + m * ld_words;
+  const T *row = x + m * ldx;
+  for (int j0 = wave * U; j0 < top; j0 += 4 * U) {
+    const T *w[U];
+    float sum[U];
+    int word[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      word[u] = j0 + u < top ? list[j0 + u] : -1;
+      if (word[u] >= vocab) word[u] = -1;
+      w[u] = weight + int64_t(word[u] < 0 ? 0 : word[u]) * ldw;
+      sum[u] = 0.0f;
+    }
+    for (int c = lane; c * kChunk<T> < width; c += 64) {
+      const vec xv = __builtin_bit_cast(vec, row_chunk<T, Aligned>(row, c, width));
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const vec wv = __builtin_bit_cast(vec, row_chunk<T, Aligned>(w[u], c, width));
+#pragma unroll
+        for (int e = 0; e < kChunk<T>; ++e) sum[u] += float(xv[e]) * float(wv[e]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int x_ = 1; x_ < 64; x_ <<= 1) sum[u] += __shfl_xor(sum[u], x_);
+      if (lane == 0 && j0 + u < top) z[j0 + u] = word[u] < 0 ? 0.0f : (bias ? sum[u] + bias[word[u]] : sum[u]) * unit;
+    }
+  }
+  __syncthreads();
+  for (int j = threadIdx.x; j < top; j += 256) logits[m * top + j] = z[j];
+  if (wave) return;
+  const Listed t = teacher_row(list, scores + m * ld_scores, top, vocab, unit, lane);
+  const float l = lse[m];
+  float sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kPlaces; ++i) {
+    if (t.word[i] < 0 || t.p[i] == 0.0f) continue;
+    const float zj = z[lane + 64 * i];
+    sum += zj == -INFINITY ? INFINITY : t.p[i] * (t.log_p[i] - (zj - l));
+  }
+#pragma unroll
+  for (int x_ = 1; x_ < 64; x_ <<= 1) sum += __shfl_xor(sum, x_);
+  if (lane == 0) loss[m] = t.kept ? sum : 0.0f;
+}
+
+// What the backward pass takes of the teacher: whether a row is kept (labels 0 or
+// -1), its gradient over the temperature, and for the first place of each of its
+// words what G has there, S (exp(z - lse) - p), and p times the row's gradient,
+// which dbias lacks; other places have the word -1.  A wave a row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_teacher(const int32_t *words, int64_t ld_words, const float *scores,
+                                                 int64_t ld_scores, const float *logits, const float *lse,
+                                                 const float *dloss, int rows, int vocab, int top, float unit,
+                                                 int32_t *labels, float *row_loss, int32_t *its_word, T *its_grad,
+                                                 float *its_share) {
+  __shared__ float p[4][LDA_OPS_MAX_TOP];
+  __shared__ int word[4][LDA_OPS_MAX_TOP];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = int(blockIdx.x) * 4 + wave;
+  if (m < rows) {
+    const Listed t = teacher_row(words + m * ld_words, scores + m * ld_scores, top, vocab, unit, lane);
+    const float l = lse[m], d = t.kept ? dloss[m] * unit : 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPlaces; ++i) {
+      p[wave][lane + 64 * i] = t.p[i];
+      word[wave][lane + 64 * i] = t.kept && l != -INFINITY ? t.word[i] : -1;
+    }
+    if (lane == 0) {
+      labels[m] = t.kept ? 0 : -1;
+      row_loss[m] = d;
+    }
+  }
+  __syncthreads();
+  if (m >= rows) return;
+  const float l = lse[m], d = row_loss[m];
+  for (int j = lane; j < top; j += 64) {
+    int mine = word[wave][j];
+    float all = 0.0f;
+    for (int i = 0; i < top; ++i) {
+      if (word[wave][i] != mine) continue;
+      all += p[wave][i];
+      if (i < j) mine = -1;
+    }
+    const int64_t at = int64_t(m) * top + j;
+    its_word[at] = mine;
+    if (mine < 0) continue;
+    its_grad[at] = T((__builtin_amdgcn_exp2f((logits[at] - l) * kLog2e) - all) * kGradUnit<T>);
+    if (its_share) its_share[at] = all * d;
+  }
+}
+
+// A piece of G where the teacher has words.
+template <typename T>
+__global__ __launch_bounds__(256) void k_teacher_words(const int32_t *its_word, const T *its_grad, int64_t count,
+                                                       int top, int first, int piece, T *grad, int64_t ldg) {
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < count; i += int64_t(gridDim.x) * 256) {
+    const int at = its_word[i] - first;
+    if (its_word[i] >= 0 && at >= 0 && at < piece) grad[int64_t(uint32_t(i) / uint32_t(top)) * ldg + at] = its_grad[i];
+  }
+}
+
 // ------------------------------------------------------------------- host ---
-// Workgroups of a kernel that strides over its elements.
-unsigned strided(int64_t workgroups) { return unsigned(workgroups < 65536 ? workgroups : 65536); }
-
-#define OPS_TRY(expr)                      \
-  do {                                     \
-    hipError_t e_ = (expr);                \
-    if (e_ != hipSuccess) return e_;       \
-  } while (0)
-
 // How many elements of a row can be moved at once: 8, 4 or 1.
 template <typename T>
 int at_once(const void *p, int64_t ld) {
@@ -1574,8 +1759,9 @@ hipError_t gated_backward_t(const lda_gated_args &a, Arena &ws, bool dry) {
                          Columns<T>{x_scaled.p, x_scaled.ld, a.width, rows}, dw, ws, dry, s);
 }
 
-template <typename T>
-hipError_t xent_forward_t(const lda_xent_args &a, Arena &ws, bool dry) {
+// With a Teacher only lse, of logits times `unit`.
+template <typename T, bool Teacher>
+hipError_t softmax_forward(const lda_xent_args &a, float unit, Arena &ws, bool dry) {
   if (a.rows == 0) return hipSuccess;
   const hipStream_t s = static_cast<hipStream_t>(a.stream);
   const int rows = int(a.rows), k = int(round_up(a.width, kChunk<T>));
@@ -1585,10 +1771,12 @@ hipError_t xent_forward_t(const lda_xent_args &a, Arena &ws, bool dry) {
     float2 *part = ws.take<float2>(int64_t(rows) * parts);
     float *label_logit = ws.take<float>(rows);
     if (dry) return hipSuccess;
-    auto kernel = in_place<T>(a.x, a.ldx, a.width) && in_place<T>(a.weight, a.ld_weight, a.width) ? k_xent_few<T, true>
-                                                                                                  : k_xent_few<T, false>;
+    auto kernel = in_place<T>(a.x, a.ldx, a.width) && in_place<T>(a.weight, a.ld_weight, a.width)
+                      ? k_xent_few<T, true, Teacher>
+                      : k_xent_few<T, false, Teacher>;
     kernel<<<unsigned(parts), 256, 0, s>>>(static_cast<const T *>(a.x), a.ldx, static_cast<const T *>(a.weight),
-                                           a.ld_weight, a.bias, a.labels, rows, a.width, a.vocab, label_logit, part);
+                                           a.ld_weight, a.bias, a.labels, rows, a.width, a.vocab, unit, label_logit,
+                                           part);
     OPS_TRY(hipGetLastError());
     k_lse_join_few<<<unsigned(rows), 256, 0, s>>>(part, parts, label_logit, a.labels, a.vocab, a.loss, a.lse);
     return hipGetLastError();
@@ -1604,12 +1792,17 @@ hipError_t xent_forward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   OPS_TRY(packs.run(s));
   OPS_TRY(with_shape<T>(tiles, [&](auto shape) {
     typedef decltype(shape) S;
-    const SoftmaxPart<S::BM, S::WN> epi{a.bias, a.labels, label_logit, part, rows, a.vocab};
+    const SoftmaxPart<S::BM, S::WN, Teacher> epi{a.bias, a.labels, label_logit, part, rows, a.vocab, unit};
     return product<T, S>(a.rows, a.vocab, k, 1, Rows<T>{x.p, x.ld, rows, k}, Rows<T>{w.p, w.ld, a.vocab, k}, epi, s);
   }));
   k_lse_join<<<unsigned(ceil_div(rows, 16)), 256, 0, s>>>(part, ntiles, label_logit, a.labels, rows, a.vocab, a.loss,
                                                           a.lse);
   return hipGetLastError();
+}
+
+template <typename T>
+hipError_t xent_forward_t(const lda_xent_args &a, Arena &ws, bool dry) {
+  return softmax_forward<T, false>(a, 1.0f, ws, dry);
 }
 
 // Words of one piece: as many as G takes 256 MiB for, but at least 1,024, so that
@@ -1621,8 +1814,18 @@ int piece_words(int64_t rows, int vocab) {
   return int(most < 1024 ? (all < 1024 ? all : 1024) : most < all ? most : all);
 }
 
+// What the backward pass of distillation has beside the cross entropy's.
 template <typename T>
-hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
+struct Teaching {
+  float unit;
+  int top;
+  const int32_t *its_word;
+  const T *its_grad;
+  const float *less;  // dbias lacks this; NULL without a bias
+};
+
+template <typename T, bool Teacher>
+hipError_t softmax_backward(const lda_xent_args &a, const Teaching<T> &teaching, Arena &ws, bool dry) {
   const hipStream_t s = static_cast<hipStream_t>(a.stream);
   T *dw = static_cast<T *>(a.dweight);
   if (a.rows == 0) {
@@ -1664,12 +1867,20 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
     if (!dry) {
       OPS_TRY(with_shape<T>(tiles_of<T>(a.rows, piece), [&](auto shape) {
         typedef decltype(shape) S;
-        const SoftmaxGrad<T, S::BN, S::WM> epi{a.bias, a.labels, a.lse, row_factor, grad, words_k, col_part, rows,
-                                               a.vocab, first, words};
+        const SoftmaxGrad<T, S::BN, S::WM, Teacher> epi{a.bias,   a.labels, a.lse, row_factor, grad,  words_k,
+                                                        col_part, rows,     a.vocab, first,    words, teaching.unit};
         return product<T, S>(a.rows, words_k, k, 1, Rows<T>{x.p, x.ld, rows, k}, Rows<T>{wp, w.ld, words, k}, epi, s);
       }));
       if (a.dbias) {
-        k_sum_parts<<<unsigned(ceil_div(words, 64)), 256, 0, s>>>(col_part, mtiles, words, a.dbias + first);
+        k_sum_parts<<<unsigned(ceil_div(words, 64)), 256, 0, s>>>(col_part, mtiles, words,
+                                                                        Teacher ? teaching.less + first : nullptr,
+                                                                        a.dbias + first);
+        OPS_TRY(hipGetLastError());
+      }
+      if constexpr (Teacher) {
+        const int64_t listed = a.rows * teaching.top;
+        k_teacher_words<T><<<strided(ceil_div(listed, 256)), 256, 0, s>>>(
+            teaching.its_word, teaching.its_grad, listed, teaching.top, first, words, grad, words_k);
         OPS_TRY(hipGetLastError());
       }
       OPS_TRY(with_shape<T>(dx_tiles, [&](auto shape) {
@@ -1695,6 +1906,69 @@ hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
   return hipGetLastError();
 }
 
+template <typename T>
+hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
+  return softmax_backward<T, false>(a, Teaching<T>{1.0f, 0, nullptr, nullptr, nullptr}, ws, dry);
+}
+
+// The softmax over the student's logits, as the cross entropy has it.
+lda_xent_args student(const lda_distill_args &a) {
+  lda_xent_args x = {};
+  x.dtype = a.dtype;
+  x.rows = a.rows;
+  x.width = a.width;
+  x.vocab = a.vocab;
+  x.x = a.x;
+  x.ldx = a.ldx;
+  x.weight = a.weight;
+  x.ld_weight = a.ld_weight;
+  x.bias = a.bias;
+  x.lse = a.lse;
+  x.dx = a.dx;
+  x.lddx = a.lddx;
+  x.dweight = a.dweight;
+  x.dbias = a.dbias;
+  x.stream = a.stream;
+  return x;
+}
+
+template <typename T>
+hipError_t distill_forward_t(const lda_distill_args &a, Arena &ws, bool dry) {
+  const float unit = 1.0f / a.temperature;
+  OPS_TRY((softmax_forward<T, true>(student(a), unit, ws, dry)));
+  if (dry || a.rows == 0) return hipSuccess;
+  auto kernel = in_place<T>(a.x, a.ldx, a.width) && in_place<T>(a.weight, a.ld_weight, a.width)
+                    ? k_distill_loss<T, true>
+                    : k_distill_loss<T, false>;
+  kernel<<<unsigned(a.rows), 256, 0, static_cast<hipStream_t>(a.stream)>>>(
+      static_cast<const T *>(a.x), a.ldx, static_cast<const T *>(a.weight), a.ld_weight, a.bias, a.words, a.ld_words,
+      a.scores, a.ld_scores, a.width, a.vocab, a.top, unit, a.lse, a.logits, a.loss);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t distill_backward_t(const lda_distill_args &a, Arena &ws, bool dry) {
+  const hipStream_t s = static_cast<hipStream_t>(a.stream);
+  const float unit = 1.0f / a.temperature;
+  const int64_t listed = a.rows * a.top;
+  lda_xent_args x = student(a);
+  int32_t *labels = ws.take<int32_t>(a.rows), *its_word = ws.take<int32_t>(listed);
+  float *row_loss = ws.take<float>(a.rows);
+  T *its_grad = ws.take<T>(listed);
+  float *its_share = a.bias ? ws.take<float>(listed) : nullptr, *less = a.bias ? ws.take<float>(a.vocab) : nullptr;
+  if (!dry && a.rows) {
+    k_teacher<T><<<unsigned(ceil_div(a.rows, 4)), 256, 0, s>>>(a.words, a.ld_words, a.scores, a.ld_scores, a.logits,
+                                                               a.lse, a.dloss, int(a.rows), a.vocab, a.top, unit,
+                                                               labels, row_loss, its_word, its_grad, its_share);
+    OPS_TRY(hipGetLastError());
+  }
+  if (a.bias && a.rows)
+    OPS_TRY(sum_by_word<float>(its_word, listed, its_share, 1, 1, a.vocab, 1.0f, less, ws, dry, s));
+  x.labels = labels;
+  x.dloss = row_loss;
+  return softmax_backward<T, true>(x, Teaching<T>{unit, a.top, its_word, its_grad, less}, ws, dry);
+}
+
 }  // namespace
 
 #define BY_TYPE(fn, ...)                              \
@@ -1708,6 +1982,8 @@ hipError_t gated_forward(const lda_gated_args &a, Arena &ws, bool dry) { BY_TYPE
 hipError_t gated_backward(const lda_gated_args &a, Arena &ws, bool dry) { BY_TYPE(gated_backward_t, a, ws, dry) }
 hipError_t xent_forward(const lda_xent_args &a, Arena &ws, bool dry) { BY_TYPE(xent_forward_t, a, ws, dry) }
 hipError_t xent_backward(const lda_xent_args &a, Arena &ws, bool dry) { BY_TYPE(xent_backward_t, a, ws, dry) }
+hipError_t distill_forward(const lda_distill_args &a, Arena &ws, bool dry) { BY_TYPE(distill_forward_t, a, ws, dry) }
+hipError_t distill_backward(const lda_distill_args &a, Arena &ws, bool dry) { BY_TYPE(distill_backward_t, a, ws, dry) }
 
 }  // namespace ops
 }  // namespace lda
