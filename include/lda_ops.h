@@ -60,7 +60,7 @@ typedef enum { LDA_SILU = 0, LDA_GELU = 1, LDA_SIGMOID = 2 } lda_act;
 #define LDA_OPS_MAX_TOP 256
 #define LDA_OPS_MAX_LISTED 268435456
 /* Rows from one kept state of a recurrence to the next. */
-#define LDA_OPS_RECUR_ROWS 32
+#define LDA_OPS_RECUR_ROWS 16
 
 /*
  * Layer norm of each row of x [rows][cols]:
@@ -302,10 +302,13 @@ lda_status lda_recurrence_step(const lda_recur_args *a);
  * the backward pass:
  *   G_iv = dloss_i / temperature * (exp(z_iv - lse_i) - p_iv)
  *   dx = G weight, dweight = G^T x, dbias = sum over rows of G
- * p_iv being the p of the row's places with word v.  As for the softmax cross
- * entropy the logits are recomputed in pieces of the vocabulary, one piece of G
- * is kept without dloss, and rows of weight must be finite.  dbias is NULL if
- * and only if bias is.  temperature and its reciprocal must be finite and positive.
+ * p_iv being the p of the row's places with word v (0 for rows left out and rows
+ * without words).  As for the softmax cross entropy the logits are recomputed in
+ * pieces of the vocabulary, one piece of G is kept, without the power of two in
+ * dloss / temperature and in 16-bit types rounded to them, and rows of weight must
+ * be finite; in half precision a row's part of dweight loses bits as there.  dbias
+ * is NULL if and only if bias is.  temperature and its reciprocal must be finite
+ * and positive.
  */
 typedef struct {
   int32_t dtype;

@@ -1,7 +1,7 @@
 // Gated linear recurrence over documents (include/lda_ops.h): forward, backward
 // and single steps.
 //
-// h_t = f_t h_{t-1} + b_t is a chain in each column.  A wave holds kRows rows of
+// h_t = f_t h_{t-1} + b_t is a chain in each column.  A wave holds some rows of
 // its columns in registers and reduces them to one map, state in -> state out,
 // m -> A m + B; a workgroup joins its waves' maps in LDS, and workgroups, which
 // start in the order of the rows, pass the state on through memory: each leaves
@@ -15,6 +15,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "ops_internal.h"
 
 #pragma clang fp contract(fast)
@@ -26,28 +28,40 @@ namespace {
 typedef __bf16 bf16;
 typedef _Float16 f16;
 
-constexpr int kRows = LDA_OPS_RECUR_ROWS;  // of a wave
+constexpr int kKept = LDA_OPS_RECUR_ROWS;  // rows from one kept state to the next
 constexpr int kWaves = 8;
-constexpr int kBlock = kRows * kWaves;  // rows of a workgroup
-constexpr int kAhead = 4;               // maps that a wave looks back to at a time
-constexpr int kWindow = kAhead * kWaves;
+// Rows of a wave, which has N columns a lane: what lies in registers is the same.
+// The backward pass has three matrices.
+template <typename T, int N, bool Back>
+constexpr int kRows = Back && sizeof(T) == 4 ? 16 : 32 / N;
+constexpr int kWindow = 32;                // workgroups that are looked back to at a time
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// f = sigmoid(g) and k = 1 - f from e = exp(-g), each to a few roundings of
-// itself: e stays below 2^120, so that e f is finite.
+// The gate f = sigmoid(g) and k = 1 - f, kept as one number: the smaller of the
+// two, from e = exp(-|g|) to a few roundings of itself, negative where it is f.
+// The larger is 1 minus it, which no approximation of the reciprocal biases: a
+// gate near 1 is multiplied by itself thousands of times.
 template <typename T>
-__device__ inline void gate(float g, float &f, float &k) {
-  float t = -kLog2e * g;
-  t = t > 120.0f ? 120.0f : t;
+__device__ inline float gate_of(float g) {
+  const float a = fabsf(g), t = -kLog2e * a;
   float e = __builtin_amdgcn_exp2f(t);
   if constexpr (sizeof(T) == 4) {
     // what the product with log2 e was rounded by
-    const float low = __builtin_fmaf(-kLog2e, g, -t) - 1.9259629911266175e-8f * g;
-    if (fabsf(t) < 120.0f) e = __builtin_fmaf(e, 0.6931471805599453f * low, e);
+    const float low = __builtin_fmaf(-kLog2e, a, -t) - 1.9259629911266175e-8f * a;
+    if (a < 100.0f) e = __builtin_fmaf(e, 0.6931471805599453f * low, e);
   }
-  f = __builtin_amdgcn_rcpf(1.0f + e);
-  k = e * f;
+  return copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), g);
+}
+__device__ inline void open(float kept, float &f, float &k) {
+  const float small = fabsf(kept), large = 1.0f - small;
+  const bool low = __builtin_signbitf(kept);
+  f = low ? small : large;
+  k = low ? large : small;
+}
+template <typename T>
+__device__ inline void gate(float g, float &f, float &k) {
+  open(gate_of<T>(g), f, k);
 }
 
 // N columns of a lane, side by side; N > 1 are moved as 32 bits.
@@ -77,14 +91,38 @@ __device__ inline void store_raw(T *p, const float (&x)[N]) {
   *reinterpret_cast<Raw<T, N> *>(p) = r;
 }
 
+// Values that the compiler takes for others here: it then computes what is made
+// of them where it is used, instead of keeping it in registers from earlier on.
+__device__ inline void anew(float &x) { asm volatile("" : "+v"(x)); }
+template <typename T, int N>
+__device__ inline void anew(Raw<T, N> &x) {
+  if constexpr (sizeof(x) == 4) {
+    uint32_t bits = __builtin_bit_cast(uint32_t, x);
+    asm volatile("" : "+v"(bits));
+    x = __builtin_bit_cast(Raw<T, N>, bits);
+  }
+}
+
 // ------------------------------------------------------------- documents -----
 // What a row is: -1 of no document, else 4 times its document, + 1 if it is the
 // first of it, + 2 if the last.
-__device__ inline bool row_in(int info) { return info >= 0; }
-__device__ inline bool row_first(int info) { return info >= 0 && (info & 1); }
-__device__ inline bool row_last(int info) { return info >= 0 && (info & 2); }
-// the chain is cut before it
 __device__ inline bool row_cuts(int info) { return info < 0 || (info & 1); }
+
+// The rows of a wave (lane r has what row r is, others -1) that are not inside a
+// document: one bit a row.
+struct Special {
+  uint64_t outs, cuts, lasts;
+  __device__ Special(int info, int rows)
+      : outs(__ballot(info < 0)), cuts(__ballot(row_cuts(info))), lasts(__ballot(info >= 0 && (info & 2))) {
+    const uint64_t all = (uint64_t(1) << rows) - 1;
+    outs &= all;
+    cuts &= all;
+  }
+  __device__ bool out(int r) const { return outs >> r & 1; }    // of no document
+  __device__ bool cut(int r) const { return cuts >> r & 1; }    // the chain is cut before it
+  __device__ bool first(int r) const { return (cuts & ~outs) >> r & 1; }
+  __device__ bool last(int r) const { return lasts >> r & 1; }
+};
 
 struct Docs {
   const int64_t *offsets;
@@ -98,26 +136,61 @@ struct Docs {
   float *out;          // NULL = none
 };
 
-// The rows' documents, by a search for each row; the states of empty documents;
-// and the chain's words cleared.
+// How many offsets are not above `row`, the same in all lanes: the wave looks at
+// 64 places at a time.
+__device__ inline int64_t offsets_upto(const Docs &d, int64_t row, int lane) {
+  int64_t low = 0, high = d.docs + 1;
+  while (low < high) {
+    const int64_t step = (high - low + 63) >> 6, at = low + (lane + 1) * step - 1;
+    const uint64_t upto = __ballot(at < high && d.offsets[at] <= row);
+    // in order: the first ones
+    const int64_t next = low + __popcll(upto) * step;
+    if (step == 1) return next;
+    high = next + step - 1 < high ? next + step - 1 : high;
+    low = next;
+  }
+  return low;
+}
+
+// The rows' documents, 64 rows a wave: a search for the first one, and the next
+// offsets from there; rows of more than 64 documents (many of them empty) are
+// searched for one by one.  And the states of empty documents, and the chain's
+// words cleared.
 __global__ __launch_bounds__(256) void k_documents(const Docs d) {
   const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x, step = int64_t(gridDim.x) * 256;
+  const int lane = threadIdx.x & 63;
   for (int64_t i = at; i < d.clear_count; i += step) d.clear[i] = 0;
-  for (int64_t i = at; i < d.rows; i += step) {
-    int64_t low = 0, high = d.docs + 1;  // offsets that are not above i
-    while (low < high) {
-      const int64_t mid = (low + high) >> 1;
-      if (d.offsets[mid] <= i) low = mid + 1;
-      else high = mid;
+  for (int64_t row0 = at - lane; row0 < d.rows; row0 += step) {
+    const int64_t upto = offsets_upto(d, row0, lane), row = row0 + lane;
+    const int64_t next = upto + lane <= d.docs ? d.offsets[upto + lane] - row0 : 65;
+    const int rel = next > 65 ? 65 : next < 0 ? 0 : int(next);  // of the offsets after the first row's
+    int64_t doc, begin, end;
+    if (__shfl(rel, 63) > 63) {
+      int count = 0;  // of them, not above the row
+#pragma unroll
+      for (int x = 32; x > 0; x >>= 1)
+        if (__shfl(rel, count + x - 1) <= lane) count += x;
+      doc = upto - 1 + count;
+      const int before = __shfl(rel, count - 1 < 0 ? 0 : count - 1), after = __shfl(rel, count);
+      begin = count > 0 ? row0 + before : upto > 0 ? d.offsets[upto - 1] : 0;
+      end = row0 + after;
+    } else {
+      int64_t low = upto, high = d.docs + 1;
+      while (low < high) {
+        const int64_t mid = (low + high) >> 1;
+        if (d.offsets[mid] <= row) low = mid + 1;
+        else high = mid;
+      }
+      doc = low - 1;
+      begin = doc >= 0 ? d.offsets[doc] : 0;
+      end = doc >= 0 && doc < d.docs ? d.offsets[doc + 1] : 0;
     }
-    const int64_t doc = low - 1;
+    if (row >= d.rows) continue;
     int info = -1;
-    if (doc >= 0 && doc < d.docs) {
-      const int64_t begin = d.offsets[doc], end = d.offsets[doc + 1];
-      // a document that begins before the first row begins with it
-      info = int(doc) * 4 + (i == begin || i == 0 ? 1 : 0) + (i + 1 == end || i + 1 == d.rows ? 2 : 0);
-    }
-    d.info[i] = info;
+    // a document that begins before the first row begins with it
+    if (doc >= 0 && doc < d.docs)
+      info = int(doc) * 4 + (row == begin || row == 0 ? 1 : 0) + (row + 1 == end || row + 1 == d.rows ? 2 : 0);
+    d.info[row] = info;
   }
   if (!d.out) return;
   for (int64_t doc = at >> 6; doc < d.docs; doc += step >> 6) {
@@ -130,10 +203,12 @@ __global__ __launch_bounds__(256) void k_documents(const Docs d) {
 }
 
 // ----------------------------------------------------------------- chain -----
-// What a workgroup leaves for the ones after it, for each of its columns: the
-// map's A and B, and the state after its last row, each with a mark beside it in
-// one word of 64 bits, so that a word is there or not.
-constexpr int kWords = 3;
+// What a workgroup leaves for the ones after it, in two words of 64 bits for each
+// of its columns: its map's A and B, and in the place of B, as soon as it has it,
+// the state after its last row.  A word holds its value and beside it what it is,
+// so that a reader needs no order between the words.
+enum : uint32_t { kNothing = 0, kMap = 1, kState = 2 };
+constexpr int kWords = 2;
 struct Chain {
   uint64_t *words;   // [blocks][kWords][cols]
   uint32_t *ticket;  // the workgroups' order
@@ -141,8 +216,8 @@ struct Chain {
   __device__ uint64_t *at(int block, int word, int c) const {
     return words + (int64_t(block) * kWords + word) * cols + c;
   }
-  __device__ void leave(int block, int word, int c, float v) const {
-    __hip_atomic_store(at(block, word, c), uint64_t(1) << 32 | __builtin_bit_cast(uint32_t, v), __ATOMIC_RELAXED,
+  __device__ void leave(int block, int word, int c, uint32_t what, float v) const {
+    __hip_atomic_store(at(block, word, c), uint64_t(what) << 32 | __builtin_bit_cast(uint32_t, v), __ATOMIC_RELAXED,
                        __HIP_MEMORY_SCOPE_AGENT);
   }
   __device__ uint64_t look(int block, int word, int c) const {
@@ -150,7 +225,7 @@ struct Chain {
   }
 };
 
-__device__ inline bool there(uint64_t word) { return word >> 32; }
+__device__ inline uint32_t what(uint64_t word) { return uint32_t(word >> 32); }
 __device__ inline float value(uint64_t word) { return __builtin_bit_cast(float, uint32_t(word)); }
 
 // A workgroup's maps and what it found by looking back, of 64 N columns.
@@ -158,126 +233,164 @@ template <int N>
 struct Shared {
   float a[kWaves][64 * N], b[kWaves][64 * N];
   float past_a[kWindow][64 * N], past_b[kWindow][64 * N];  // of a state: b
-  int cut[kWaves];   // whether a wave's rows cut the chain
-  int state[kWindow];  // whether it is a state
+  int cut[kWaves];  // whether a wave's rows cut the chain
+  int nearest;      // the state among the past that is nearest, kWindow if there is none
   int ticket;
 };
 
-// The state that comes into this wave, after the waves' maps have been left in
-// `s` and synchronised: wave `order` of the workgroup's order, `block` of the
-// workgroups'.  Leaves the workgroup's own map and state.  `needed`: the first
-// row does not cut the chain.
+// What a wave has seen of another workgroup's words.
+template <int N>
+struct Look {
+  uint64_t a[N], b[N];
+  __device__ void take(const Chain &chain, int from, int word, int c, bool in) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) (word ? b : a)[e] = in ? chain.look(from, word, c + e) : 0;
+  }
+  __device__ bool all(const uint64_t (&w)[N], uint32_t is, bool in) const {
+    bool yes = true;
+#pragma unroll
+    for (int e = 0; e < N; ++e) yes &= !in || what(w[e]) == is;
+    return !__ballot(!yes);
+  }
+};
+
+// The state that comes into this wave, whose rows' map is (a, b) and cuts the
+// chain or not: wave `order` of the workgroup's order, `block` of the
+// workgroups'.  Leaves the workgroup's own map and state.  `needed`: the
+// workgroup's first row does not cut the chain.
 //
 // Waits only for workgroups of smaller tickets, which run already and leave
-// their maps without waiting for anything.
+// their maps without waiting for anything.  A look at memory takes 1.5 us in a
+// full machine, as long as a sixth of a workgroup's life, and 2 KiB of all
+// columns' words: a wave looks at one word until it knows that it needs the others
+// (with all columns at each look 366 us instead of 306 for both passes over 65536
+// rows x 1024 of bf16; with the first look before the workgroup's maps are joined
+// 362).
 template <int N>
 __device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int order, bool needed, int c, bool in,
-                                float (&m)[N]) {
+                                const float (&map_a)[N], const float (&map_b)[N], bool cuts, float (&m)[N]) {
   const int lane = threadIdx.x & 63, first = lane * N;
-  // the workgroup's map, and that of the waves before this one
-  float a[N], b[N], own_a[N], own_b[N];
-  bool cut = false, own_cut = false;
+  needed &= block > 0;  // the same in all waves
 #pragma unroll
   for (int e = 0; e < N; ++e) {
-    a[e] = own_a[e] = 1.0f;
-    b[e] = own_b[e] = 0.0f;
+    s.a[order][first + e] = map_a[e];
+    s.b[order][first + e] = map_b[e];
   }
+  if (lane == 0) s.cut[order] = cuts;
+  __syncthreads();
+  // the map of the waves before this one; the first wave's turn is the whole workgroup's
+  float a[N], b[N];
+  bool cut = false;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w == order) {
-      own_cut = cut;
+  for (int e = 0; e < N; ++e) {
+    a[e] = 1.0f;
+    b[e] = 0.0f;
+  }
+  const uint32_t all_cuts = uint32_t(__ballot(lane < kWaves && s.cut[lane & (kWaves - 1)]));
+  const int waves = order == 0 ? kWaves : order;
+  for (int w0 = 0; w0 < waves; w0 += 4) {
+    float wa[4][N], wb[4][N];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        own_a[e] = a[e];
-        own_b[e] = b[e];
+        wa[i][e] = s.a[w0 + i][first + e];
+        wb[i][e] = s.b[w0 + i][first + e];
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool in_turn = w0 + i < waves, now = in_turn && (all_cuts >> (w0 + i) & 1);
+      cut |= now;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float next = __builtin_fmaf(wa[i][e], now ? 0.0f : b[e], wb[i][e]);
+        b[e] = in_turn ? next : b[e];
+        a[e] = in_turn ? a[e] * wa[i][e] : a[e];
       }
     }
-    const bool now = s.cut[w];
-    cut |= now;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      b[e] = now ? s.b[w][first + e] : __builtin_fmaf(s.a[w][first + e], b[e], s.b[w][first + e]);
-      a[e] *= s.a[w][first + e];
-    }
   }
-  const bool known = cut || block == 0;  // the state after the workgroup
+  const bool known = cut || block == 0;  // the state after the workgroup, in its first wave
   if (order == 0 && in) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      if (known) {
-        chain.leave(block, 2, c + e, b[e]);
-      } else {
-        chain.leave(block, 0, c + e, a[e]);
-        chain.leave(block, 1, c + e, b[e]);
-      }
+      if (!known) chain.leave(block, 0, c + e, kMap, a[e]);
+      chain.leave(block, 1, c + e, known ? kState : kMap, b[e]);
     }
   }
   float carry[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) carry[e] = 0.0f;
-  if (block > 0 && needed) {  // the same in all waves
+  if (needed) {
+    const int column = __builtin_amdgcn_readfirstlane(c);
     int found;
-    do {
-      // each wave waits for the maps or states of kAhead workgroups before this one
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int back = order * kAhead + i, from = block - 1 - back;
-        if (from < 0) {
-          if (lane == 0) s.state[back] = 1;  // never reached: block 0 leaves a state
-          continue;
+    while (true) {
+      // each wave looks at every kWaves-th workgroup before this one, until it or another wave has a state that is
+      // nearer than what it waits for
+      for (int back = order; back < kWindow && back < block; back += kWaves) {
+        const int from = block - 1 - back;
+        Look<N> seen;
+        bool state = false;
+        while (true) {
+          const uint32_t peek = __builtin_amdgcn_readfirstlane(what(chain.look(from, 1, column)));
+          if (peek == kState && lane == 0) atomicMin(&s.nearest, back);
+          if (__hip_atomic_load(&s.nearest, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) < back) break;
+          if (peek == kNothing) {
+            __builtin_amdgcn_s_sleep(2);
+            continue;
+          }
+          seen.take(chain, from, 1, c, in);
+          state = seen.all(seen.b, kState, in);
+          if (state) break;
+          if (seen.all(seen.b, kMap, in)) {
+            seen.take(chain, from, 0, c, in);
+            if (seen.all(seen.a, kMap, in)) break;
+          }
         }
-        uint64_t wa[N], wb[N], ws[N];
-        bool map, state;
-        do {
-          map = state = true;
-#pragma unroll
-          for (int e = 0; e < N; ++e) {
-            wa[e] = in ? chain.look(from, 0, c + e) : 0;
-            wb[e] = in ? chain.look(from, 1, c + e) : 0;
-            ws[e] = in ? chain.look(from, 2, c + e) : 0;
-          }
-#pragma unroll
-          for (int e = 0; e < N; ++e) {
-            map &= !in || (there(wa[e]) && there(wb[e]));
-            state &= !in || there(ws[e]);
-          }
-          map = !__ballot(!map);
-          state = !__ballot(!state);
-          if (!map && !state) __builtin_amdgcn_s_sleep(1);
-        } while (!map && !state);
+        if (!state && __hip_atomic_load(&s.nearest, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) < back) break;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-          s.past_a[back][first + e] = value(wa[e]);
-          s.past_b[back][first + e] = state ? value(ws[e]) : value(wb[e]);
+          s.past_a[back][first + e] = value(seen.a[e]);
+          s.past_b[back][first + e] = value(seen.b[e]);
         }
-        if (lane == 0) s.state[back] = state;
+        if (state) {
+          // the word that was peeked at may have been a map then
+          if (lane == 0) atomicMin(&s.nearest, back);
+          break;
+        }
       }
       __syncthreads();
-      found = kWindow;
-#pragma unroll 4
-      for (int i = kWindow - 1; i >= 0; --i) found = s.state[i] ? i : found;
-      if (found == kWindow) __syncthreads();
-    } while (found == kWindow);
+      found = s.nearest;
+      if (found < kWindow) break;
+      __syncthreads();
+    }
 #pragma unroll
     for (int e = 0; e < N; ++e) carry[e] = s.past_b[found][first + e];
     for (int i = found - 1; i >= 0; --i)
 #pragma unroll
       for (int e = 0; e < N; ++e) carry[e] = __builtin_fmaf(s.past_a[i][first + e], carry[e], s.past_b[i][first + e]);
   }
-  if (!known && order == 0 && in) {
+  if (order == 0) {
+    if (!known && in) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) chain.leave(block, 2, c + e, __builtin_fmaf(a[e], carry[e], b[e]));
+      for (int e = 0; e < N; ++e) chain.leave(block, 1, c + e, kState, __builtin_fmaf(a[e], carry[e], b[e]));
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) m[e] = carry[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) m[e] = cut ? b[e] : __builtin_fmaf(a[e], carry[e], b[e]);
   }
-#pragma unroll
-  for (int e = 0; e < N; ++e) m[e] = own_cut ? own_b[e] : __builtin_fmaf(own_a[e], carry[e], own_b[e]);
 }
 
 // The workgroup's place in the order: workgroups of a smaller ticket run.
 template <int N>
 __device__ inline int take_ticket(Shared<N> &s, const Chain &chain) {
-  if (threadIdx.x == 0) s.ticket = int(atomicAdd(chain.ticket, 1u));
+  if (threadIdx.x == 0) {
+    s.ticket = int(atomicAdd(chain.ticket, 1u));
+    s.nearest = kWindow;
+  }
   __syncthreads();
-  return s.ticket;
+  return __builtin_amdgcn_readfirstlane(s.ticket);
 }
 
 template <typename T>
@@ -289,89 +402,78 @@ struct Forward {
   T *h;
   int64_t ldh;
   float *last, *kept;
-  int64_t rows;
-  int cols, groups;
+  int rows, cols, groups;
   Chain chain;
 };
 
 // Bound by its bytes: x and gate in, h out.
 template <typename T, int N>
-__global__ __launch_bounds__(64 * kWaves) void k_recur(const Forward<T> p) {
+__global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
+  constexpr int R = kRows<T, N, false>;
   __shared__ Shared<N> s;
   const int t = take_ticket(s, p.chain), block = t / p.groups;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = (t % p.groups * 64 + lane) * N;
   const bool in = c < p.cols;
   const int at = in ? c : 0;
-  const int64_t row0 = int64_t(block) * kBlock + wave * kRows;
+  const int row0 = block * R * kWaves + wave * R;
   // rows past the end repeat the last one; what they are says that they are of no document
-  const int mine = lane < kRows && row0 + lane < p.rows ? p.info[row0 + lane] : -1;
-  Raw<T, N> x[kRows], g[kRows];
+  const int mine = lane < R && row0 + lane < p.rows ? p.info[row0 + lane] : -1;
+  const int begins = p.info[block * R * kWaves];
+  Raw<T, N> x[R], g[R];
 #pragma unroll
-  for (int r = 0; r < kRows; ++r) {
-    const int64_t row = row0 + r < p.rows ? row0 + r : p.rows - 1;
+  for (int r = 0; r < R; ++r) {
+    const int64_t row = min(row0 + r, p.rows - 1);
     x[r] = load_raw<T, N>(p.x + row * p.ldx + at);
     g[r] = load_raw<T, N>(p.gate + row * p.ld_gate + at);
   }
-  float f[kRows][N], b[kRows][N];
+  float f[R][N], b[R][N];
   float a[N], sum[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) {
     a[e] = 1.0f;
     sum[e] = 0.0f;
   }
+  const Special special(mine, R);
 #pragma unroll
-  for (int r = 0; r < kRows; ++r) {
-    const int info = __builtin_amdgcn_readlane(mine, r);
+  for (int r = 0; r < R; ++r) {
+    const bool cut = special.cut(r);
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       float keep;
       gate<T>(g[r][e], f[r][e], keep);
       b[r][e] = keep * x[r][e];
     }
-    if (row_cuts(info)) {
-      const bool from = p.state && row_first(info);
-      const float *state = p.state + int64_t(info >> 2) * p.cols + at;
+    if (special.first(r) && p.state) {
+      const float *state = p.state + int64_t(__builtin_amdgcn_readlane(mine, r) >> 2) * p.cols + at;
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        if (from) b[r][e] = __builtin_fmaf(f[r][e], state[e], b[r][e]);
-        if (!row_in(info)) b[r][e] = 0.0f;
-        sum[e] = b[r][e];
-        a[e] = 0.0f;
-      }
-    } else {
+      for (int e = 0; e < N; ++e) b[r][e] = __builtin_fmaf(f[r][e], state[e], b[r][e]);
+    }
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        sum[e] = __builtin_fmaf(f[r][e], sum[e], b[r][e]);
-        a[e] *= f[r][e];
-      }
+    for (int e = 0; e < N; ++e) {
+      if (special.out(r)) b[r][e] = 0.0f;
+      f[r][e] = cut ? 0.0f : f[r][e];
+      sum[e] = __builtin_fmaf(f[r][e], cut ? 0.0f : sum[e], b[r][e]);
+      a[e] *= f[r][e];
     }
   }
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    s.a[wave][lane * N + e] = a[e];
-    s.b[wave][lane * N + e] = sum[e];
-  }
-  const bool cuts = __ballot(lane < kRows && row_cuts(mine));
-  if (lane == 0) s.cut[wave] = cuts;
-  const int begins = p.info[int64_t(block) * kBlock];
-  __syncthreads();
   float m[N];
-  state_in<N>(s, p.chain, block, wave, !row_cuts(begins), c, in, m);
+  state_in<N>(s, p.chain, block, wave, !row_cuts(begins), c, in, a, sum, special.cuts != 0, m);
   if (!in || row0 >= p.rows) return;
 #pragma unroll
-  for (int e = 0; e < N; ++e) p.kept[row0 / kRows * p.cols + c + e] = m[e];
-#pragma unroll
-  for (int r = 0; r < kRows; ++r) {
+  for (int r = 0; r < R; ++r) {
     if (row0 + r >= p.rows) break;
-    const int info = __builtin_amdgcn_readlane(mine, r);
-    const bool cut = row_cuts(info);
+    if (r % kKept == 0)
 #pragma unroll
-    for (int e = 0; e < N; ++e) m[e] = cut ? b[r][e] : __builtin_fmaf(f[r][e], m[e], b[r][e]);
-    store_raw<T, N>(p.h + (row0 + r) * p.ldh + c, m);
-    if (row_last(info))
+      for (int e = 0; e < N; ++e) p.kept[int64_t((row0 + r) / kKept) * p.cols + c + e] = m[e];
 #pragma unroll
-      for (int e = 0; e < N; ++e) p.last[int64_t(info >> 2) * p.cols + c + e] = m[e];
+    for (int e = 0; e < N; ++e) m[e] = __builtin_fmaf(f[r][e], special.cut(r) ? 0.0f : m[e], b[r][e]);
+    store_raw<T, N>(p.h + int64_t(row0 + r) * p.ldh + c, m);
+    if (special.last(r)) {
+      float *last = p.last + int64_t(__builtin_amdgcn_readlane(mine, r) >> 2) * p.cols + c;
+#pragma unroll
+      for (int e = 0; e < N; ++e) last[e] = m[e];
+    }
   }
 }
 
@@ -384,8 +486,7 @@ struct Backward {
   T *dx, *dgate;
   int64_t lddx, ld_dgate;
   float *dstate;
-  int64_t rows;
-  int cols, groups, blocks;
+  int rows, cols, groups, blocks;
   Chain chain;
 };
 
@@ -393,96 +494,99 @@ struct Backward {
 // other way: row t passes l_t g_t on to row t - 1, where l_t is f_t, or nothing
 // where the chain is cut; m -> l (dh + m) is a row's map.
 template <typename T, int N>
-__global__ __launch_bounds__(64 * kWaves) void k_recur_backward(const Backward<T> p) {
+__global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backward<T> p) {
+  constexpr int R = kRows<T, N, true>;
   __shared__ Shared<N> s;
   const int t = take_ticket(s, p.chain), back = t / p.groups, block = p.blocks - 1 - back;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = (t % p.groups * 64 + lane) * N;
   const bool in = c < p.cols;
   const int at = in ? c : 0;
-  const int64_t row0 = int64_t(block) * kBlock + wave * kRows;
-  const int mine = lane < kRows && row0 + lane < p.rows ? p.info[row0 + lane] : -1;
-  Raw<T, N> x[kRows], g[kRows], d[kRows];
+  const int row0 = block * R * kWaves + wave * R;
+  const int mine = lane < R && row0 + lane < p.rows ? p.info[row0 + lane] : -1;
+  // whether the row after the workgroup's last one passes anything on
+  const int after = (block + 1) * R * kWaves;
+  const int follows = after < p.rows ? p.info[after] : -1;
+  Raw<T, N> x[R], g[R], d[R];
 #pragma unroll
-  for (int r = 0; r < kRows; ++r) {
-    const int64_t row = row0 + r < p.rows ? row0 + r : p.rows - 1;
+  for (int r = 0; r < R; ++r) {
+    const int64_t row = min(row0 + r, p.rows - 1);
     x[r] = load_raw<T, N>(p.x + row * p.ldx + at);
     g[r] = load_raw<T, N>(p.gate + row * p.ld_gate + at);
     d[r] = load_raw<T, N>(p.dh + row * p.lddh + at);
   }
-  // what the state before a row is above the row's x; the rows' maps from the first row on
-  float u[kRows][N], h[N], a[N], sum[N];
-  const int64_t kept_row = row0 < p.rows ? row0 / kRows : 0;
+  // the rows' gates, and what a row's gradient is multiplied by for dgate; their maps from the first row on
+  float z[R][N], w[R][N], h[N], a[N], sum[N];
+  const int64_t kept_row = row0 < p.rows ? row0 / kKept : 0;
 #pragma unroll
   for (int e = 0; e < N; ++e) {
     h[e] = p.kept[kept_row * p.cols + at + e];
     a[e] = 1.0f;
     sum[e] = 0.0f;
   }
-  bool cut = false;
+  const Special special(mine, R);
+  // only the first of the wave's last rows may lie before a cut
+  const int last = p.dlast && special.lasts ? __ffsll((unsigned long long)special.lasts) - 1 : -1;
+  float more[N];
 #pragma unroll
-  for (int r = 0; r < kRows; ++r) {
-    const int info = __builtin_amdgcn_readlane(mine, r);
-    if (row_cuts(info)) {
-      const bool from = p.state && row_first(info);
+  for (int e = 0; e < N; ++e)
+    more[e] = last < 0 ? 0.0f : p.dlast[int64_t(__builtin_amdgcn_readlane(mine, last) >> 2) * p.cols + at + e];
 #pragma unroll
-      for (int e = 0; e < N; ++e) h[e] = from ? p.state[int64_t(info >> 2) * p.cols + at + e] : 0.0f;
-      cut = true;
+  for (int r = 0; r < R; ++r) {
+    if (special.cut(r)) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) h[e] = 0.0f;
+      if (special.first(r) && p.state)
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          h[e] = p.state[int64_t(__builtin_amdgcn_readlane(mine, r) >> 2) * p.cols + at + e];
     }
-    const bool end = p.dlast && row_last(info);
+    const bool cut = special.cuts << (63 - r);  // this row or one before it: its part goes to no row before them
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      float f, keep;
-      gate<T>(g[r][e], f, keep);
+      float f, k;
+      z[r][e] = gate_of<T>(g[r][e]);
+      open(z[r][e], f, k);
       const float xv = x[r][e];
-      u[r][e] = h[e] - xv;
-      h[e] = __builtin_fmaf(f, h[e], keep * xv);
-      if (!cut) {
-        float dv = d[r][e];
-        if (end) dv += p.dlast[int64_t(info >> 2) * p.cols + at + e];
-        a[e] *= f;
-        sum[e] = __builtin_fmaf(a[e], dv, sum[e]);
-      }
+      w[r][e] = (h[e] - xv) * (f * k);
+      anew(w[r][e]);
+      h[e] = __builtin_fmaf(f, h[e], k * xv);
+      a[e] = cut ? 0.0f : a[e] * f;
+      sum[e] = cut ? sum[e] : __builtin_fmaf(a[e], r == last ? d[r][e] + more[e] : d[r][e], sum[e]);
     }
   }
   const int order = kWaves - 1 - wave;
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    s.a[order][lane * N + e] = cut ? 0.0f : a[e];
-    s.b[order][lane * N + e] = sum[e];
-  }
-  if (lane == 0) s.cut[order] = cut;
-  // whether the row after the workgroup's last one passes anything on
-  const int64_t after = int64_t(block + 1) * kBlock;
-  const int follows = after < p.rows ? p.info[after] : -1;
-  __syncthreads();
   float m[N];
-  state_in<N>(s, p.chain, back, order, !row_cuts(follows), c, in, m);
+  state_in<N>(s, p.chain, back, order, !row_cuts(follows), c, in, a, sum, special.cuts != 0, m);
   if (!in || row0 >= p.rows) return;
 #pragma unroll
-  for (int r = kRows - 1; r >= 0; --r) {
+  for (int r = R - 1; r >= 0; --r) {
     if (row0 + r >= p.rows) continue;
-    const int info = __builtin_amdgcn_readlane(mine, r);
-    const bool inside = row_in(info), end = p.dlast && row_last(info);
-    float dx[N], dg[N], next[N];
+    const int64_t doc = __builtin_amdgcn_readlane(mine, r) >> 2;
+    float dx[N], dg[N];
+    anew(d[r]);
+    // nothing comes to a last row from the next one
+    if (special.last(r) && p.dlast)
+#pragma unroll
+      for (int e = 0; e < N; ++e) m[e] = p.dlast[doc * p.cols + c + e];
+    const bool out = special.out(r);
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      float f, keep;
-      gate<T>(g[r][e], f, keep);
-      float grad = d[r][e] + m[e];
-      if (end) grad += p.dlast[int64_t(info >> 2) * p.cols + c + e];
-      dx[e] = inside ? keep * grad : 0.0f;
-      dg[e] = inside ? grad * u[r][e] * (f * keep) : 0.0f;
-      next[e] = f * grad;
+      float f, k;
+      anew(z[r][e]);
+      open(z[r][e], f, k);
+      const float grad = d[r][e] + m[e];
+      dx[e] = out ? 0.0f : k * grad;
+      dg[e] = out ? 0.0f : w[r][e] * grad;
+      m[e] = f * grad;
     }
-    store_raw<T, N>(p.dx + (row0 + r) * p.lddx + c, dx);
-    store_raw<T, N>(p.dgate + (row0 + r) * p.ld_dgate + c, dg);
-    const bool first = row_cuts(info);
-    if (p.dstate && row_first(info))
+    store_raw<T, N>(p.dx + int64_t(row0 + r) * p.lddx + c, dx);
+    store_raw<T, N>(p.dgate + int64_t(row0 + r) * p.ld_dgate + c, dg);
+    if (special.first(r) && p.dstate)
 #pragma unroll
-      for (int e = 0; e < N; ++e) p.dstate[int64_t(info >> 2) * p.cols + c + e] = next[e];
+      for (int e = 0; e < N; ++e) p.dstate[doc * p.cols + c + e] = m[e];
 #pragma unroll
-    for (int e = 0; e < N; ++e) m[e] = first ? 0.0f : next[e];
+    for (int e = 0; e < N; ++e) m[e] = special.cut(r) ? 0.0f : m[e];
   }
 }
 
@@ -522,8 +626,8 @@ struct Scan {
   int blocks, groups;
   int *info;
   Chain chain;
-  Scan(const lda_recur_args &a, int columns, Arena &ws) {
-    blocks = int(ceil_div(a.rows, kBlock));
+  Scan(const lda_recur_args &a, int columns, int rows_each, Arena &ws) {
+    blocks = int(ceil_div(a.rows, rows_each));
     groups = int(ceil_div(a.cols, 64 * columns));
     info = ws.take<int>(a.rows);
     const int64_t words = int64_t(blocks) * kWords * a.cols;
@@ -552,12 +656,12 @@ struct Scan {
 
 template <typename T, int N>
 hipError_t forward_n(const lda_recur_args &a, Arena &ws, bool dry) {
-  const Scan scan(a, N, ws);
+  const Scan scan(a, N, kRows<T, N, false> * kWaves, ws);
   if (dry) return hipSuccess;
   OPS_TRY(scan.documents(a, a.state, a.last));
   if (a.rows == 0) return hipSuccess;
   const Forward<T> p{static_cast<const T *>(a.x), static_cast<const T *>(a.gate), a.ldx, a.ld_gate, scan.info, a.state,
-                     static_cast<T *>(a.h), a.ldh, a.last, a.kept, a.rows, a.cols, scan.groups, scan.chain};
+                     static_cast<T *>(a.h), a.ldh, a.last, a.kept, int(a.rows), a.cols, scan.groups, scan.chain};
   k_recur<T, N><<<unsigned(scan.blocks) * unsigned(scan.groups), 64 * kWaves, 0, static_cast<hipStream_t>(a.stream)>>>(
       p);
   return hipGetLastError();
@@ -565,13 +669,13 @@ hipError_t forward_n(const lda_recur_args &a, Arena &ws, bool dry) {
 
 template <typename T, int N>
 hipError_t backward_n(const lda_recur_args &a, Arena &ws, bool dry) {
-  const Scan scan(a, N, ws);
+  const Scan scan(a, N, kRows<T, N, true> * kWaves, ws);
   if (dry) return hipSuccess;
   OPS_TRY(scan.documents(a, a.dlast, a.dstate));
   if (a.rows == 0) return hipSuccess;
   const Backward<T> p{static_cast<const T *>(a.x), static_cast<const T *>(a.gate), static_cast<const T *>(a.dh), a.ldx,
                       a.ld_gate, a.lddh, scan.info, a.state, a.kept, a.dlast, static_cast<T *>(a.dx),
-                      static_cast<T *>(a.dgate), a.lddx, a.ld_dgate, a.dstate, a.rows, a.cols, scan.groups, scan.blocks,
+                      static_cast<T *>(a.dgate), a.lddx, a.ld_dgate, a.dstate, int(a.rows), a.cols, scan.groups, scan.blocks,
                       scan.chain};
   k_recur_backward<T, N>
       <<<unsigned(scan.blocks) * unsigned(scan.groups), 64 * kWaves, 0, static_cast<hipStream_t>(a.stream)>>>(p);

@@ -28,7 +28,7 @@ _SIZE = ctypes.c_size_t
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 ACTIVATIONS = {"silu": 0, "gelu": 1, "sigmoid": 2}
 MAX_ROWS, MAX_COLS, MAX_VOCAB, MAX_TILES = 1 << 24, 1 << 20, 1 << 24, 1 << 23
-MAX_TOP, MAX_LISTED, RECUR_ROWS = 256, 1 << 28, 32
+MAX_TOP, MAX_LISTED, RECUR_ROWS = 256, 1 << 28, 16
 
 # Every symbol include/lda_ops.h declares.
 EXPORTS = ("lda_layer_norm", "lda_layer_norm_backward_workspace", "lda_layer_norm_backward", "lda_gated_workspace",

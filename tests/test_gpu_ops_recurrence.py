@@ -96,9 +96,10 @@ def case(ops, dtype, rows, cols, offsets, with_state, with_dlast=True, pad=0, of
         assert not bool(t[outside.cuda()].any())
 
 
-# a wave has 32 rows, a workgroup 256; documents of one row, empty ones, ones over the ends of both
+# a wave has 16 or 32 rows, a workgroup 128 or 256; documents of one row, empty ones, ones over the ends of both
 LENGTHS = [[1], [2], [31], [32], [33], [255], [256], [257], [1, 1, 1], [0, 5, 0, 0, 3, 0], [32, 32], [31, 1, 32, 1],
-           [200, 300, 7, 0, 90], [256, 256, 1], [700], [1] * 70, [3] * 90 + [500]]
+           [200, 300, 7, 0, 90], [256, 256, 1], [700], [1] * 70, [3] * 90 + [500], [15, 1, 16, 17], [127, 1, 128],
+           [129, 127, 128, 0, 0, 128], [0] * 200 + [40] + [0] * 100 + [1, 0, 1] + [0] * 70 + [90] + [0] * 65]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
