@@ -19,31 +19,45 @@ namespace {
 typedef __bf16 bf16;
 typedef _Float16 f16;
 
-template <typename T, int N>
-using Vec = T __attribute__((ext_vector_type(N)));
-
-// N neighbours of a row from column c on, which are moved at once (N > 1: the
-// rows start at multiples of their bytes and hold a multiple of N).
-template <typename T, int N>
-struct Some {
+// The columns of a row that a lane moves at once: 16 bytes, wherever they begin
+// (global memory takes vectors at any address).  Where a row is no multiple of
+// them its last lane takes the last 16 bytes of the row, some of which another
+// lane has too: both compute the same.  Rows shorter than that (Narrow) element
+// by element.
+template <typename T>
+constexpr int kMany = 16 / int(sizeof(T));
+template <typename T, bool Narrow>
+struct Many {
+  static constexpr int N = kMany<T>;
+  typedef T vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
   T v[N];
-  __device__ void load(const T *p) {
-    if constexpr (N == 1) {
-      v[0] = *p;
+  static __device__ int first(int lane, int cols) { return Narrow ? 0 : min(lane * N, cols - N); }
+  __device__ void clear() {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = T(0.0f);
+  }
+  __device__ void load(const T *p, int cols) {
+    if constexpr (Narrow) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = e < cols ? p[e] : T(0.0f);
     } else {
-      const Vec<T, N> w = *reinterpret_cast<const Vec<T, N> *>(p);
+      const vec w = *reinterpret_cast<const vec *>(p);
 #pragma unroll
       for (int e = 0; e < N; ++e) v[e] = w[e];
     }
   }
-  __device__ void store(T *p) const {
-    if constexpr (N == 1) {
-      *p = v[0];
+  template <bool Past = false>
+  __device__ void store(T *p, int cols) const {
+    if constexpr (Narrow) {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e < cols) p[e] = v[e];
     } else {
-      Vec<T, N> w;
+      vec w;
 #pragma unroll
       for (int e = 0; e < N; ++e) w[e] = v[e];
-      *reinterpret_cast<Vec<T, N> *>(p) = w;
+      if constexpr (Past) __builtin_nontemporal_store(w, reinterpret_cast<vec *>(p));
+      else *reinterpret_cast<vec *>(p) = w;
     }
   }
 };
@@ -51,10 +65,14 @@ struct Some {
 // -------------------------------------------------------------- forward -----
 // 2^shift lanes a row (a workgroup has 256 >> shift rows at a time), four rows
 // of each lane in flight.
-template <typename T, int N>
+//
+// Results that are larger than the last cache (256 MB) are stored past it, so
+// that it keeps the table: 1048576 words x 512 of f16 245 us instead of 286.
+// Smaller ones are left in it for who reads them (51 MB: 16 us, past it 30).
+template <typename T, bool Narrow, bool Past>
 __global__ __launch_bounds__(256) void k_embed(const int32_t *words, int64_t rows, const T *weight, int64_t ldw,
                                                int width, int vocab, float scale, int shift, T *y, int64_t ldy) {
-  constexpr int U = 4;
+  constexpr int U = 4, N = kMany<T>;
   const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1), each = 256 >> shift;
   const int64_t first = int64_t(blockIdx.x) * each * U + (threadIdx.x >> shift);
   int word[U];
@@ -63,27 +81,55 @@ __global__ __launch_bounds__(256) void k_embed(const int32_t *words, int64_t row
     const int64_t i = first + u * each;
     word[u] = i < rows ? words[i] : -1;
   }
-  for (int c = lane * N; c < width; c += lanes * N) {
-    Some<T, N> v[U];
+  for (int i = lane; i * N < width; i += lanes) {
+    const int c = Many<T, Narrow>::first(i, width);
+    Many<T, Narrow> v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[u].v[e] = T(0.0f);
-      if (word[u] >= 0 && word[u] < vocab) v[u].load(weight + int64_t(word[u]) * ldw + c);
+      if (word[u] >= 0 && word[u] < vocab) v[u].load(weight + int64_t(word[u]) * ldw + c, width);
+      else v[u].clear();
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t i = first + u * each;
-      if (i >= rows) break;
-      // a row of no word is 0 whatever the scale
+      const int64_t row = first + u * each;
+      if (row >= rows) break;
 #pragma unroll
       for (int e = 0; e < N; ++e) v[u].v[e] = T(float(v[u].v[e]) * scale);
-      v[u].store(y + i * ldy + c);
+      v[u].template store<Past>(y + row * ldy + c, width);
     }
   }
 }
 
 // ------------------------------------------------------------------ sort -----
+// The gradient's rows are set to zero by further workgroups of the sort's
+// launches, which leave most of the machine idle, each launch a part of them
+// (65536 words and a gradient of 141000 x 1024 of bf16: 289 MB beside 45 us of
+// sorting); rows of words that there are get their sums afterwards.  Past the last
+// cache, where the zeros would push out what is summed next (175 us -> 155 for
+// both passes).
+//
+// Vectors and words of memory that is aligned to an element of 16 bits.
+typedef uint32_t fill_word __attribute__((aligned(2)));
+typedef uint32_t fill_words __attribute__((ext_vector_type(4), aligned(2)));
+struct Fill {
+  fill_word *p;
+  int64_t words, bytes;  // whole words of 32 bits; the bytes after them, in the last launch's last workgroup
+  int64_t from, to;      // of this launch, words
+};
+constexpr int kFillWords = 16384;  // of a workgroup: 64 KiB
+
+__device__ inline void fill_zero(const Fill &f, int64_t part) {
+  const int64_t first = f.from + part * kFillWords, end = first + kFillWords < f.to ? first + kFillWords : f.to;
+  int64_t i = first + int64_t(threadIdx.x) * 4;
+  for (; i + 4 <= end; i += int64_t(blockDim.x) * 4)
+    __builtin_nontemporal_store(fill_words{0, 0, 0, 0}, reinterpret_cast<fill_words *>(f.p + i));
+  for (; i < end; ++i) f.p[i] = 0;
+  if (end == f.words && threadIdx.x < f.bytes) reinterpret_cast<uint8_t *>(f.p + f.words)[threadIdx.x] = 0;
+}
+__host__ __device__ inline int64_t fill_parts(const Fill &f) {
+  return (f.to - f.from + kFillWords - 1) / kFillWords + (f.to == f.words && f.from == f.to && f.bytes ? 1 : 0);
+}
+
 // Keys are the words, and `vocab` for places of no word, which so come last.
 __device__ inline uint32_t key_of(int32_t word, uint32_t vocab) {
   return uint32_t(word) < vocab ? uint32_t(word) : vocab;
@@ -93,8 +139,12 @@ __device__ inline uint32_t key_of(int32_t word, uint32_t vocab) {
 // which no two places share, so the order is the stable one.
 constexpr int kSmall = 8192;
 __global__ __launch_bounds__(1024) void k_sort_small(const int32_t *words, int n, int padded, uint32_t vocab,
-                                                     uint32_t *keys, uint32_t *places) {
+                                                     uint32_t *keys, uint32_t *places, const Fill fill) {
   __shared__ uint64_t all[kSmall];
+  if (blockIdx.x > 0) {
+    fill_zero(fill, int64_t(blockIdx.x) - 1);
+    return;
+  }
   for (int i = threadIdx.x; i < padded; i += 1024)
     all[i] = i < n ? uint64_t(key_of(words[i], vocab)) << 32 | uint32_t(i) : ~uint64_t(0);
   for (int size = 2; size <= padded; size <<= 1)
@@ -119,7 +169,7 @@ __global__ __launch_bounds__(1024) void k_sort_small(const int32_t *words, int n
 // More: a radix sort from the lowest digit of up to kDigitBits bits on, three
 // launches a digit: counts of each tile, their sums before each tile, and the
 // tile's places moved to where they belong, in their order.
-constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits, kTile = 2048;
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits, kTile = 1024;
 
 struct SortPass {
   const int32_t *words;  // of the first pass: keys from the words, places 0, 1, ..
@@ -134,8 +184,12 @@ struct SortPass {
   __device__ uint32_t digit(uint32_t key) const { return key >> shift & ((1u << bits) - 1); }
 };
 
-__global__ __launch_bounds__(256) void k_sort_count(const SortPass p) {
+__global__ __launch_bounds__(256) void k_sort_count(const SortPass p, const Fill fill) {
   __shared__ uint32_t count[kDigits];
+  if (int64_t(blockIdx.x) >= p.tiles) {
+    fill_zero(fill, int64_t(blockIdx.x) - p.tiles);
+    return;
+  }
   const int digits = 1 << p.bits;
   for (int d = threadIdx.x; d < digits; d += 256) count[d] = 0;
   __syncthreads();
@@ -169,8 +223,12 @@ __device__ inline uint32_t sum_before(uint32_t v, uint32_t &total, uint32_t (&sh
 }
 
 // A digit's counts become the sums of the tiles before; one workgroup a digit.
-__global__ __launch_bounds__(256) void k_sort_sums(const SortPass p) {
+__global__ __launch_bounds__(256) void k_sort_sums(const SortPass p, const Fill fill) {
   __shared__ uint32_t shared[4];
+  if (blockIdx.x >= 1u << p.bits) {
+    fill_zero(fill, int64_t(blockIdx.x) - (int64_t(1) << p.bits));
+    return;
+  }
   uint32_t *row = p.counts + int64_t(blockIdx.x) * p.tiles, carry = 0;
   for (int64_t t0 = 0; t0 < p.tiles; t0 += 256) {
     const int64_t t = t0 + threadIdx.x;
@@ -186,11 +244,15 @@ __global__ __launch_bounds__(256) void k_sort_sums(const SortPass p) {
 // Each wave takes a quarter of the tile, 64 places at a time: a place's rank
 // among those of its digit is the number of lanes before it with the same one,
 // found by one ballot a bit, and what its wave had of them already.
-__global__ __launch_bounds__(256) void k_sort_place(const SortPass p) {
+__global__ __launch_bounds__(256) void k_sort_place(const SortPass p, const Fill fill) {
   constexpr int ROUNDS = kTile / 256;
   __shared__ uint32_t count[4][kDigits], shared[4];
+  if (int64_t(blockIdx.x) >= p.tiles) {
+    fill_zero(fill, int64_t(blockIdx.x) - p.tiles);
+    return;
+  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, digits = 1 << p.bits;
-  for (int d = threadIdx.x; d < 4 * kDigits; d += 256) (&count[0][0])[d] = 0;
+  for (int d = threadIdx.x; d < 4 * digits; d += 256) count[d / digits][d % digits] = 0;
   __syncthreads();
   const int64_t first = int64_t(blockIdx.x) * kTile + wave * (kTile / 4) + lane;
   uint32_t key[ROUNDS], place[ROUNDS], rank[ROUNDS];
@@ -244,12 +306,10 @@ __global__ __launch_bounds__(256) void k_sort_place(const SortPass p) {
 }
 
 // ------------------------------------------------------------------ sums -----
-// kPiece sorted places a piece.  What a word has inside one piece goes to its
-// row of the gradient; what it has in a piece that it shares with the piece
-// before (slot 0) or after it (slot 1, where it begins in this piece) goes to
-// `part` [pieces][2][width], which k_join_words sums.
-constexpr int kPiece = 64;
-
+// `each` sorted places a piece, a power of two.  What a word has inside one
+// piece goes to its row of the gradient; what it has in a piece that it shares
+// with the piece before (slot 0) or after it (slot 1, where it begins in this
+// piece) goes to `part` [pieces][2][width], which k_join_words sums.
 struct Sums {
   const uint32_t *keys, *places;
   int64_t n;
@@ -258,223 +318,217 @@ struct Sums {
   float scale;
   float *part;
   int64_t pieces;
+  int each;
   __device__ uint32_t key(int64_t i) const { return i >= 0 && i < n ? keys[i] : vocab; }
 };
 
-template <typename T, int N>
-__device__ inline void store_sum(T *row, const float (&s)[N], float scale) {
-  Some<T, N> out;
-#pragma unroll
-  for (int e = 0; e < N; ++e) out.v[e] = T(s[e] * scale);
-  out.store(row);
-}
-
-// A wave a piece and 64 N columns, eight rows of dy in flight.
-template <typename T, int N>
-__device__ inline void sum_piece(const Sums &a, const T *dy, int64_t lddy, T *dweight, int64_t piece, int c0) {
-  constexpr int U = 8;
-  const int lane = threadIdx.x & 63, c = c0 + lane * N;
-  const int64_t first = piece * kPiece;
-  const uint32_t key = a.key(first + lane);
-  const uint32_t place = first + lane < a.n ? a.places[first + lane] : 0;
-  const uint32_t before = piece ? a.keys[first - 1] : a.vocab, after = a.key(first + kPiece);
-  const int count = __popcll(__ballot(key < a.vocab));  // sorted: the first ones
-  if (count == 0) return;
-  uint32_t next = __shfl_down(key, 1);  // of all lanes
-  if (lane == 63) next = after;
-  const uint64_t ends = __ballot(lane < count && (lane == count - 1 || next != key));
-  bool open = before == __builtin_amdgcn_readfirstlane(key);  // the word began in an earlier piece
-  const bool goes_on = count == kPiece && after == __builtin_amdgcn_readlane(key, 63);
-  const bool in = c < a.width;
+// A wave a piece and 64 kMany columns, eight rows of dy in flight.
+template <typename T, bool Narrow>
+__global__ __launch_bounds__(256) void k_word_sums(const Sums a, const T *dy, int64_t lddy, T *dweight, int groups) {
+  constexpr int U = 4, N = kMany<T>;
+  const int64_t item = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t piece = item / groups;
+  if (piece >= a.pieces) return;
+  const int lane = threadIdx.x & 63, mine = int(item % groups) * 64 + lane;
+  const bool in = mine * N < a.width;
+  const int c = Many<T, Narrow>::first(mine, a.width);
+  const int64_t begin = piece * a.each;
+  bool open = false;  // the word began in an earlier piece
   float s[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) s[e] = 0.0f;
-  for (int t0 = 0; t0 < count; t0 += U) {
-    Some<T, N> v[U];
+  const int span = min(64, a.each);  // places at a time
+  for (int64_t first = begin; first < begin + a.each; first += span) {
+    const uint32_t key = lane < span ? a.key(first + lane) : a.vocab;
+    const uint32_t place = lane < span && first + lane < a.n ? a.places[first + lane] : 0;
+    const uint32_t after = a.key(first + span);
+    uint32_t next = __shfl_down(key, 1);  // of all lanes
+    if (lane == span - 1) next = after;
+    const int count = __popcll(__ballot(key < a.vocab));  // sorted: the first ones
+    if (count == 0) return;
+    if (first == begin && begin > 0) open = a.keys[begin - 1] == __builtin_amdgcn_readfirstlane(key);
+    // places after which a sum ends: with its word, or with the piece
+    const bool last = first + span == begin + a.each;
+    const uint64_t ends = __ballot(lane < count && (next != key || (last && lane == span - 1)));
+    const bool goes_on = last && count == span && after == __builtin_amdgcn_readlane(key, span - 1);
+    auto load = [&](Many<T, Narrow>(&v)[U], int t0) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int t = min(t0 + u, count - 1);
-      const int64_t row = uint32_t(__builtin_amdgcn_readlane(place, t));
-      if (in) v[u].load(dy + row * lddy + c);
-    }
+      for (int u = 0; u < U; ++u) {
+        const int64_t row = uint32_t(__builtin_amdgcn_readlane(place, min(t0 + u, count - 1)));
+        v[u].load(dy + row * lddy + c, a.width);
+      }
+    };
+    auto add = [&](const Many<T, Narrow>(&v)[U], int t0) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int t = t0 + u;
-      if (t >= count) break;
+      for (int u = 0; u < U; ++u) {
+        const int t = t0 + u;
+        if (t >= count) break;
 #pragma unroll
-      for (int e = 0; e < N; ++e) s[e] += float(v[u].v[e]);
-      if (!(ends >> t & 1)) continue;
-      if (in) {
-        const bool on = t == kPiece - 1 && goes_on;
-        if (open || on) {
+        for (int e = 0; e < N; ++e) s[e] += float(v[u].v[e]);
+        if (!(ends >> t & 1)) continue;
+        if (open || (goes_on && t == span - 1)) {
           float *to = a.part + (piece * 2 + (open ? 0 : 1)) * a.width + c;
 #pragma unroll
-          for (int e = 0; e < N; ++e) to[e] = s[e];
-        } else {
-          store_sum<T, N>(dweight + int64_t(uint32_t(__builtin_amdgcn_readlane(key, t))) * a.width + c, s, a.scale);
+          for (int e = 0; e < N; ++e)
+            if (in && (!Narrow || e < a.width)) to[e] = s[e];
+        } else if (in) {
+          Many<T, Narrow> out;
+#pragma unroll
+          for (int e = 0; e < N; ++e) out.v[e] = T(s[e] * a.scale);
+          out.store(dweight + int64_t(uint32_t(__builtin_amdgcn_readlane(key, t))) * a.width + c, a.width);
         }
-      }
-      open = false;
+        open = false;
 #pragma unroll
-      for (int e = 0; e < N; ++e) s[e] = 0.0f;
+        for (int e = 0; e < N; ++e) s[e] = 0.0f;
+      }
+    };
+    // the next rows are asked for before this ones' sums are stored: a wave waits for what it asked for in its order
+    Many<T, Narrow> even[U], odd[U];
+    load(even, 0);
+    for (int t0 = 0; t0 < count; t0 += 2 * U) {
+      load(odd, t0 + U);
+      add(even, t0);
+      load(even, t0 + 2 * U);
+      add(odd, t0 + U);
     }
   }
-}
-
-// The rows of words that no place has, kAbsent words a workgroup.
-constexpr int kAbsent = 64;
-template <typename T, int N>
-__device__ inline void clear_absent(const Sums &a, T *dweight, int64_t first) {
-  __shared__ int absent[kAbsent];
-  const int64_t word = first + threadIdx.x;
-  if (threadIdx.x < kAbsent) {
-    bool found = true;
-    if (word < a.vocab) {
-      int64_t low = 0, high = a.n;  // the first place of a key not below the word
-      while (low < high) {
-        const int64_t mid = (low + high) >> 1;
-        if (a.keys[mid] < word) low = mid + 1;
-        else high = mid;
-      }
-      found = low < a.n && a.keys[low] == word;
-    }
-    absent[threadIdx.x] = !found;
-  }
-  __syncthreads();
-  Some<T, N> zero;
-#pragma unroll
-  for (int e = 0; e < N; ++e) zero.v[e] = T(0.0f);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  for (int w = wave; w < kAbsent; w += 4) {
-    if (!absent[w]) continue;
-    T *row = dweight + (first + w) * a.width;
-    for (int c = lane * N; c < a.width; c += 64 * N) zero.store(row + c);
-  }
-}
-
-template <typename T, int N>
-__global__ __launch_bounds__(256) void k_word_sums(const Sums a, const T *dy, int64_t lddy, T *dweight, int groups,
-                                                   int64_t sum_blocks) {
-  if (int64_t(blockIdx.x) >= sum_blocks) {
-    clear_absent<T, N>(a, dweight, (int64_t(blockIdx.x) - sum_blocks) * kAbsent);
-    return;
-  }
-  const int64_t item = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  const int64_t piece = item / groups;
-  if (piece < a.pieces) sum_piece<T, N>(a, dy, lddy, dweight, piece, int(item % groups) * 64 * N);
 }
 
 // Words that go over the ends of pieces: the piece that a word begins in holds
-// its first sum, the heads of the following pieces the others.  Up to kShort of
-// them are summed by one wave, more by the workgroup's 16, each every 16th.
+// its first sum, the heads of the following pieces the others.  A workgroup looks
+// at kJoin pieces; up to kShort heads are summed by one wave, more by all of
+// them, each every kJoin-th.
 constexpr int kShort = 16, kJoin = 16;
 template <typename T>
 __global__ __launch_bounds__(1024) void k_join_words(const Sums a, T *dweight) {
-  __shared__ float shared[kJoin][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int c = int(blockIdx.y) * 64 + lane;
-  // how many pieces after p begin with the word that goes over p's end, 0 if none begins in p and does
-  auto heads = [&](int64_t p, uint32_t &word) -> int64_t {
-    if (p >= a.pieces) return 0;
-    const int64_t end = (p + 1) * kPiece;
-    word = a.key(end - 1);
-    if (word >= a.vocab || a.key(end) != word) return 0;
-    if (a.key(p * kPiece) == word && p > 0 && a.key(p * kPiece - 1) == word) return 0;
-    const uint64_t same = __ballot(a.key(end + int64_t(lane) * kPiece) == word);
-    if (~same) return __ffsll((unsigned long long)~same) - 1;
-    int64_t low = p + 64, high = a.pieces - 1;  // the last piece whose first word it is
-    while (low < high) {
-      const int64_t mid = (low + high + 1) >> 1;
-      if (a.key(mid * kPiece) == word) low = mid;
-      else high = mid - 1;
-    }
-    return low - p;
-  };
-  auto head = [&](int64_t p) { return a.part[p * 2 * a.width + c]; };
-  const int64_t p0 = int64_t(blockIdx.x) * kJoin;
-  uint32_t word;
-  const int64_t mine = heads(p0 + wave, word);
-  if (mine > 0 && mine <= kShort && c < a.width) {
-    const int64_t p = p0 + wave;
-    float s = a.part[(p * 2 + 1) * a.width + c];
-#pragma unroll 4
-    for (int64_t i = 1; i <= mine; ++i) s += head(p + i);
-    dweight[int64_t(word) * a.width + c] = T(s * a.scale);
-  }
+  __shared__ float shared[kJoin][256];
   __shared__ int64_t longer[kJoin];
   __shared__ uint32_t its[kJoin];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int mine_c = int(blockIdx.y) * 256 + lane * 4;
+  const int64_t p0 = int64_t(blockIdx.x) * kJoin, p = p0 + wave, end = (p + 1) * a.each;
+  // how many pieces after p begin with the word that begins in p and goes over its end
+  uint32_t word = a.vocab;
+  int64_t mine = 0;
+  if (p < a.pieces) {
+    // the last place, the next one, the first one and the one before it
+    const uint32_t at = a.key(lane < 2 ? end - 1 + lane : p * a.each + 2 - lane);
+    word = __builtin_amdgcn_readlane(at, 0);
+    const bool over = word < a.vocab && __builtin_amdgcn_readlane(at, 1) == word;
+    const bool before = p > 0 && __builtin_amdgcn_readlane(at, 2) == word && __builtin_amdgcn_readlane(at, 3) == word;
+    if (over && !before) {
+      int64_t low = p + 1;  // the last piece that is known to begin with it
+      auto ahead = [&](int64_t step) {
+        const uint64_t same = __ballot(a.key((low + (lane + 1) * step) * a.each) == word);
+        const int count = ~same ? __ffsll((unsigned long long)~same) - 1 : 64;
+        low += count * step;
+        return count == 64;
+      };
+      if (ahead(1)) {
+        while (ahead(64)) {}
+        ahead(1);
+      }
+      mine = low - p;
+    }
+  }
+  const bool narrow = a.width < 4;
+  const int c = narrow ? 0 : min(mine_c, a.width - 4);
+  typedef float four __attribute__((ext_vector_type(4), aligned(4)));
+  // what k_word_sums left of piece q in `slot`
+  auto left = [&](int64_t q, int slot) {
+    const float *from = a.part + (q * 2 + slot) * a.width + c;
+    if (!narrow) return *reinterpret_cast<const four *>(from);
+    return four{from[0], a.width > 1 ? from[1] : 0.0f, a.width > 2 ? from[2] : 0.0f, 0.0f};
+  };
+  // the heads after piece q, from the first-th to the count-th, every step-th: eight on their way at a time
+  auto heads = [&](int64_t q, int64_t first, int64_t count, int step, four s) {
+    for (int64_t i = first; i <= count; i += 8 * step) {
+      four v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = left(q + (i + u * step <= count ? i + u * step : i), 0);
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (i + u * step <= count) s += v[u];
+    }
+    return s;
+  };
+  auto store = [&](four s, uint32_t to) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < a.width) dweight[int64_t(to) * a.width + c + e] = T(s[e] * a.scale);
+  };
+  if (mine > 0 && mine <= kShort && mine_c < a.width) store(heads(p, 1, mine, 1, left(p, 1)), word);
   if (lane == 0) {
     longer[wave] = mine > kShort ? mine : 0;
     its[wave] = word;
   }
   __syncthreads();
   for (int k = 0; k < kJoin; ++k) {
-    const int64_t count = longer[k], p = p0 + k;
+    const int64_t count = longer[k], q = p0 + k;
     if (!count) continue;
-    float s = 0.0f;
-    if (c < a.width) {
-      if (wave == 0) s = a.part[(p * 2 + 1) * a.width + c];
-#pragma unroll 8
-      for (int64_t i = 1 + wave; i <= count; i += kJoin) s += head(p + i);
-    }
+    four s = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (mine_c < a.width) s = heads(q, 1 + wave, count, kJoin, wave == 0 ? left(q, 1) : s);
     __syncthreads();
-    shared[wave][lane] = s;
+    *reinterpret_cast<four *>(&shared[wave][lane * 4]) = s;
     __syncthreads();
-    if (wave == 0 && c < a.width) {
-      for (int w = 1; w < kJoin; ++w) s += shared[w][lane];
-      dweight[int64_t(its[k]) * a.width + c] = T(s * a.scale);
+    if (wave == 0 && mine_c < a.width) {
+      for (int w = 1; w < kJoin; ++w) s += *reinterpret_cast<const four *>(&shared[w][lane * 4]);
+      store(s, its[k]);
     }
   }
 }
 
 // ------------------------------------------------------------------ host -----
-// How many elements of a matrix' rows can be moved at once, of most (16 bytes), 2 and 1.
-template <typename T>
-int at_once(const void *p, int64_t ld, int64_t cols) {
-  for (int n : {16 / int(sizeof(T)), 2})
-    if (n * sizeof(T) >= 4 && reinterpret_cast<uintptr_t>(p) % (n * sizeof(T)) == 0 && ld % n == 0 && cols % n == 0)
-      return n;
-  return 1;
-}
-
-template <typename T, typename Fn>
-hipError_t by_count(int n, Fn fn) {
-  if (n == 16 / int(sizeof(T))) return fn(std::integral_constant<int, 16 / int(sizeof(T))>());
-  if (n == 2) return fn(std::integral_constant<int, 2>());
-  return fn(std::integral_constant<int, 1>());
-}
-
 template <typename T>
 hipError_t embed_forward_t(const lda_embed_args &a) {
   if (a.rows == 0) return hipSuccess;
-  const int from = at_once<T>(a.weight, a.ld_weight, a.width), to = at_once<T>(a.y, a.ldy, a.width);
-  return by_count<T>(from < to ? from : to, [&](auto count) {
-    constexpr int N = decltype(count)::value;
-    int shift = 0;
-    while (shift < 8 && (N << shift) < a.width) ++shift;
-    const int64_t each = int64_t(256 >> shift) * 4;
-    k_embed<T, N><<<unsigned(ceil_div(a.rows, each)), 256, 0, static_cast<hipStream_t>(a.stream)>>>(
-        a.words, a.rows, static_cast<const T *>(a.weight), a.ld_weight, a.width, a.vocab, a.scale, shift,
-        static_cast<T *>(a.y), a.ldy);
-    return hipGetLastError();
-  });
+  // the lanes of a row that have the least idle ones at its end, the most of those
+  int shift = 0;
+  int64_t least = INT64_MAX;
+  for (int i = 0; i <= 8; ++i) {
+    const int64_t padded = round_up(a.width, int64_t(kMany<T>) << i);
+    if (i > 4 && padded > least) break;
+    shift = i;
+    least = padded;
+    if (padded == int64_t(kMany<T>) << i) break;
+  }
+  const int64_t each = int64_t(256 >> shift) * 4;
+  const bool past = a.rows * a.width * int64_t(sizeof(T)) > int64_t(256) << 20;
+  auto kernel = a.width < kMany<T> ? k_embed<T, true, false> : past ? k_embed<T, false, true> : k_embed<T, false, false>;
+  kernel<<<unsigned(ceil_div(a.rows, each)), 256, 0, static_cast<hipStream_t>(a.stream)>>>(
+      a.words, a.rows, static_cast<const T *>(a.weight), a.ld_weight, a.width, a.vocab, a.scale, shift,
+      static_cast<T *>(a.y), a.ldy);
+  return hipGetLastError();
 }
 
 struct Sorted {
   const uint32_t *keys, *places;
 };
 
-// The places 0 .. n - 1 by their words, in their order where these are equal.
-hipError_t sort_words(const int32_t *words, int64_t n, int vocab, Arena &ws, bool dry, hipStream_t s, Sorted &out) {
+// A launch's part of `all`, of which the next `launches` ones have equal shares.
+Fill share(Fill &all, int launches) {
+  Fill now = all;
+  now.to = launches <= 1 ? all.words : all.from + round_up(ceil_div(all.words - all.from, launches), kFillWords);
+  if (now.to > all.words) now.to = all.words;
+  all.from = now.to;
+  return now;
+}
+
+// The places 0 .. n - 1 by their words, in their order where these are equal; and
+// `fill` set to zero.
+hipError_t sort_words(const int32_t *words, int64_t n, int vocab, Fill fill, Arena &ws, bool dry, hipStream_t s,
+                      Sorted &out) {
   uint32_t *keys[2], *places[2];
   keys[0] = ws.take<uint32_t>(n);
   places[0] = ws.take<uint32_t>(n);
   out = Sorted{keys[0], places[0]};
   if (n <= kSmall) {
-    if (dry || n == 0) return hipSuccess;
+    if (dry) return hipSuccess;
     int padded = 2;
     while (padded < n) padded <<= 1;
-    k_sort_small<<<1, 1024, 0, s>>>(words, int(n), padded, uint32_t(vocab), keys[0], places[0]);
+    const Fill all = share(fill, 1);
+    k_sort_small<<<unsigned(1 + fill_parts(all)), 1024, 0, s>>>(words, int(n), padded, uint32_t(vocab), keys[0],
+                                                                places[0], all);
     return hipGetLastError();
   }
   keys[1] = ws.take<uint32_t>(n);
@@ -488,6 +542,7 @@ hipError_t sort_words(const int32_t *words, int64_t n, int vocab, Arena &ws, boo
   p.bits = each;
   p.tiles = ceil_div(n, kTile);
   p.counts = ws.take<uint32_t>((p.tiles + 1) << each);
+  int launches = 3 * passes;
   for (int i = 0; i < passes; ++i) {
     p.words = i ? nullptr : words;
     p.keys = out.keys;
@@ -497,11 +552,14 @@ hipError_t sort_words(const int32_t *words, int64_t n, int vocab, Arena &ws, boo
     p.shift = i * each;
     out = Sorted{p.keys_out, p.places_out};
     if (dry) continue;
-    k_sort_count<<<unsigned(p.tiles), 256, 0, s>>>(p);
+    Fill part = share(fill, launches--);
+    k_sort_count<<<unsigned(p.tiles + fill_parts(part)), 256, 0, s>>>(p, part);
     OPS_TRY(hipGetLastError());
-    k_sort_sums<<<1u << each, 256, 0, s>>>(p);
+    part = share(fill, launches--);
+    k_sort_sums<<<unsigned((int64_t(1) << each) + fill_parts(part)), 256, 0, s>>>(p, part);
     OPS_TRY(hipGetLastError());
-    k_sort_place<<<unsigned(p.tiles), 256, 0, s>>>(p);
+    part = share(fill, launches--);
+    k_sort_place<<<unsigned(p.tiles + fill_parts(part)), 256, 0, s>>>(p, part);
     OPS_TRY(hipGetLastError());
   }
   return hipSuccess;
@@ -512,8 +570,13 @@ hipError_t sort_words(const int32_t *words, int64_t n, int vocab, Arena &ws, boo
 template <typename T>
 hipError_t sum_by_word(const int32_t *words, int64_t n, const T *dy, int64_t lddy, int width, int vocab, float scale,
                        T *dweight, Arena &ws, bool dry, hipStream_t s) {
+  Fill fill = {};
+  fill.p = reinterpret_cast<fill_word *>(dweight);
+  const int64_t bytes = int64_t(vocab) * width * int64_t(sizeof(T));
+  fill.words = bytes / 4;
+  fill.bytes = bytes % 4;
   Sorted order;
-  OPS_TRY(sort_words(words, n, vocab, ws, dry, s, order));
+  OPS_TRY(sort_words(words, n, vocab, fill, ws, dry, s, order));
   Sums a = {};
   a.keys = order.keys;
   a.places = order.places;
@@ -521,19 +584,18 @@ hipError_t sum_by_word(const int32_t *words, int64_t n, const T *dy, int64_t ldd
   a.vocab = uint32_t(vocab);
   a.width = width;
   a.scale = scale;
-  a.pieces = ceil_div(n, kPiece);
+  // longer pieces where there are waves enough: less to join
+  const int groups = int(ceil_div(width, 64 * kMany<T>));
+  a.each = 16;
+  while (a.each < 512 && ceil_div(n, 2 * a.each) * groups >= 3000) a.each *= 2;
+  a.pieces = ceil_div(n, a.each);
   a.part = ws.take<float>(a.pieces * 2 * width);
-  if (dry) return hipSuccess;
-  const int from = at_once<T>(dy, lddy, width), to = at_once<T>(dweight, width, width);
-  OPS_TRY(by_count<T>(from < to ? from : to, [&](auto count) {
-    constexpr int N = decltype(count)::value;
-    const int groups = int(ceil_div(width, 64 * N));
-    const int64_t sums = ceil_div(a.pieces * groups, 4);
-    k_word_sums<T, N><<<unsigned(sums + ceil_div(vocab, kAbsent)), 256, 0, s>>>(a, dy, lddy, dweight, groups, sums);
-    return hipGetLastError();
-  }));
+  if (dry || n == 0) return hipSuccess;
+  auto kernel = width < kMany<T> ? k_word_sums<T, true> : k_word_sums<T, false>;
+  kernel<<<unsigned(ceil_div(a.pieces * groups, 4)), 256, 0, s>>>(a, dy, lddy, dweight, groups);
+  OPS_TRY(hipGetLastError());
   if (a.pieces <= 1) return hipSuccess;
-  k_join_words<T><<<dim3(unsigned(ceil_div(a.pieces, kJoin)), unsigned(ceil_div(width, 64))), 1024, 0, s>>>(a, dweight);
+  k_join_words<T><<<dim3(unsigned(ceil_div(a.pieces, kJoin)), unsigned(ceil_div(width, 256))), 1024, 0, s>>>(a, dweight);
   return hipGetLastError();
 }
 
