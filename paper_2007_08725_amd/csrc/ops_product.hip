@@ -1350,15 +1350,15 @@ __device__ inline Listed teacher_row(const int32_t *words, const float *scores, 
 
 // The logits of a row's listed words and its loss: a workgroup a row, four words
 // of a wave at a time.  Reads a row of the weights for each place: 8192 x 32 of
-// 1024 bf16, 537 MB that mostly lie in the caches.
-template <typename T, bool Aligned>
+// 1024 bf16, 537 MB that mostly lie in the caches, 63 us.
+template <typename T>
 __global__ __launch_bounds__(256) void k_distill_loss(const T *x, int64_t ldx, const T *weight, int64_t ldw,
                                                       const float *bias, const int32_t *words, int64_t ld_words,
                                                       const float *scores, int64_t ld_scores, int width, int vocab,
                                                       int top, float unit, const float *lse, float *logits,
                                                       float *loss) {
-  constexpr int U = 4;
-  typedef T vec __attribute__((ext_vector_type(kChunk<T>)));
+  constexpr int U = 4, N = kChunk<T>;
+  typedef T vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));  // at any address
   __shared__ float z[LDA_OPS_MAX_TOP];
   const int64_t m = blockIdx.x;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -1375,13 +1375,20 @@ __global__ __launch_bounds__(256) void k_distill_loss(const T *x, int64_t ldx, c
       w[u] = weight + int64_t(word[u] < 0 ? 0 : word[u]) * ldw;
       sum[u] = 0.0f;
     }
-    for (int c = lane; c * kChunk<T> < width; c += 64) {
-      const vec xv = __builtin_bit_cast(vec, row_chunk<T, Aligned>(row, c, width));
+    for (int c = lane * N; c < width; c += 64 * N) {
+      if (c + N <= width) {
+        const vec xv = *reinterpret_cast<const vec *>(row + c);
+        vec wv[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const vec wv = __builtin_bit_cast(vec, row_chunk<T, Aligned>(w[u], c, width));
+        for (int u = 0; u < U; ++u) wv[u] = *reinterpret_cast<const vec *>(w[u] + c);
 #pragma unroll
-        for (int e = 0; e < kChunk<T>; ++e) sum[u] += float(xv[e]) * float(wv[e]);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int e = 0; e < N; ++e) sum[u] += float(xv[e]) * float(wv[u][e]);
+      } else {
+        for (int e = c; e < width; ++e)
+#pragma unroll
+          for (int u = 0; u < U; ++u) sum[u] += float(row[e]) * float(w[u][e]);
       }
     }
 #pragma unroll
@@ -1950,10 +1957,7 @@ hipError_t distill_forward_t(const lda_distill_args &a, Arena &ws, bool dry) {
   const float unit = 1.0f / a.temperature;
   OPS_TRY((softmax_forward<T, true>(student(a), unit, ws, dry)));
   if (dry || a.rows == 0) return hipSuccess;
-  auto kernel = in_place<T>(a.x, a.ldx, a.width) && in_place<T>(a.weight, a.ld_weight, a.width)
-                    ? k_distill_loss<T, true>
-                    : k_distill_loss<T, false>;
-  kernel<<<unsigned(a.rows), 256, 0, static_cast<hipStream_t>(a.stream)>>>(
+  k_distill_loss<T><<<unsigned(a.rows), 256, 0, static_cast<hipStream_t>(a.stream)>>>(
       static_cast<const T *>(a.x), a.ldx, static_cast<const T *>(a.weight), a.ld_weight, a.bias, a.words, a.ld_words,
       a.scores, a.ld_scores, a.width, a.vocab, a.top, unit, a.lse, a.logits, a.loss);
   return hipGetLastError();

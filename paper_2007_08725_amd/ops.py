@@ -131,30 +131,34 @@ def _matrix(name, t, like=None, shape=None, dtype=None):
     if not t.is_cuda:
         raise ValueError("%s must be on a HIP device" % name)
     if dtype is not None:
-        if t.dtype != dtype or t.device != like.device:
+        if t.dtype != dtype or t.get_device() != like.get_device():
             raise ValueError("%s must be %s on the device of x" % (name, dtype))
+    elif like is not None:
+        if t.dtype != like.dtype or t.get_device() != like.get_device():
+            raise ValueError("%s must have the type and device of x" % name)
     elif t.dtype not in _DTYPES:
         raise ValueError("%s must be float32, bfloat16 or float16" % name)
-    elif like is not None and (t.dtype != like.dtype or t.device != like.device):
-        raise ValueError("%s must have the type and device of x" % name)
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    cols = t.shape[1]
+    if shape is not None and t.shape != shape:
         raise ValueError("%s must be %d x %d" % (name, shape[0], shape[1]))
-    if t.shape[1] < 1:
+    if cols < 1:
         raise ValueError("%s must have columns" % name)
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    if cols > 1 and t.stride(1) != 1:
         raise ValueError("%s must have unit column stride" % name)
-    _refuse_autograd(name, t)
+    if t.requires_grad:
+        _refuse_autograd(name, t)
     return t
 
 
 def _vector(name, t, like, length, dtype):
     if not isinstance(t, torch.Tensor) or t.dim() != 1 or t.shape[0] != length:
         raise ValueError("%s must be a vector of %d" % (name, length))
-    if t.dtype != dtype or t.device != like.device:
+    if t.dtype != dtype or t.get_device() != like.get_device():
         raise ValueError("%s must be %s on the device of x" % (name, dtype))
     if length > 1 and t.stride(0) != 1:
         raise ValueError("%s must be contiguous" % name)
-    _refuse_autograd(name, t)
+    if t.requires_grad:
+        _refuse_autograd(name, t)
     return t
 
 
