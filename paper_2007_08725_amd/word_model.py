@@ -11,7 +11,11 @@ trained on the corpus' tokens with Adam.  Its score is the log-likelihood per
 token in base 2, as ``LDA.loglik`` gives it for the fitted counts, so the two
 stand side by side.  Scoring new words of a document needs no sampling.
 
-    python -m paper_2007_08725_amd.word_model --workload c1 --iters 50 --steps 300
+With ``--reader`` a second model is trained, that needs no topics of a document
+but reads its words in order (``word_reader.py``), from the words alone or, with
+``--distil``, from the fitted topics' most likely words for each document too.
+
+    python -m paper_2007_08725_amd.word_model --workload c1 --iters 50 --steps 300 --reader --distil 0.5
 """
 import argparse
 import json
@@ -36,7 +40,63 @@ def topic_proportions(counts, K: int, alpha: float, device="cuda"):
     return theta * (K / theta.sum(1, keepdim=True))
 
 
-class WordModel:
+def topic_teacher(counts, V: int, K: int, alpha: float, beta: float, top: int = 32, device="cuda"):
+    """The fitted topics' most likely words of every document and their log-probabilities: int32 and float32 [M, top].
+
+    p(v | d) = sum_k theta_dk phi_kv with theta as ``topic_proportions`` and phi_kv = (W[v][k] + beta) / (T[k] + V beta).
+    """
+    off, total = np.asarray(counts["W_off"]), np.asarray(counts["T"], np.float64)
+    rows = torch.from_numpy(np.repeat(np.arange(V), np.diff(off))).to(device)
+    phi = torch.full((V, K), float(beta), device=device)
+    entries = torch.from_numpy(np.asarray(counts["W_topic"], np.int64)).to(device)
+    phi[rows, entries] += torch.from_numpy(np.asarray(counts["W_count"], np.float32)).to(device)
+    phi /= torch.from_numpy(total + V * beta).to(device=device, dtype=torch.float32)
+    theta = topic_proportions(counts, K, alpha, device) / K
+    words, scores = [], []
+    for i in range(0, theta.shape[0], 1024):
+        p, v = torch.topk(theta[i:i + 1024] @ phi.t(), top)
+        words.append(v.to(torch.int32))
+        scores.append(torch.log(p))
+    return torch.cat(words), torch.cat(scores)
+
+
+class Trained:
+    """Parameters in float32 under ``params``, their Adam averages, and the type that products run in."""
+
+    def _start(self, params, dtype):
+        self.params, self.dtype = params, dtype
+        # half precision takes the gradients of this many times the mean loss: those of the mean over a batch of
+        # thousands are below its normal numbers
+        self._loss_scale = 1024.0 if dtype == torch.float16 else 1.0
+        self._moments = {n: (torch.zeros_like(p), torch.zeros_like(p)) for n, p in params.items()}
+        self._steps = 0
+
+    def _cast(self):
+        # the softmax's bias stays in float32
+        return {n: p if n == "bias" else p.to(self.dtype) for n, p in self.params.items()}
+
+    def _adam(self, grads, lr: float):
+        """One Adam step with gradients of ``_loss_scale`` times the loss."""
+        self._steps += 1
+        c1, c2 = 1 - 0.9 ** self._steps, 1 - 0.999 ** self._steps
+        for name, param in self.params.items():
+            g = grads[name].float()
+            if self._loss_scale != 1.0:
+                g = g / self._loss_scale
+            m, v = self._moments[name]
+            m.mul_(0.9).add_(g, alpha=0.1)
+            v.mul_(0.999).addcmul_(g, g, value=0.001)
+            param.addcdiv_(m / c1, (v / c2).sqrt_().add_(1e-8), value=-lr)
+
+
+def word_bias(word_counts, V: int, device):
+    """The logarithm of the words' frequencies, from which the softmax's bias starts."""
+    freq = torch.ones(V, device=device) if word_counts is None else torch.as_tensor(
+        np.asarray(word_counts), device=device).float() + 0.5
+    return torch.log(freq / freq.sum())
+
+
+class WordModel(Trained):
     """The model's parameters (float32) and their training; products run in ``dtype``."""
 
     def __init__(self, K: int, V: int, hidden: int = 256, act: str = "silu", dtype=torch.bfloat16, word_counts=None,
@@ -46,22 +106,11 @@ class WordModel:
         def normal(*shape, scale):
             return torch.randn(*shape, generator=gen, device=device) * scale
 
-        self.act, self.dtype = act, dtype
-        # the bias starts as the logarithm of the words' frequencies
-        freq = torch.ones(V, device=device) if word_counts is None else torch.as_tensor(
-            np.asarray(word_counts), device=device).float() + 0.5
-        self.params = dict(norm_weight=torch.ones(K, device=device), norm_bias=torch.zeros(K, device=device),
-                           w_gate=normal(hidden, K, scale=K ** -0.5), w_value=normal(hidden, K, scale=K ** -0.5),
-                           weight=normal(V, hidden, scale=0.1 * hidden ** -0.5), bias=torch.log(freq / freq.sum()))
-        # half precision takes the gradients of this many times the mean loss: those of the mean over a batch of
-        # thousands are below its normal numbers
-        self._loss_scale = 1024.0 if dtype == torch.float16 else 1.0
-        self._moments = {n: (torch.zeros_like(p), torch.zeros_like(p)) for n, p in self.params.items()}
-        self._steps = 0
-
-    def _cast(self):
-        # the softmax's bias stays in float32
-        return {n: p if n == "bias" else p.to(self.dtype) for n, p in self.params.items()}
+        self.act = act
+        self._start(dict(norm_weight=torch.ones(K, device=device), norm_bias=torch.zeros(K, device=device),
+                         w_gate=normal(hidden, K, scale=K ** -0.5), w_value=normal(hidden, K, scale=K ** -0.5),
+                         weight=normal(V, hidden, scale=0.1 * hidden ** -0.5),
+                         bias=word_bias(word_counts, V, device)), dtype)
 
     def loss(self, theta, words):
         """Negative log-likelihood of each word (natural log), and what the backward pass takes."""
@@ -85,16 +134,7 @@ class WordModel:
         """One Adam step on a batch of tokens; returns the batch's mean loss, on the device."""
         loss, kept = self.loss(theta, words)
         grads = self.gradients(kept, torch.full_like(loss, self._loss_scale / loss.shape[0]))
-        self._steps += 1
-        c1, c2 = 1 - 0.9 ** self._steps, 1 - 0.999 ** self._steps
-        for name, param in self.params.items():
-            g = grads[name].float()
-            if self._loss_scale != 1.0:
-                g = g / self._loss_scale
-            m, v = self._moments[name]
-            m.mul_(0.9).add_(g, alpha=0.1)
-            v.mul_(0.999).addcmul_(g, g, value=0.001)
-            param.addcdiv_(m / c1, (v / c2).sqrt_().add_(1e-8), value=-lr)
+        self._adam(grads, lr)
         return loss.mean()
 
     def llpt(self, proportions, word, doc, batch: int = 8192):
@@ -125,6 +165,10 @@ def main(argv=None):
     ap.add_argument("--batch", type=int, default=4096)
     ap.add_argument("--hidden", type=int, default=256)
     ap.add_argument("--lr", type=float, default=1e-2)
+    ap.add_argument("--reader", action="store_true", help="train a reader of the words in order too")
+    ap.add_argument("--distil", type=float, default=0.0, help="the fitted topics' part of the reader's loss, 0 to 1")
+    ap.add_argument("--top", type=int, default=32, help="words that the fitted topics list for a document")
+    ap.add_argument("--temperature", type=float, default=1.0)
     ap.add_argument("--eval-tokens", type=int, default=1 << 20, help="tokens scored at the end, from the corpus' start")
     args = ap.parse_args(argv)
 
@@ -137,7 +181,7 @@ def main(argv=None):
     with LDA(c.word, c.doc, c.V, c.K, c.alpha, c.beta, lda_synth.SAMPLER_SEED) as m:
         m.iterate(args.iters)
         fitted = m.loglik()
-        counts = m.counts(z=False, W=False)
+        counts = m.counts(z=False, W=args.reader)
     proportions = topic_proportions(counts, c.K, c.alpha)
     word = torch.from_numpy(c.word).cuda()
     doc = torch.from_numpy(c.doc).long().cuda()
@@ -149,11 +193,15 @@ def main(argv=None):
     t0 = time.perf_counter()
     losses = train(model, proportions, word, doc, args.steps, args.batch, args.lr)
     elapsed = time.perf_counter() - t0
-    print(json.dumps(dict(workload=args.workload, tokens=c.N, V=c.V, K=c.K, llpt_fitted_topics=fitted,
-                          llpt_word_model_before=before,
-                          llpt_word_model=model.llpt(proportions, word[some], doc[some]),
-                          first_loss=losses[0] if losses else None, last_loss=losses[-1] if losses else None,
-                          ms_per_step=elapsed * 1e3 / max(1, args.steps))))
+    said = dict(workload=args.workload, tokens=c.N, V=c.V, K=c.K, llpt_fitted_topics=fitted,
+                llpt_word_model_before=before, llpt_word_model=model.llpt(proportions, word[some], doc[some]),
+                first_loss=losses[0] if losses else None, last_loss=losses[-1] if losses else None,
+                ms_per_step=elapsed * 1e3 / max(1, args.steps))
+    if args.reader:
+        from . import word_reader
+        said.update(word_reader.fit(c, args, freq, topic_teacher(counts, c.V, c.K, c.alpha, c.beta, args.top)
+                                    if args.distil > 0 else None))
+    print(json.dumps(said))
     return 0
 
 
