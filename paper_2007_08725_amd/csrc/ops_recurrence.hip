@@ -64,10 +64,10 @@ __device__ inline void gate(float g, float &f, float &k) {
   open(gate_of<T>(g), f, k);
 }
 
-// N columns of a lane, side by side; N > 1 are moved as 32 bits.
+// N columns of a lane, side by side, moved at once from wherever they begin.
 template <typename T, int N>
 struct Raw {
-  typedef T vec __attribute__((ext_vector_type(N)));
+  typedef T vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
   vec v;
   __device__ float operator[](int e) const { return float(v[e]); }
 };
@@ -101,6 +101,15 @@ __device__ inline void anew(Raw<T, N> &x) {
     asm volatile("" : "+v"(bits));
     x = __builtin_bit_cast(Raw<T, N>, bits);
   }
+}
+
+// A lane's first column.  The last lane of an odd row has the last N, one of which
+// its neighbour has too: both compute and store the same.  Lanes past the end have
+// the first ones, and store nothing.
+template <int N>
+__device__ inline int column_of(int group, int lane, int cols) {
+  const int c = (group * 64 + lane) * N;
+  return c < cols ? min(c, cols - N) : 0;
 }
 
 // ------------------------------------------------------------- documents -----
@@ -413,19 +422,21 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
   __shared__ Shared<N> s;
   const int t = take_ticket(s, p.chain), block = t / p.groups;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = (t % p.groups * 64 + lane) * N;
-  const bool in = c < p.cols;
-  const int at = in ? c : 0;
+  const bool in = (t % p.groups * 64 + lane) * N < p.cols;
+  const int c = column_of<N>(t % p.groups, lane, p.cols);
   const int row0 = block * R * kWaves + wave * R;
   // rows past the end repeat the last one; what they are says that they are of no document
   const int mine = lane < R && row0 + lane < p.rows ? p.info[row0 + lane] : -1;
   const int begins = p.info[block * R * kWaves];
   Raw<T, N> x[R], g[R];
+  const int last_row = p.rows - 1;
+  const T *px = p.x + int64_t(min(row0, last_row)) * p.ldx, *pg = p.gate + int64_t(min(row0, last_row)) * p.ld_gate;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int64_t row = min(row0 + r, p.rows - 1);
-    x[r] = load_raw<T, N>(p.x + row * p.ldx + at);
-    g[r] = load_raw<T, N>(p.gate + row * p.ld_gate + at);
+    x[r] = load_raw<T, N>(px + c);
+    g[r] = load_raw<T, N>(pg + c);
+    px += row0 + r < last_row ? p.ldx : 0;
+    pg += row0 + r < last_row ? p.ld_gate : 0;
   }
   float f[R][N], b[R][N];
   float a[N], sum[N];
@@ -445,7 +456,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
       b[r][e] = keep * x[r][e];
     }
     if (special.first(r) && p.state) {
-      const float *state = p.state + int64_t(__builtin_amdgcn_readlane(mine, r) >> 2) * p.cols + at;
+      const float *state = p.state + int64_t(__builtin_amdgcn_readlane(mine, r) >> 2) * p.cols + c;
 #pragma unroll
       for (int e = 0; e < N; ++e) b[r][e] = __builtin_fmaf(f[r][e], state[e], b[r][e]);
     }
@@ -460,15 +471,16 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
   float m[N];
   state_in<N>(s, p.chain, block, wave, !row_cuts(begins), c, in, a, sum, special.cuts != 0, m);
   if (!in || row0 >= p.rows) return;
+  T *h = p.h + int64_t(row0) * p.ldh;
+  float *kept = p.kept + int64_t(row0 / kKept) * p.cols;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    if (row0 + r >= p.rows) break;
-    if (r % kKept == 0)
-#pragma unroll
-      for (int e = 0; e < N; ++e) p.kept[int64_t((row0 + r) / kKept) * p.cols + c + e] = m[e];
+    if (row0 + r >= p.rows) continue;
+    if (r % kKept == 0) store_raw<float, N>(kept + int64_t(r / kKept) * p.cols + c, m);
 #pragma unroll
     for (int e = 0; e < N; ++e) m[e] = __builtin_fmaf(f[r][e], special.cut(r) ? 0.0f : m[e], b[r][e]);
-    store_raw<T, N>(p.h + int64_t(row0 + r) * p.ldh + c, m);
+    store_raw<T, N>(h + c, m);
+    h += p.ldh;
     if (special.last(r)) {
       float *last = p.last + int64_t(__builtin_amdgcn_readlane(mine, r) >> 2) * p.cols + c;
 #pragma unroll
@@ -499,28 +511,32 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
   __shared__ Shared<N> s;
   const int t = take_ticket(s, p.chain), back = t / p.groups, block = p.blocks - 1 - back;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = (t % p.groups * 64 + lane) * N;
-  const bool in = c < p.cols;
-  const int at = in ? c : 0;
+  const bool in = (t % p.groups * 64 + lane) * N < p.cols;
+  const int c = column_of<N>(t % p.groups, lane, p.cols);
   const int row0 = block * R * kWaves + wave * R;
   const int mine = lane < R && row0 + lane < p.rows ? p.info[row0 + lane] : -1;
   // whether the row after the workgroup's last one passes anything on
   const int after = (block + 1) * R * kWaves;
   const int follows = after < p.rows ? p.info[after] : -1;
   Raw<T, N> x[R], g[R], d[R];
+  const int last_row = p.rows - 1;
+  const T *px = p.x + int64_t(min(row0, last_row)) * p.ldx, *pg = p.gate + int64_t(min(row0, last_row)) * p.ld_gate;
+  const T *pd = p.dh + int64_t(min(row0, last_row)) * p.lddh;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int64_t row = min(row0 + r, p.rows - 1);
-    x[r] = load_raw<T, N>(p.x + row * p.ldx + at);
-    g[r] = load_raw<T, N>(p.gate + row * p.ld_gate + at);
-    d[r] = load_raw<T, N>(p.dh + row * p.lddh + at);
+    x[r] = load_raw<T, N>(px + c);
+    g[r] = load_raw<T, N>(pg + c);
+    d[r] = load_raw<T, N>(pd + c);
+    px += row0 + r < last_row ? p.ldx : 0;
+    pg += row0 + r < last_row ? p.ld_gate : 0;
+    pd += row0 + r < last_row ? p.lddh : 0;
   }
   // the rows' gates, and what a row's gradient is multiplied by for dgate; their maps from the first row on
   float z[R][N], w[R][N], h[N], a[N], sum[N];
   const int64_t kept_row = row0 < p.rows ? row0 / kKept : 0;
 #pragma unroll
   for (int e = 0; e < N; ++e) {
-    h[e] = p.kept[kept_row * p.cols + at + e];
+    h[e] = p.kept[kept_row * p.cols + c + e];
     a[e] = 1.0f;
     sum[e] = 0.0f;
   }
@@ -530,7 +546,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
   float more[N];
 #pragma unroll
   for (int e = 0; e < N; ++e)
-    more[e] = last < 0 ? 0.0f : p.dlast[int64_t(__builtin_amdgcn_readlane(mine, last) >> 2) * p.cols + at + e];
+    more[e] = last < 0 ? 0.0f : p.dlast[int64_t(__builtin_amdgcn_readlane(mine, last) >> 2) * p.cols + c + e];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     if (special.cut(r)) {
@@ -539,7 +555,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
       if (special.first(r) && p.state)
 #pragma unroll
         for (int e = 0; e < N; ++e)
-          h[e] = p.state[int64_t(__builtin_amdgcn_readlane(mine, r) >> 2) * p.cols + at + e];
+          h[e] = p.state[int64_t(__builtin_amdgcn_readlane(mine, r) >> 2) * p.cols + c + e];
     }
     const bool cut = special.cuts << (63 - r);  // this row or one before it: its part goes to no row before them
 #pragma unroll
@@ -559,8 +575,11 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
   float m[N];
   state_in<N>(s, p.chain, back, order, !row_cuts(follows), c, in, a, sum, special.cuts != 0, m);
   if (!in || row0 >= p.rows) return;
+  T *dx_row = p.dx + int64_t(row0 + R) * p.lddx, *dg_row = p.dgate + int64_t(row0 + R) * p.ld_dgate;
 #pragma unroll
   for (int r = R - 1; r >= 0; --r) {
+    dx_row -= p.lddx;
+    dg_row -= p.ld_dgate;
     if (row0 + r >= p.rows) continue;
     const int64_t doc = __builtin_amdgcn_readlane(mine, r) >> 2;
     float dx[N], dg[N];
@@ -580,8 +599,8 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
       dg[e] = out ? 0.0f : w[r][e] * grad;
       m[e] = f * grad;
     }
-    store_raw<T, N>(p.dx + int64_t(row0 + r) * p.lddx + c, dx);
-    store_raw<T, N>(p.dgate + int64_t(row0 + r) * p.ld_dgate + c, dg);
+    store_raw<T, N>(dx_row + c, dx);
+    store_raw<T, N>(dg_row + c, dg);
     if (special.first(r) && p.dstate)
 #pragma unroll
       for (int e = 0; e < N; ++e) p.dstate[doc * p.cols + c + e] = m[e];
@@ -591,11 +610,13 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
 }
 
 // ------------------------------------------------------------------ step -----
+// N columns a lane, of which a row is a multiple: the new state may take the place
+// of the old one, so no column is computed twice.
 template <typename T, int N>
 __global__ __launch_bounds__(256) void k_recur_step(const T *x, int64_t ldx, const T *gates, int64_t ldg,
                                                     const float *state, int64_t rows, int cols, T *h, int64_t ldh,
                                                     float *last) {
-  const int each = (cols + N - 1) / N;
+  const int each = cols / N;
   const int64_t all = rows * each, step = int64_t(gridDim.x) * 256;
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += step) {
     const int64_t row = all <= 0xffffffffll ? uint32_t(i) / uint32_t(each) : i / each;
@@ -615,12 +636,6 @@ __global__ __launch_bounds__(256) void k_recur_step(const T *x, int64_t ldx, con
 }
 
 // ------------------------------------------------------------------ host -----
-// Whether n columns can be moved at once.
-template <typename T>
-bool by(int n, const void *p, int64_t ld, int64_t cols) {
-  return reinterpret_cast<uintptr_t>(p) % (n * sizeof(T)) == 0 && ld % n == 0 && cols % n == 0;
-}
-
 // The scratch of a scan over `rows`, and what finds the rows' documents.
 struct Scan {
   int blocks, groups;
@@ -682,11 +697,11 @@ hipError_t backward_n(const lda_recur_args &a, Arena &ws, bool dry) {
   return hipGetLastError();
 }
 
+// 16-bit columns in pairs, 32 bits a lane as in single precision.
 template <typename T>
 hipError_t forward_t(const lda_recur_args &a, Arena &ws, bool dry) {
   if constexpr (sizeof(T) == 2) {
-    if (by<T>(2, a.x, a.ldx, a.cols) && by<T>(2, a.gate, a.ld_gate, a.cols) && by<T>(2, a.h, a.ldh, a.cols))
-      return forward_n<T, 2>(a, ws, dry);
+    if (a.cols > 1) return forward_n<T, 2>(a, ws, dry);
   }
   return forward_n<T, 1>(a, ws, dry);
 }
@@ -694,9 +709,7 @@ hipError_t forward_t(const lda_recur_args &a, Arena &ws, bool dry) {
 template <typename T>
 hipError_t backward_t(const lda_recur_args &a, Arena &ws, bool dry) {
   if constexpr (sizeof(T) == 2) {
-    if (by<T>(2, a.x, a.ldx, a.cols) && by<T>(2, a.gate, a.ld_gate, a.cols) && by<T>(2, a.dh, a.lddh, a.cols) &&
-        by<T>(2, a.dx, a.lddx, a.cols) && by<T>(2, a.dgate, a.ld_dgate, a.cols))
-      return backward_n<T, 2>(a, ws, dry);
+    if (a.cols > 1) return backward_n<T, 2>(a, ws, dry);
   }
   return backward_n<T, 1>(a, ws, dry);
 }
@@ -707,8 +720,7 @@ hipError_t step_t(const lda_recur_args &a) {
   const auto s = static_cast<hipStream_t>(a.stream);
   const T *x = static_cast<const T *>(a.x), *g = static_cast<const T *>(a.gate);
   T *h = static_cast<T *>(a.h);
-  const bool wide = by<T>(4, x, a.ldx, a.cols) && by<T>(4, g, a.ld_gate, a.cols) && by<T>(4, h, a.ldh, a.cols) &&
-                    by<float>(4, a.state, a.cols, a.cols) && by<float>(4, a.last, a.cols, a.cols);
+  const bool wide = a.cols % 4 == 0;
   const int64_t needed = ceil_div(a.rows * (wide ? a.cols / 4 : a.cols), 256);
   const unsigned blocks = unsigned(needed < 65536 ? needed : 65536);
   auto kernel = wide ? k_recur_step<T, 4> : k_recur_step<T, 1>;

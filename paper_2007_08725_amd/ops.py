@@ -393,6 +393,8 @@ def recurrence_step(x, gate, state, out=None):
         out = torch.empty(rows, cols, dtype=torch.float32, device=x.device)
     else:
         _state("out", out, x, rows, cols)
+        if 0 < abs(out.data_ptr() - state.data_ptr()) < 4 * rows * cols:
+            raise ValueError("out must be state or apart from it")
     h = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
     a = RecurArgs(dtype=_DTYPES[x.dtype], rows=rows, cols=cols, docs=rows, x=x.data_ptr(), ldx=x.stride(0),
                   gate=gate.data_ptr(), ld_gate=gate.stride(0), state=state.data_ptr(), h=h.data_ptr(), ldh=cols,

@@ -108,6 +108,23 @@ def test_embedding_large_vocabulary(ops):  # noqa: F811
     assert torch.equal(dw[:, 0], torch.bincount(words[kept].long(), minlength=vocab).float())
 
 
+def test_embedding_far_offsets(ops):  # noqa: F811
+    """Elements beyond 2^32 of y, of dy and of the gradient."""
+    rows, width, vocab = 4300000, 1024, 4300000
+    words = torch.arange(rows, dtype=torch.int32, device="cuda").flip(0)
+    words[5] = vocab - 7  # twice, the word 4299994 not at all
+    weight = torch.zeros(vocab, width, dtype=torch.bfloat16, device="cuda")
+    weight[:] = torch.arange(vocab, device="cuda")[:, None] % 251
+    y = ops.embedding(words, weight, 2.0)
+    want = (words.long() % 251 * 2).to(torch.bfloat16)
+    assert bool((y == want[:, None]).all())
+    del weight
+    dw = ops.embedding_backward(y, words, vocab, 0.5)
+    del y
+    sums = torch.zeros(vocab, device="cuda").index_add_(0, words.long(), want.float()) * 0.5
+    assert bool((dw == sums.to(torch.bfloat16)[:, None]).all())
+
+
 def test_embedding_empty(ops):  # noqa: F811
     words = torch.empty(0, dtype=torch.int32, device="cuda")
     weight = rand(1, 70, 24, dtype=torch.bfloat16)

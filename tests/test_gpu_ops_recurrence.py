@@ -118,6 +118,34 @@ def test_recurrence_widths_and_strides(ops, dtype, cols, pad, offset):  # noqa: 
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [1, 2, 3, 5001])
+def test_recurrence_narrow_and_wide(ops, dtype, cols):  # noqa: F811
+    case(ops, dtype, 50, cols, offsets_of([3, 47]), True)
+    case(ops, dtype, 50, cols, offsets_of([50]), False, pad=1, offset=1)
+
+
+def test_recurrence_far_offsets(ops):  # noqa: F811
+    """Elements beyond 2^32 of their matrices: the last documents as they are by themselves."""
+    rows, cols = 4300000, 1024
+    tail = 3000
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    gate = torch.ones(1, cols, dtype=torch.bfloat16, device="cuda").expand(rows, cols)
+    x[-tail:] = rand(1, tail, cols, dtype=torch.bfloat16)
+    off = torch.tensor([0, rows - tail, rows - tail + 1000, rows], device="cuda")
+    h, last, kept = ops.recurrence(x, gate, off)
+    alone, alone_last, alone_kept = ops.recurrence(x[-tail:], gate[:tail], off[1:] - off[1])
+    assert not bool(h[:-tail].any())
+    # one rounding to bf16, on either side of a border, of states that are some 100 roundings of 32 bits apart
+    assert bool(((h[-tail:] - alone).float().abs() <= 2 * 2.0 ** -8 * alone.float().abs() + 1e-5).all())
+    assert torch.allclose(last[1:], alone_last, rtol=0, atol=1e-4 * float(alone_last.abs().max()))
+    dx, dgate, _ = ops.recurrence_backward(x, x, gate, off, kept)
+    adx, adgate, _ = ops.recurrence_backward(x[-tail:], x[-tail:], gate[:tail], off[1:] - off[1], alone_kept)
+    for a, b in ((dx, adx), (dgate, adgate)):
+        assert not bool(a[:-tail].any())
+        assert bool(((a[-tail:] - b).float().abs() <= 2 * 2.0 ** -8 * b.float().abs() + 1e-4).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_recurrence_rows_of_no_document(ops, dtype):  # noqa: F811
     """Rows before the first document and behind the last one, and offsets that lie outside the rows."""
     case(ops, dtype, 400, 40, offsets_of([60, 0, 200], 50), True)
@@ -308,7 +336,7 @@ def test_recurrence_joint_matrix_and_broadcast(ops):  # noqa: F811
 
 def test_recurrence_refusals(ops):  # noqa: F811
     x, gate, state, dh, dlast = inputs(torch.float32, 10, 8, 2, True)
-    off = offsets_of([4, 6])
+    off, two = offsets_of([4, 6]), rand(6, 3, 8)
     _, _, kept = ops.recurrence(x, gate, off, state)
     bad = [lambda: ops.recurrence(x.cpu(), gate, off), lambda: ops.recurrence(x, gate[:5], off),
            lambda: ops.recurrence(x, gate.half(), off), lambda: ops.recurrence(x, gate, off.int()),
@@ -324,7 +352,8 @@ def test_recurrence_refusals(ops):  # noqa: F811
            lambda: ops.recurrence_backward(dh, x, gate, off, kept, state, dlast[:1]),
            lambda: ops.recurrence_step(x, gate, state), lambda: ops.recurrence_step(x[:2], gate[:2], state.half()),
            lambda: ops.recurrence_step(x[:2], gate[:2], state, out=state[:1]),
-           lambda: ops.recurrence_step(x[:2], gate[:2], state, out=state.double())]
+           lambda: ops.recurrence_step(x[:2], gate[:2], state, out=state.double()),
+           lambda: ops.recurrence_step(x[:2], gate[:2], two[:2], out=two[1:])]
     for i, call in enumerate(bad):
         with pytest.raises(ValueError):
             call()
