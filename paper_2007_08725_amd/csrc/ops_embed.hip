@@ -157,7 +157,8 @@ __device__ inline uint32_t rank_in_wave(uint32_t digit, int bits, bool in, int l
 
 // Up to kSmall places in one workgroup, which has them in its registers and moves
 // them through LDS, a radix sort from the lowest 6 bits on: 8192 words of a
-// vocabulary of 102000 (three passes) SMALL_US us.
+// vocabulary of 102000 (three passes) 24 us,
+// 4096 of one of 2000 (two) 11; a bitonic network took 75 and 37.
 constexpr int kSmall = 8192, kSmallBits = 6;
 __global__ __launch_bounds__(1024) void k_sort_small(const int32_t *words, int n, int passes, uint32_t vocab,
                                                      uint32_t *keys, uint32_t *places, const Fill fill) {
@@ -228,8 +229,9 @@ __global__ __launch_bounds__(1024) void k_sort_small(const int32_t *words, int n
 // More: a radix sort from the lowest digit of up to kDigitBits bits on, three
 // launches a digit: counts of each tile, their sums before each tile, and the
 // tile's places moved to where they belong, in their order.
-constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits, kTile = 1024;
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 
+constexpr int kTile = 1024;
 struct SortPass {
   const int32_t *words;  // of the first pass: keys from the words, places 0, 1, ..
   const uint32_t *keys, *places;
@@ -237,8 +239,11 @@ struct SortPass {
   int64_t n;
   uint32_t vocab;
   int shift, bits;
+  // places of a tile, a multiple of 256: few where there are few places, so that they spread over the CUs (16384: 256
+  // instead of 1024 49 us for both passes instead of 56), up to kTile (1048576 with 512: 614 us, with 1024 601)
+  int tile;
   int64_t tiles;
-  uint32_t *counts;  // [digits][tiles], then the digits' totals
+  uint32_t *counts;  // [tiles][digits], then the digits' totals
   __device__ uint32_t key(int64_t i) const { return words ? key_of(words[i], vocab) : keys[i]; }
   __device__ uint32_t digit(uint32_t key) const { return key >> shift & ((1u << bits) - 1); }
 };
@@ -252,11 +257,11 @@ __global__ __launch_bounds__(256) void k_sort_count(const SortPass p, const Fill
   const int digits = 1 << p.bits;
   for (int d = threadIdx.x; d < digits; d += 256) count[d] = 0;
   __syncthreads();
-  const int64_t first = int64_t(blockIdx.x) * kTile;
-  for (int i = threadIdx.x; i < kTile; i += 256)
+  const int64_t first = int64_t(blockIdx.x) * p.tile;
+  for (int i = threadIdx.x; i < p.tile; i += 256)
     if (first + i < p.n) atomicAdd(&count[p.digit(p.key(first + i))], 1u);
   __syncthreads();
-  for (int d = threadIdx.x; d < digits; d += 256) p.counts[d * p.tiles + blockIdx.x] = count[d];
+  for (int d = threadIdx.x; d < digits; d += 256) p.counts[int64_t(blockIdx.x) * digits + d] = count[d];
 }
 
 // The sum of the values of the threads before this one; `total` of all 256.
@@ -281,23 +286,52 @@ __device__ inline uint32_t sum_before(uint32_t v, uint32_t &total, uint32_t (&sh
   return before;
 }
 
-// A digit's counts become the sums of the tiles before; one workgroup a digit.
-__global__ __launch_bounds__(256) void k_sort_sums(const SortPass p, const Fill fill) {
-  __shared__ uint32_t shared[4];
-  if (blockIdx.x >= 1u << p.bits) {
-    fill_zero(fill, int64_t(blockIdx.x) - (int64_t(1) << p.bits));
+// The digits' counts become the sums of the tiles before.  A workgroup takes
+// kSide digits (64 bytes of a tile's counts), and kLong tiles at a time in
+// kLong / kDeep threads a digit, each with kDeep neighbouring tiles.
+constexpr int kSide = 16, kDeep = 16, kLong = 1024 / kSide * kDeep;
+__global__ __launch_bounds__(1024) void k_sort_sums(const SortPass p, const Fill fill) {
+  __shared__ uint32_t shared[16][kSide];
+  const int digits = 1 << p.bits, groups = (digits + kSide - 1) / kSide;
+  if (int(blockIdx.x) >= groups) {
+    fill_zero(fill, int64_t(blockIdx.x) - groups);
     return;
   }
-  uint32_t *row = p.counts + int64_t(blockIdx.x) * p.tiles, carry = 0;
-  for (int64_t t0 = 0; t0 < p.tiles; t0 += 256) {
-    const int64_t t = t0 + threadIdx.x;
-    const uint32_t v = t < p.tiles ? row[t] : 0;
-    uint32_t total;
-    const uint32_t before = sum_before(v, total, shared);
-    if (t < p.tiles) row[t] = carry + before;
-    carry += total;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int d = int(blockIdx.x) * kSide + (lane & (kSide - 1)), row = int(threadIdx.x) / kSide;
+  const bool in = d < digits;
+  uint32_t carry = 0;
+  for (int64_t t0 = 0; t0 < p.tiles; t0 += kLong) {
+    const int64_t first = t0 + row * kDeep;
+    uint32_t v[kDeep], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) v[i] = in && first + i < p.tiles ? p.counts[(first + i) * digits + d] : 0;
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) sum += v[i];
+    // over the wave's four rows, then over the waves
+    uint32_t upto = sum;
+#pragma unroll
+    for (int x = kSide; x < 64; x <<= 1) {
+      const uint32_t other = __shfl_up(upto, x);
+      if (lane >= x) upto += other;
+    }
+    __syncthreads();
+    if (lane >= 64 - kSide) shared[wave][lane & (kSide - 1)] = upto;
+    __syncthreads();
+    uint32_t before = carry + upto - sum;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      const uint32_t all = shared[w][lane & (kSide - 1)];
+      if (w < wave) before += all;
+      carry += all;
+    }
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) {
+      if (in && first + i < p.tiles) p.counts[(first + i) * digits + d] = before;
+      before += v[i];
+    }
   }
-  if (threadIdx.x == 0) p.counts[(int64_t(1) << p.bits) * p.tiles + blockIdx.x] = carry;
+  if (row == 0 && in) p.counts[p.tiles * digits + d] = carry;
 }
 
 // Each wave takes a quarter of the tile, 64 places at a time.
@@ -311,28 +345,30 @@ __global__ __launch_bounds__(256) void k_sort_place(const SortPass p, const Fill
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, digits = 1 << p.bits;
   for (int d = threadIdx.x; d < 4 * digits; d += 256) count[d / digits][d % digits] = 0;
   __syncthreads();
-  const int64_t first = int64_t(blockIdx.x) * kTile + wave * (kTile / 4) + lane;
+  const int64_t first = int64_t(blockIdx.x) * p.tile + wave * (p.tile / 4) + lane;
+  const int64_t end = min(p.n, first - lane + p.tile / 4);
   uint32_t key[ROUNDS], place[ROUNDS], rank[ROUNDS];
 #pragma unroll
   for (int r = 0; r < ROUNDS; ++r) {
     const int64_t i = first + r * 64;
-    key[r] = i < p.n ? p.key(i) : 0;
-    place[r] = i < p.n ? (p.words ? uint32_t(i) : p.places[i]) : 0;
+    key[r] = i < end ? p.key(i) : 0;
+    place[r] = i < end ? (p.words ? uint32_t(i) : p.places[i]) : 0;
   }
 #pragma unroll
   for (int r = 0; r < ROUNDS; ++r) {
-    rank[r] = rank_in_wave(p.digit(key[r]), p.bits, first + r * 64 < p.n, lane, count[wave]);
+    if (r * 256 >= p.tile) break;
+    rank[r] = rank_in_wave(p.digit(key[r]), p.bits, first + r * 64 < end, lane, count[wave]);
   }
   __syncthreads();
   // counts of the waves become the first place of each one's digit
-  const uint32_t *totals = p.counts + int64_t(digits) * p.tiles;
+  const uint32_t *totals = p.counts + int64_t(digits) * p.tiles, *mine = p.counts + int64_t(blockIdx.x) * digits;
   uint32_t carry = 0;
   for (int d0 = 0; d0 < digits; d0 += 256) {
     const int d = d0 + int(threadIdx.x);
     uint32_t total;
     const uint32_t before = sum_before(d < digits ? totals[d] : 0, total, shared);
     if (d < digits) {
-      uint32_t at = carry + before + p.counts[d * p.tiles + blockIdx.x];
+      uint32_t at = carry + before + mine[d];
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const uint32_t c = count[w][d];
@@ -345,7 +381,7 @@ __global__ __launch_bounds__(256) void k_sort_place(const SortPass p, const Fill
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < ROUNDS; ++r)
-    if (first + r * 64 < p.n) {
+    if (first + r * 64 < end) {
       const uint32_t to = count[wave][p.digit(key[r])] + rank[r];
       p.keys_out[to] = key[r];
       p.places_out[to] = place[r];
@@ -585,7 +621,8 @@ hipError_t sort_words(const int32_t *words, int64_t n, int vocab, Fill fill, Are
   p.n = n;
   p.vocab = uint32_t(vocab);
   p.bits = each;
-  p.tiles = ceil_div(n, kTile);
+  p.tile = n < int64_t(1) << 17 ? kTile / 4 : n < int64_t(1) << 19 ? kTile / 2 : kTile;
+  p.tiles = ceil_div(n, p.tile);
   p.counts = ws.take<uint32_t>((p.tiles + 1) << each);
   int launches = 3 * passes;
   for (int i = 0; i < passes; ++i) {
@@ -601,7 +638,7 @@ hipError_t sort_words(const int32_t *words, int64_t n, int vocab, Fill fill, Are
     k_sort_count<<<unsigned(p.tiles + fill_parts(part)), 256, 0, s>>>(p, part);
     OPS_TRY(hipGetLastError());
     part = share(fill, launches--);
-    k_sort_sums<<<unsigned((int64_t(1) << each) + fill_parts(part)), 256, 0, s>>>(p, part);
+    k_sort_sums<<<unsigned(ceil_div(int64_t(1) << each, kSide) + fill_parts(part)), 1024, 0, s>>>(p, part);
     OPS_TRY(hipGetLastError());
     part = share(fill, launches--);
     k_sort_place<<<unsigned(p.tiles + fill_parts(part)), 256, 0, s>>>(p, part);
