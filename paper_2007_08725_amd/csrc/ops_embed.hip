@@ -576,7 +576,7 @@ hipError_t embed_forward_t(const lda_embed_args &a) {
     if (padded == int64_t(kMany<T>) << i) break;
   }
   const int64_t each = int64_t(256 >> shift) * 4;
-  const bool past = a.rows * a.width * int64_t(sizeof(T)) > int64_t(256) << 20;
+  const bool past = a.rows * a.width * int64_t(sizeof(T)) >= int64_t(256) << 20;
   auto kernel = a.width < kMany<T> ? k_embed<T, true, false> : past ? k_embed<T, false, true> : k_embed<T, false, false>;
   kernel<<<unsigned(ceil_div(a.rows, each)), 256, 0, static_cast<hipStream_t>(a.stream)>>>(
       a.words, a.rows, static_cast<const T *>(a.weight), a.ld_weight, a.width, a.vocab, a.scale, shift,

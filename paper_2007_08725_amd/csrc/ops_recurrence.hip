@@ -29,12 +29,16 @@ typedef __bf16 bf16;
 typedef _Float16 f16;
 
 constexpr int kKept = LDA_OPS_RECUR_ROWS;  // rows from one kept state to the next
+constexpr int kWindow = 32;                // workgroups that are looked back to at a time
 constexpr int kWaves = 8;
-// Rows of a wave, which has N columns a lane: what lies in registers is the same.
-// The backward pass has three matrices.
+// Rows of a wave, which has N columns a lane: as many as leave room in the
+// registers for two workgroups a CU (128 a lane), so that one loads while the
+// other waits or computes.  Both passes over 65536 rows x 1024 of bf16: 8 waves of
+// 16 rows 277 us, 4 waves 309, 16 waves 312, 8 waves of 32 rows (one workgroup a
+// CU) 625.  In single precision the backward pass' three matrices fill twice as
+// many registers.
 template <typename T, int N, bool Back>
 constexpr int kRows = Back && sizeof(T) == 4 ? 16 : 32 / N;
-constexpr int kWindow = 32;                // workgroups that are looked back to at a time
 
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -81,14 +85,17 @@ template <typename T, int N>
 __device__ inline Raw<T, N> load_raw(const T *p) {
   return *reinterpret_cast<const Raw<T, N> *>(p);
 }
-template <typename T, int N>
+// Past: past the last cache, for results that it does not hold.
+template <typename T, int N, bool Past = false>
 __device__ inline void store_raw(T *p, const float (&x)[N]) {
   Raw<T, N> r;
   if constexpr (N == 1) r.v = T(x[0]);
   else
 #pragma unroll
     for (int e = 0; e < N; ++e) r.v[e] = T(x[e]);
-  *reinterpret_cast<Raw<T, N> *>(p) = r;
+  if constexpr (!Past) *reinterpret_cast<Raw<T, N> *>(p) = r;
+  else if constexpr (N == 1) __builtin_nontemporal_store(r.v, p);
+  else __builtin_nontemporal_store(r.v, reinterpret_cast<typename Raw<T, N>::vec *>(p));
 }
 
 // Values that the compiler takes for others here: it then computes what is made
@@ -268,8 +275,9 @@ struct Look {
 // workgroups'.  Leaves the workgroup's own map and state.  `needed`: the
 // workgroup's first row does not cut the chain.
 //
-// Waits only for workgroups of smaller tickets, which run already and leave
-// their maps without waiting for anything.  A look at memory takes 1.5 us in a
+// Waits only for workgroups of smaller tickets, which run already: they leave
+// their maps without waiting for anything, and their states once the one before
+// them has (the first at once).  A look at memory takes 1.5 us in a
 // full machine, as long as a sixth of a workgroup's life, and 2 KiB of all
 // columns' words: a wave looks at one word until it knows that it needs the others
 // (with all columns at each look 366 us instead of 306 for both passes over 65536
@@ -415,8 +423,12 @@ struct Forward {
   Chain chain;
 };
 
-// Bound by its bytes: x and gate in, h out.
-template <typename T, int N>
+// Bound by its bytes, x and gate in and h out, with an eighth of h more in the kept
+// states and a tenth of the time in looking back: 65536 rows x 1024 of bf16 103 us
+// = 3.9 TB/s of x, gate and h (a copy reaches 4.8), 262144 x 1000 of f16 390 us =
+// 4.0; one document of 65537 rows x 257 in single precision, where every workgroup
+// waits for the state of those before it, 69 us = 2.9.
+template <typename T, int N, bool Past>
 __global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
   constexpr int R = kRows<T, N, false>;
   __shared__ Shared<N> s;
@@ -479,7 +491,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
     if (r % kKept == 0) store_raw<float, N>(kept + int64_t(r / kKept) * p.cols + c, m);
 #pragma unroll
     for (int e = 0; e < N; ++e) m[e] = __builtin_fmaf(f[r][e], special.cut(r) ? 0.0f : m[e], b[r][e]);
-    store_raw<T, N>(h + c, m);
+    store_raw<T, N, Past>(h + c, m);
     h += p.ldh;
     if (special.last(r)) {
       float *last = p.last + int64_t(__builtin_amdgcn_readlane(mine, r) >> 2) * p.cols + c;
@@ -504,8 +516,10 @@ struct Backward {
 
 // The states are computed again from the kept ones, and the gradients run the
 // other way: row t passes l_t g_t on to row t - 1, where l_t is f_t, or nothing
-// where the chain is cut; m -> l (dh + m) is a row's map.
-template <typename T, int N>
+// where the chain is cut; m -> l (dh + m) is a row's map.  65536 rows x 1024 of
+// bf16: 168 us = 4.0 TB/s of x, gate, dh, dx and dgate; 65537 x 257 in single
+// precision 110 us = 3.1.
+template <typename T, int N, bool Past>
 __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backward<T> p) {
   constexpr int R = kRows<T, N, true>;
   __shared__ Shared<N> s;
@@ -599,8 +613,8 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
       dg[e] = out ? 0.0f : w[r][e] * grad;
       m[e] = f * grad;
     }
-    store_raw<T, N>(dx_row + c, dx);
-    store_raw<T, N>(dg_row + c, dg);
+    store_raw<T, N, Past>(dx_row + c, dx);
+    store_raw<T, N, Past>(dg_row + c, dg);
     if (special.first(r) && p.dstate)
 #pragma unroll
       for (int e = 0; e < N; ++e) p.dstate[doc * p.cols + c + e] = m[e];
@@ -669,6 +683,13 @@ struct Scan {
   }
 };
 
+// Whether the results, of so many bytes a row and column, are stored past the last
+// cache of 256 MB: 262144 x 1000 of f16 404 -> 395 us, both passes over 65536 x 1024
+// of bf16 275 -> 269.  Smaller ones are left there for who reads them next.
+bool past_cache(const lda_recur_args &a, size_t bytes) {
+  return a.rows * a.cols * int64_t(bytes) >= int64_t(256) << 20;
+}
+
 template <typename T, int N>
 hipError_t forward_n(const lda_recur_args &a, Arena &ws, bool dry) {
   const Scan scan(a, N, kRows<T, N, false> * kWaves, ws);
@@ -677,7 +698,8 @@ hipError_t forward_n(const lda_recur_args &a, Arena &ws, bool dry) {
   if (a.rows == 0) return hipSuccess;
   const Forward<T> p{static_cast<const T *>(a.x), static_cast<const T *>(a.gate), a.ldx, a.ld_gate, scan.info, a.state,
                      static_cast<T *>(a.h), a.ldh, a.last, a.kept, int(a.rows), a.cols, scan.groups, scan.chain};
-  k_recur<T, N><<<unsigned(scan.blocks) * unsigned(scan.groups), 64 * kWaves, 0, static_cast<hipStream_t>(a.stream)>>>(
+  auto kernel = past_cache(a, sizeof(T)) ? k_recur<T, N, true> : k_recur<T, N, false>;
+  kernel<<<unsigned(scan.blocks) * unsigned(scan.groups), 64 * kWaves, 0, static_cast<hipStream_t>(a.stream)>>>(
       p);
   return hipGetLastError();
 }
@@ -692,8 +714,8 @@ hipError_t backward_n(const lda_recur_args &a, Arena &ws, bool dry) {
                       a.ld_gate, a.lddh, scan.info, a.state, a.kept, a.dlast, static_cast<T *>(a.dx),
                       static_cast<T *>(a.dgate), a.lddx, a.ld_dgate, a.dstate, int(a.rows), a.cols, scan.groups, scan.blocks,
                       scan.chain};
-  k_recur_backward<T, N>
-      <<<unsigned(scan.blocks) * unsigned(scan.groups), 64 * kWaves, 0, static_cast<hipStream_t>(a.stream)>>>(p);
+  auto kernel = past_cache(a, 2 * sizeof(T)) ? k_recur_backward<T, N, true> : k_recur_backward<T, N, false>;
+  kernel<<<unsigned(scan.blocks) * unsigned(scan.groups), 64 * kWaves, 0, static_cast<hipStream_t>(a.stream)>>>(p);
   return hipGetLastError();
 }
 

@@ -160,6 +160,28 @@ def test_embedding_same_bits_and_streams(ops):  # noqa: F811
     assert torch.equal(first, second) and torch.equal(first, ops.embedding_backward(dy, words, 5000))
 
 
+@pytest.mark.parametrize("rows", [300, 30000])
+def test_embedding_in_a_graph(ops, rows):  # noqa: F811
+    """Captured once, replayed on new words, with the program's own work between."""
+    words, dy, weight = words_of(1, rows, 900), rand(2, rows, 40), rand(3, 900, 40)
+
+    def everything():
+        return ops.embedding(words, weight, 3.0), ops.embedding_backward(dy, words, 900, 3.0)
+
+    everything()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = everything()
+    for i in range(4):
+        words.copy_(words_of(10 + i, rows, 900, -50, 450 + 100 * i))
+        dy.copy_(rand(20 + i, rows, 40))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, everything()):
+            assert torch.equal(a, b), i
+
+
 def test_embedding_refusals(ops):  # noqa: F811
     weight, words, dy = rand(1, 8, 16), words_of(2, 4, 8), rand(3, 4, 16)
     bad = [lambda: ops.embedding(words.long(), weight), lambda: ops.embedding(words, weight.double()),
