@@ -1350,7 +1350,7 @@ __device__ inline Listed teacher_row(const int32_t *words, const float *scores, 
 
 // The logits of a row's listed words and its loss: a workgroup a row, four words
 // of a wave at a time.  Reads a row of the weights for each place: 8192 x 32 of
-// 1024 bf16, 537 MB that mostly lie in the caches, 63 us.
+// 1024 bf16, 537 MB that mostly lie in the caches, 68 us.
 template <typename T>
 __global__ __launch_bounds__(256) void k_distill_loss(const T *x, int64_t ldx, const T *weight, int64_t ldw,
                                                       const float *bias, const int32_t *words, int64_t ld_words,
@@ -1952,6 +1952,9 @@ lda_xent_args student(const lda_distill_args &a) {
   return x;
 }
 
+// 8192 x 1024 x 141000 of bf16, 32 words listed: forward 2.2 ms, as the cross
+// entropy's and 68 us for the listed words; backward 6.7 ms, of which the teacher's
+// part, its words' sort for dbias included, is 0.16.
 template <typename T>
 hipError_t distill_forward_t(const lda_distill_args &a, Arena &ws, bool dry) {
   const float unit = 1.0f / a.temperature;
