@@ -808,7 +808,8 @@ constexpr float kGradUnit<f16> = 16384.0f;
 //
 // With a Teacher the logits are multiplied by `unit`, `labels` says only which
 // rows are kept (0) or left out (-1), and G lacks what the teacher gives its
-// words, which k_teacher_words puts right.
+// words, which k_teacher_words puts right; `rest` (NULL: not wanted) gets what the
+// rounding of G left.
 template <typename T, int BN, int WM, bool Teacher = false>
 struct SoftmaxGrad {
   static constexpr bool kRuns = true;
@@ -820,6 +821,7 @@ struct SoftmaxGrad {
   float *col_part;  // [mtiles][piece], NULL without a bias
   int rows, vocab, first, piece;
   float unit;
+  T *rest;
   template <int MI, int NI>
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
     f32x4 b[NI], sums[NI];
@@ -856,6 +858,15 @@ struct SoftmaxGrad {
       for (int j = 0; j < NI; ++j) sums[j] += z[j] * d;
       if (m < rows)
         store_row<kRuns, T, NI>(grad + m * ldg, at.n0, at.lane >> 4, int(ldg), 8, [&](int j) { return z[j]; });
+      if constexpr (Teacher && sizeof(T) == 2 && BN < 256) {  // few rows have smaller tiles
+        if (rest && m < rows)
+          store_row<kRuns, T, NI>(rest + m * ldg, at.n0, at.lane >> 4, int(ldg), 8, [&](int j) {
+            f32x4 left;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) left[r] = z[j][r] - float(T(z[j][r]));
+            return left;
+          });
+      }
     }
     if (!col_part) return;
     float *shared = reinterpret_cast<float *>(at.lds);  // [WM][BN]
@@ -1429,7 +1440,7 @@ __global__ __launch_bounds__(256) void k_teacher(const int32_t *words, int64_t l
                                                  int64_t ld_scores, const float *logits, const float *lse,
                                                  const float *dloss, int rows, int vocab, int top, float unit,
                                                  int32_t *labels, float *row_loss, float *shifted,
-                                                 int32_t *its_word, T *its_grad, float *its_share) {
+                                                 int32_t *its_word, float *its_grad, float *its_share) {
   __shared__ float p[4][LDA_OPS_MAX_TOP];
   __shared__ int word[4][LDA_OPS_MAX_TOP];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = int(blockIdx.x) * 4 + wave;
@@ -1468,18 +1479,23 @@ __global__ __launch_bounds__(256) void k_teacher(const int32_t *words, int64_t l
     const int64_t at = int64_t(m) * top + j;
     its_word[at] = mine;
     if (mine < 0) continue;
-    its_grad[at] = T((__builtin_amdgcn_exp2f((logits[at] - l) * kLog2e) - all) * (s * kGradUnit<T>));
+    its_grad[at] = (__builtin_amdgcn_exp2f((logits[at] - l) * kLog2e) - all) * (s * kGradUnit<T>);
     if (its_share) its_share[at] = all * d;
   }
 }
 
-// A piece of G where the teacher has words.
+// A piece of G where the teacher has words, and of what its rounding left (`rest`,
+// NULL: not wanted).
 template <typename T>
-__global__ __launch_bounds__(256) void k_teacher_words(const int32_t *its_word, const T *its_grad, int64_t count,
-                                                       int top, int first, int piece, T *grad, int64_t ldg) {
+__global__ __launch_bounds__(256) void k_teacher_words(const int32_t *its_word, const float *its_grad, int64_t count,
+                                                       int top, int first, int piece, T *grad, T *rest, int64_t ldg) {
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < count; i += int64_t(gridDim.x) * 256) {
     const int at = its_word[i] - first;
-    if (its_word[i] >= 0 && at >= 0 && at < piece) grad[int64_t(uint32_t(i) / uint32_t(top)) * ldg + at] = its_grad[i];
+    if (its_word[i] < 0 || at < 0 || at >= piece) continue;
+    const int64_t to = int64_t(uint32_t(i) / uint32_t(top)) * ldg + at;
+    const T g = T(its_grad[i]);
+    grad[to] = g;
+    if (rest) rest[to] = T(its_grad[i] - float(g));
   }
 }
 
@@ -1835,17 +1851,29 @@ int piece_words(int64_t rows, int vocab) {
 }
 
 // What the backward pass of distillation has beside the cross entropy's.
-template <typename T>
 struct Teaching {
   float unit;
   int top;
   const int32_t *its_word;
-  const T *its_grad;
+  const float *its_grad;
   const float *less;  // dbias lacks this; NULL without a bias
 };
 
+// G in 16 bits is a rounding more than a product of single precision has, and costs
+// distillation, whose listed words have any p, dx and dweight up to 1.4 times the
+// error of their own rounding over many entries, 1.6 times over few (the cross
+// entropy's -1 and powers of two are exact).  Up to this many rows, where
+// products are bound by the weights and not by G, it is kept in twice its bits: as
+// G and what its rounding left, which stands below it as further rows, so that
+// both products take the two and the error is the results' rounding alone.
+// Training, us of G once / twice: 8, 32, 128 x 1024 x 141000 of bf16 344 / 378,
+// 415 / 477, 473 / 557; 128 x 257 x 9001 of f16 83 / 88.  For 8192 rows twice
+// would double two thirds of the operations.  Tiles of 256 x 256 never have the
+// least time at so few rows, and their epilogue is without it.
+constexpr int kTwiceRows = 128;
+
 template <typename T, bool Teacher>
-hipError_t softmax_backward(const lda_xent_args &a, const Teaching<T> &teaching, Arena &ws, bool dry) {
+hipError_t softmax_backward(const lda_xent_args &a, const Teaching &teaching, Arena &ws, bool dry) {
   const hipStream_t s = static_cast<hipStream_t>(a.stream);
   T *dw = static_cast<T *>(a.dweight);
   if (a.rows == 0) {
@@ -1855,25 +1883,26 @@ hipError_t softmax_backward(const lda_xent_args &a, const Teaching<T> &teaching,
   }
   const int rows = int(a.rows), piece = piece_words<T>(a.rows, a.vocab), k = int(round_up(a.width, kChunk<T>));
   const int mtiles = int(ceil_div(a.rows, tiles_of<T>(a.rows, piece).m));
+  const int times = Teacher && sizeof(T) == 2 && rows <= kTwiceRows ? 2 : 1, all = times * rows;  // of G
   Packs<T> packs;
   const Matrix<T> x = operand<T>(a.x, a.ldx, a.rows, a.width, ws, packs);
   const Matrix<T> w = operand<T>(a.weight, a.ld_weight, a.vocab, a.width, ws, packs);
   float *top = ws.take<float>(1), *row_factor = ws.take<float>(rows), *x_factor = ws.take<float>(rows);
   Sizes<T> sizes;
   const float2 *x_size = kScaledRows<T> ? sizes.add(a.x, a.ldx, a.rows, a.width, ws) : nullptr;
-  T *x_scaled = ws.take<T>(a.rows * k);
-  T *grad = ws.take<T>(a.rows * piece);
+  T *x_scaled = ws.take<T>(int64_t(all) * k);
+  T *grad = ws.take<T>(int64_t(all) * piece);
   float *col_part = a.bias ? ws.take<float>(int64_t(mtiles) * piece) : nullptr;
-  const Tiles dx_tiles = tiles_of<T>(a.rows, a.width, steps_of<T>(piece < a.vocab ? piece : a.vocab));
+  const Tiles dx_tiles = tiles_of<T>(all, a.width, steps_of<T>(piece < a.vocab ? piece : a.vocab));
   const int splits = dx_tiles.splits;
   const int64_t cols4 = round_up(a.width, 4);
-  float *dx_part = ws.take<float>(splits * a.rows * cols4);
+  float *dx_part = ws.take<float>(splits * all * cols4);
   if (!dry) {
     if constexpr (kScaledRows<T>) OPS_TRY(sizes.run(s));
     k_grad_factors<<<1, 1024, 0, s>>>(a.dloss, a.lse, a.labels, x_size, rows, a.vocab, kGradUnit<T>, top, row_factor,
                                       x_factor);
     OPS_TRY(hipGetLastError());
-    packs.add(a.x, a.ldx, a.rows, a.width, x_factor, x_scaled, k);
+    for (int i = 0; i < times; ++i) packs.add(a.x, a.ldx, a.rows, a.width, x_factor, x_scaled + a.rows * k * i, k);
     OPS_TRY(packs.run(s));
   }
   // the pieces' products share the scratch of their parts
@@ -1883,12 +1912,13 @@ hipError_t softmax_backward(const lda_xent_args &a, const Teaching<T> &teaching,
     const int words = a.vocab - first < piece ? a.vocab - first : piece;
     const int words_k = int(round_up(words, kChunk<T>));
     const T *wp = w.p + int64_t(first) * w.ld;
+    T *rest = times > 1 ? grad + a.rows * words_k : nullptr;
     ws.used = mark;
     if (!dry) {
       OPS_TRY(with_shape<T>(tiles_of<T>(a.rows, piece), [&](auto shape) {
         typedef decltype(shape) S;
         const SoftmaxGrad<T, S::BN, S::WM, Teacher> epi{a.bias,   a.labels, a.lse, row_factor, grad,  words_k,
-                                                        col_part, rows,     a.vocab, first,    words, teaching.unit};
+                                                        col_part, rows,     a.vocab, first,    words, teaching.unit, rest};
         return product<T, S>(a.rows, words_k, k, 1, Rows<T>{x.p, x.ld, rows, k}, Rows<T>{wp, w.ld, words, k}, epi, s);
       }));
       if (a.dbias) {
@@ -1900,35 +1930,35 @@ hipError_t softmax_backward(const lda_xent_args &a, const Teaching<T> &teaching,
       if constexpr (Teacher) {
         const int64_t listed = a.rows * teaching.top;
         k_teacher_words<T><<<strided(ceil_div(listed, 256)), 256, 0, s>>>(
-            teaching.its_word, teaching.its_grad, listed, teaching.top, first, words, grad, words_k);
+            teaching.its_word, teaching.its_grad, listed, teaching.top, first, words, grad, rest, words_k);
         OPS_TRY(hipGetLastError());
       }
       OPS_TRY(with_shape<T>(dx_tiles, [&](auto shape) {
-        const Rows<T> gr{grad, words_k, rows, words_k};
+        const Rows<T> gr{grad, words_k, all, words_k};
         const Columns<T> wc{wp, w.ld, a.width, words};
         if (first == 0)
-          return product<T, decltype(shape)>(a.rows, a.width, words, splits, gr, wc,
-                                             StorePart<false>{dx_part, rows, int(cols4)}, s);
-        return product<T, decltype(shape)>(a.rows, a.width, words, splits, gr, wc,
-                                           StorePart<true>{dx_part, rows, int(cols4)}, s);
+          return product<T, decltype(shape)>(all, a.width, words, splits, gr, wc,
+                                             StorePart<false>{dx_part, all, int(cols4)}, s);
+        return product<T, decltype(shape)>(all, a.width, words, splits, gr, wc,
+                                           StorePart<true>{dx_part, all, int(cols4)}, s);
       }));
     }
     T *dwp = dw + int64_t(first) * a.width;
     const Target<T> out{dwp, nullptr, a.width, words, false, at_once<T>(dwp, a.width), top, 0};
-    OPS_TRY(product_into<T>(words, a.width, a.rows, Columns<T>{grad, words_k, words, rows},
-                            Columns<T>{x_scaled, k, a.width, rows}, out, ws, dry, s));
+    OPS_TRY(product_into<T>(words, a.width, all, Columns<T>{grad, words_k, words, all},
+                            Columns<T>{x_scaled, k, a.width, all}, out, ws, dry, s));
     if (ws.used > most) most = ws.used;
   }
   ws.used = most;
   if (dry) return hipSuccess;
   const Target<T> out{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, at_once<T>(a.dx, a.lddx), row_factor, 1};
-  k_join<T><<<strided(ceil_div(a.rows * cols4, 1024)), 256, 0, s>>>(dx_part, splits, rows, a.width, int(cols4), out);
+  k_join<T><<<strided(ceil_div(a.rows * cols4, 1024)), 256, 0, s>>>(dx_part, times * splits, rows, a.width, int(cols4), out);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t xent_backward_t(const lda_xent_args &a, Arena &ws, bool dry) {
-  return softmax_backward<T, false>(a, Teaching<T>{1.0f, 0, nullptr, nullptr, nullptr}, ws, dry);
+  return softmax_backward<T, false>(a, Teaching{1.0f, 0, nullptr, nullptr, nullptr}, ws, dry);
 }
 
 // The softmax over the student's logits, as the cross entropy has it.
@@ -1974,7 +2004,7 @@ hipError_t distill_backward_t(const lda_distill_args &a, Arena &ws, bool dry) {
   lda_xent_args x = student(a);
   int32_t *labels = ws.take<int32_t>(a.rows), *its_word = ws.take<int32_t>(listed);
   float *row_loss = ws.take<float>(a.rows), *shifted = ws.take<float>(a.rows);
-  T *its_grad = ws.take<T>(listed);
+  float *its_grad = ws.take<float>(listed);
   float *its_share = a.bias ? ws.take<float>(listed) : nullptr, *less = a.bias ? ws.take<float>(a.vocab) : nullptr;
   if (!dry && a.rows) {
     k_teacher<T><<<unsigned(ceil_div(a.rows, 4)), 256, 0, s>>>(a.words, a.ld_words, a.scores, a.ld_scores, a.logits,
@@ -1987,7 +2017,7 @@ hipError_t distill_backward_t(const lda_distill_args &a, Arena &ws, bool dry) {
   x.labels = labels;
   x.dloss = row_loss;
   x.lse = shifted;
-  return softmax_backward<T, true>(x, Teaching<T>{unit, a.top, its_word, its_grad, less}, ws, dry);
+  return softmax_backward<T, true>(x, Teaching{unit, a.top, its_word, its_grad, less}, ws, dry);
 }
 
 }  // namespace

@@ -3,8 +3,9 @@
 Bounds as in test_gpu_ops.py for the student's softmax (the logits and their
 logarithm divided by the temperature).  The teacher's p and its logarithm carry
 the scores' rounding, a few E of the largest, and g(top) of the sum.  G of the
-16-bit types is rounded once, the rows of x for dweight once more; dbias takes
-the students' and the teachers' parts in two sums.
+16-bit types is rounded once (up to 128 rows what that leaves is kept too, rounded
+to the same type: off by U of U); dbias takes the students' and the teachers' parts
+in two sums.
 """
 import math
 
@@ -79,7 +80,7 @@ def case(ops, dtype, rows, width, vocab, top, with_bias, temperature, pad=0, off
     egiven = torch.zeros_like(q).scatter_add_(1, at, torch.where(there, p * (ep + top * E), zero))
     grad = d8 * (q - given)
     top_d = float(d8.abs().max())
-    u = (U[dtype] if dtype != torch.float32 else 0.0) + 6 * E
+    u = (0.0 if dtype == torch.float32 else U[dtype] ** 2 if rows <= 128 else U[dtype]) + 6 * E
     eq = q * (2 * elsum + 6 * E * 40 + 2 * elogit)[:, None]
     eg = d8.abs() * (eq + egiven + 2 * E * (q + given)) + u * grad.abs()
     if dtype == torch.float16:
