@@ -477,7 +477,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
       if (special.out(r)) b[r][e] = 0.0f;
       f[r][e] = cut ? 0.0f : f[r][e];
       sum[e] = __builtin_fmaf(f[r][e], cut ? 0.0f : sum[e], b[r][e]);
-      a[e] *= f[r][e];
+      a[e] = cut ? 0.0f : a[e] * f[r][e];  // a document before may have a gate that is NaN
     }
   }
   float m[N];

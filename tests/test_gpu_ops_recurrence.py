@@ -274,6 +274,33 @@ def test_recurrence_gradients_against_differences(ops):  # noqa: F811
     assert abs(got - want) <= ROOM * max(1.0, abs(want))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_recurrence_bad_documents_between_sound_ones(ops, dtype, bad):  # noqa: F811
+    """Documents of nothing but infinities or NaN, which begin and end inside the rows of a wave."""
+    lengths = [5, 7, 200, 20, 3, 1, 400, 300, 90]
+    rows, cols = sum(lengths), 10
+    off = offsets_of(lengths)
+    x, gate, state, dh, dlast = inputs(dtype, rows, cols, len(lengths), True)
+
+    def everything():
+        h, last, kept = ops.recurrence(x, gate, off, state)
+        return [h, last, *ops.recurrence_backward(dh, x, gate, off, kept, state, dlast)]
+
+    want = [t.clone() for t in everything()]
+    sound = torch.ones(rows, dtype=torch.bool, device="cuda")
+    for s in (1, 3, 5, 7):
+        part = slice(int(off[s]), int(off[s + 1]))
+        sound[part] = False
+        for t in (x, gate, dh):
+            t[part] = bad
+        state[s], dlast[s] = bad, bad
+    got = everything()
+    for name, a, b in zip(("h", "last", "dx", "dgate", "dstate"), got, want):
+        at = slice(0, None, 2) if name in ("last", "dstate") else sound
+        assert torch.equal(a[at], b[at]), name
+
+
 def test_recurrence_same_bits_and_streams(ops):  # noqa: F811
     """Long and short documents: the same bits whichever workgroup comes first, on any stream, twice at once."""
     lengths = [9000, 3, 0, 500, 20000, 100]
