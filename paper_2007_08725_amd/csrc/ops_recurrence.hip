@@ -220,24 +220,26 @@ __global__ __launch_bounds__(256) void k_documents(const Docs d) {
 
 // ----------------------------------------------------------------- chain -----
 // What a workgroup leaves for the ones after it, in two words of 64 bits for each
-// of its columns: its map's A and B, and in the place of B, as soon as it has it,
-// the state after its last row.  A word holds its value and beside it what it is,
-// so that a reader needs no order between the words.
+// of its lanes' columns: its map's A and B, and in the place of B, as soon as it
+// has it, the state after its last row.  A word holds its value and beside it what
+// it is, so that a reader needs no order between the words.  They are numbered by
+// the lanes, not by the columns: a column that two parts of a row have (column_of)
+// has words of each, or the map of one could take the place of the other's state.
 enum : uint32_t { kNothing = 0, kMap = 1, kState = 2 };
 constexpr int kWords = 2;
 struct Chain {
-  uint64_t *words;   // [blocks][kWords][cols]
+  uint64_t *words;   // [blocks][kWords][slots]
   uint32_t *ticket;  // the workgroups' order
-  int cols;
-  __device__ uint64_t *at(int block, int word, int c) const {
-    return words + (int64_t(block) * kWords + word) * cols + c;
+  int slots;         // N for each lane of a row's parts
+  __device__ uint64_t *at(int block, int word, int slot) const {
+    return words + (int64_t(block) * kWords + word) * slots + slot;
   }
-  __device__ void leave(int block, int word, int c, uint32_t what, float v) const {
-    __hip_atomic_store(at(block, word, c), uint64_t(what) << 32 | __builtin_bit_cast(uint32_t, v), __ATOMIC_RELAXED,
+  __device__ void leave(int block, int word, int slot, uint32_t what, float v) const {
+    __hip_atomic_store(at(block, word, slot), uint64_t(what) << 32 | __builtin_bit_cast(uint32_t, v), __ATOMIC_RELAXED,
                        __HIP_MEMORY_SCOPE_AGENT);
   }
-  __device__ uint64_t look(int block, int word, int c) const {
-    return __hip_atomic_load(at(block, word, c), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __device__ uint64_t look(int block, int word, int slot) const {
+    return __hip_atomic_load(at(block, word, slot), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 };
 
@@ -258,9 +260,9 @@ struct Shared {
 template <int N>
 struct Look {
   uint64_t a[N], b[N];
-  __device__ void take(const Chain &chain, int from, int word, int c, bool in) {
+  __device__ void take(const Chain &chain, int from, int word, int slot, bool in) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) (word ? b : a)[e] = in ? chain.look(from, word, c + e) : 0;
+    for (int e = 0; e < N; ++e) (word ? b : a)[e] = in ? chain.look(from, word, slot + e) : 0;
   }
   __device__ bool all(const uint64_t (&w)[N], uint32_t is, bool in) const {
     bool yes = true;
@@ -284,9 +286,9 @@ struct Look {
 // rows x 1024 of bf16; with the first look before the workgroup's maps are joined
 // 362).
 template <int N>
-__device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int order, bool needed, int c, bool in,
+__device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int order, bool needed, int group, bool in,
                                 const float (&map_a)[N], const float (&map_b)[N], bool cuts, float (&m)[N]) {
-  const int lane = threadIdx.x & 63, first = lane * N;
+  const int lane = threadIdx.x & 63, first = lane * N, slot = (group * 64 + lane) * N;
   needed &= block > 0;  // the same in all waves
 #pragma unroll
   for (int e = 0; e < N; ++e) {
@@ -330,15 +332,14 @@ __device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int
   if (order == 0 && in) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      if (!known) chain.leave(block, 0, c + e, kMap, a[e]);
-      chain.leave(block, 1, c + e, known ? kState : kMap, b[e]);
+      if (!known) chain.leave(block, 0, slot + e, kMap, a[e]);
+      chain.leave(block, 1, slot + e, known ? kState : kMap, b[e]);
     }
   }
   float carry[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) carry[e] = 0.0f;
   if (needed) {
-    const int column = __builtin_amdgcn_readfirstlane(c);
     int found;
     while (true) {
       // each wave looks at every kWaves-th workgroup before this one, until it or another wave has a state that is
@@ -348,18 +349,18 @@ __device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int
         Look<N> seen;
         bool state = false;
         while (true) {
-          const uint32_t peek = __builtin_amdgcn_readfirstlane(what(chain.look(from, 1, column)));
+          const uint32_t peek = __builtin_amdgcn_readfirstlane(what(chain.look(from, 1, group * 64 * N)));
           if (peek == kState && lane == 0) atomicMin(&s.nearest, back);
           if (__hip_atomic_load(&s.nearest, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) < back) break;
           if (peek == kNothing) {
             __builtin_amdgcn_s_sleep(2);
             continue;
           }
-          seen.take(chain, from, 1, c, in);
+          seen.take(chain, from, 1, slot, in);
           state = seen.all(seen.b, kState, in);
           if (state) break;
           if (seen.all(seen.b, kMap, in)) {
-            seen.take(chain, from, 0, c, in);
+            seen.take(chain, from, 0, slot, in);
             if (seen.all(seen.a, kMap, in)) break;
           }
         }
@@ -389,7 +390,7 @@ __device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int
   if (order == 0) {
     if (!known && in) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) chain.leave(block, 1, c + e, kState, __builtin_fmaf(a[e], carry[e], b[e]));
+      for (int e = 0; e < N; ++e) chain.leave(block, 1, slot + e, kState, __builtin_fmaf(a[e], carry[e], b[e]));
     }
 #pragma unroll
     for (int e = 0; e < N; ++e) m[e] = carry[e];
@@ -481,7 +482,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
     }
   }
   float m[N];
-  state_in<N>(s, p.chain, block, wave, !row_cuts(begins), c, in, a, sum, special.cuts != 0, m);
+  state_in<N>(s, p.chain, block, wave, !row_cuts(begins), t % p.groups, in, a, sum, special.cuts != 0, m);
   if (!in || row0 >= p.rows) return;
   T *h = p.h + int64_t(row0) * p.ldh;
   float *kept = p.kept + int64_t(row0 / kKept) * p.cols;
@@ -587,7 +588,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
   }
   const int order = kWaves - 1 - wave;
   float m[N];
-  state_in<N>(s, p.chain, back, order, !row_cuts(follows), c, in, a, sum, special.cuts != 0, m);
+  state_in<N>(s, p.chain, back, order, !row_cuts(follows), t % p.groups, in, a, sum, special.cuts != 0, m);
   if (!in || row0 >= p.rows) return;
   T *dx_row = p.dx + int64_t(row0 + R) * p.lddx, *dg_row = p.dgate + int64_t(row0 + R) * p.ld_dgate;
 #pragma unroll
@@ -659,10 +660,10 @@ struct Scan {
     blocks = int(ceil_div(a.rows, rows_each));
     groups = int(ceil_div(a.cols, 64 * columns));
     info = ws.take<int>(a.rows);
-    const int64_t words = int64_t(blocks) * kWords * a.cols;
+    chain.slots = groups * 64 * columns;
+    const int64_t words = int64_t(blocks) * kWords * chain.slots;
     chain.words = ws.take<uint64_t>(words + 1);
     chain.ticket = reinterpret_cast<uint32_t *>(chain.words + words);
-    chain.cols = a.cols;
   }
   hipError_t documents(const lda_recur_args &a, const float *from, float *out) const {
     Docs d = {};
@@ -672,7 +673,7 @@ struct Scan {
     d.cols = a.cols;
     d.info = info;
     d.clear = chain.words;
-    d.clear_count = int64_t(blocks) * kWords * a.cols + 1;
+    d.clear_count = int64_t(blocks) * kWords * chain.slots + 1;
     d.from = from;
     d.out = out;
     int64_t most = a.rows > d.clear_count / 4 ? a.rows : d.clear_count / 4;

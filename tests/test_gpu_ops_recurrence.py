@@ -301,6 +301,25 @@ def test_recurrence_bad_documents_between_sound_ones(ops, dtype, bad):  # noqa: 
         assert torch.equal(a[at], b[at]), name
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [129, 257, 385])
+def test_recurrence_columns_of_two_workgroups(ops, dtype, cols):  # noqa: F811
+    """A row's last column alone in a part of 128, so that its pair has a column of the part before: as by themselves."""
+    rows = 30000
+    off = offsets_of([rows - 900, 900])
+    x, gate, state, dh, dlast = inputs(dtype, rows, cols, 2, True, level=4.0)
+
+    def everything(at):
+        h, last, kept = ops.recurrence(x[:, at], gate[:, at], off, state[:, at].contiguous())
+        return [h, last, kept, *ops.recurrence_backward(dh[:, at], x[:, at], gate[:, at], off, kept,
+                                                        state[:, at].contiguous(), dlast[:, at].contiguous())]
+
+    want = everything(slice(cols - 2, cols))
+    for _ in range(5):
+        for a, b in zip(everything(slice(0, cols)), want):
+            assert torch.equal(a[:, -2:], b)
+
+
 def test_recurrence_same_bits_and_streams(ops):  # noqa: F811
     """Long and short documents: the same bits whichever workgroup comes first, on any stream, twice at once."""
     lengths = [9000, 3, 0, 500, 20000, 100]
