@@ -101,6 +101,7 @@ __device__ inline void store_raw(T *p, const float (&x)[N]) {
 // Values that the compiler takes for others here: it then computes what is made
 // of them where it is used, instead of keeping it in registers from earlier on.
 __device__ inline void anew(float &x) { asm volatile("" : "+v"(x)); }
+__device__ inline void anew(int &x) { asm volatile("" : "+v"(x)); }
 template <typename T, int N>
 __device__ inline void anew(Raw<T, N> &x) {
   if constexpr (sizeof(x) == 4) {
@@ -231,15 +232,16 @@ struct Chain {
   uint64_t *words;   // [blocks][kWords][slots]
   uint32_t *ticket;  // the workgroups' order
   int slots;         // N for each lane of a row's parts
-  __device__ uint64_t *at(int block, int word, int slot) const {
-    return words + (int64_t(block) * kWords + word) * slots + slot;
+  // `part` begins the workgroup's slots, `slot` is a lane's in them
+  __device__ uint64_t *at(int block, int word, int part, int slot) const {
+    return words + ((int64_t(block) * kWords + word) * slots + part) + slot;
   }
-  __device__ void leave(int block, int word, int slot, uint32_t what, float v) const {
-    __hip_atomic_store(at(block, word, slot), uint64_t(what) << 32 | __builtin_bit_cast(uint32_t, v), __ATOMIC_RELAXED,
+  __device__ void leave(int block, int word, int part, int slot, uint32_t what, float v) const {
+    __hip_atomic_store(at(block, word, part, slot), uint64_t(what) << 32 | __builtin_bit_cast(uint32_t, v), __ATOMIC_RELAXED,
                        __HIP_MEMORY_SCOPE_AGENT);
   }
-  __device__ uint64_t look(int block, int word, int slot) const {
-    return __hip_atomic_load(at(block, word, slot), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __device__ uint64_t look(int block, int word, int part, int slot) const {
+    return __hip_atomic_load(at(block, word, part, slot), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 };
 
@@ -260,9 +262,9 @@ struct Shared {
 template <int N>
 struct Look {
   uint64_t a[N], b[N];
-  __device__ void take(const Chain &chain, int from, int word, int slot, bool in) {
+  __device__ void take(const Chain &chain, int from, int word, int part, int slot, bool in) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) (word ? b : a)[e] = in ? chain.look(from, word, slot + e) : 0;
+    for (int e = 0; e < N; ++e) (word ? b : a)[e] = in ? chain.look(from, word, part, slot + e) : 0;
   }
   __device__ bool all(const uint64_t (&w)[N], uint32_t is, bool in) const {
     bool yes = true;
@@ -288,7 +290,7 @@ struct Look {
 template <int N>
 __device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int order, bool needed, int group, bool in,
                                 const float (&map_a)[N], const float (&map_b)[N], bool cuts, float (&m)[N]) {
-  const int lane = threadIdx.x & 63, first = lane * N, slot = (group * 64 + lane) * N;
+  const int lane = threadIdx.x & 63, first = lane * N, part = group * 64 * N;
   needed &= block > 0;  // the same in all waves
 #pragma unroll
   for (int e = 0; e < N; ++e) {
@@ -332,8 +334,8 @@ __device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int
   if (order == 0 && in) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      if (!known) chain.leave(block, 0, slot + e, kMap, a[e]);
-      chain.leave(block, 1, slot + e, known ? kState : kMap, b[e]);
+      if (!known) chain.leave(block, 0, part, first + e, kMap, a[e]);
+      chain.leave(block, 1, part, first + e, known ? kState : kMap, b[e]);
     }
   }
   float carry[N];
@@ -349,18 +351,18 @@ __device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int
         Look<N> seen;
         bool state = false;
         while (true) {
-          const uint32_t peek = __builtin_amdgcn_readfirstlane(what(chain.look(from, 1, group * 64 * N)));
+          const uint32_t peek = __builtin_amdgcn_readfirstlane(what(chain.look(from, 1, part, 0)));
           if (peek == kState && lane == 0) atomicMin(&s.nearest, back);
           if (__hip_atomic_load(&s.nearest, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) < back) break;
           if (peek == kNothing) {
             __builtin_amdgcn_s_sleep(2);
             continue;
           }
-          seen.take(chain, from, 1, slot, in);
+          seen.take(chain, from, 1, part, first, in);
           state = seen.all(seen.b, kState, in);
           if (state) break;
           if (seen.all(seen.b, kMap, in)) {
-            seen.take(chain, from, 0, slot, in);
+            seen.take(chain, from, 0, part, first, in);
             if (seen.all(seen.a, kMap, in)) break;
           }
         }
@@ -390,7 +392,7 @@ __device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int
   if (order == 0) {
     if (!known && in) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) chain.leave(block, 1, slot + e, kState, __builtin_fmaf(a[e], carry[e], b[e]));
+      for (int e = 0; e < N; ++e) chain.leave(block, 1, part, first + e, kState, __builtin_fmaf(a[e], carry[e], b[e]));
     }
 #pragma unroll
     for (int e = 0; e < N; ++e) m[e] = carry[e];
@@ -527,7 +529,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
   const int t = take_ticket(s, p.chain), back = t / p.groups, block = p.blocks - 1 - back;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool in = (t % p.groups * 64 + lane) * N < p.cols;
-  const int c = column_of<N>(t % p.groups, lane, p.cols);
+  int c = column_of<N>(t % p.groups, lane, p.cols);
   const int row0 = block * R * kWaves + wave * R;
   const int mine = lane < R && row0 + lane < p.rows ? p.info[row0 + lane] : -1;
   // whether the row after the workgroup's last one passes anything on
@@ -590,6 +592,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
   float m[N];
   state_in<N>(s, p.chain, back, order, !row_cuts(follows), t % p.groups, in, a, sum, special.cuts != 0, m);
   if (!in || row0 >= p.rows) return;
+  // the column once more: kept in a register until here it would send others to memory
+  int again = threadIdx.x & 63;
+  anew(again);
+  c = column_of<N>(t % p.groups, again, p.cols);
   T *dx_row = p.dx + int64_t(row0 + R) * p.lddx, *dg_row = p.dgate + int64_t(row0 + R) * p.ld_dgate;
 #pragma unroll
   for (int r = R - 1; r >= 0; --r) {
