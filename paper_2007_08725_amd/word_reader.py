@@ -114,20 +114,19 @@ class WordReader(Trained):
         return float(total) / (max(1, ends[-1] - ends[0]) * math.log(2))
 
     def start(self, docs: int):
-        """The state of ``docs`` documents of which nothing is read."""
+        """The state of ``docs`` documents of which nothing is read, for the parameters as they are now."""
         device = self.params["bias"].device
-        return (torch.zeros(docs, self.width, dtype=self.dtype, device=device),
+        return (self._cast(), torch.zeros(docs, self.width, dtype=self.dtype, device=device),
                 torch.zeros(docs, self.width, device=device))
 
     def read(self, state, words):
         """Scores the next word of each document and reads it: ``(loss, state)``, as ``loss`` has them for the whole."""
-        p = self._cast()
-        s, exact = state
+        p, s, exact = state
         _, _, _, h = self._hidden(p, s)
         loss, _ = ops.softmax_xent(h, p["weight"], words, p["bias"])
         e = ops.embedding(words, p["embed"], math.sqrt(self.width))
         g = ops.embedding(words, p["gate"])
-        return loss, ops.recurrence_step(e, g, exact)
+        return loss, (p, *ops.recurrence_step(e, g, exact))
 
 
 def train(model, words, offsets, steps: int, batch: int = 4096, lr: float = 1e-2, teacher=None, part: float = 0.5,
