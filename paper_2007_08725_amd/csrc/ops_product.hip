@@ -442,10 +442,13 @@ __global__ __launch_bounds__(64 * WM *WN, 2) void k_product(Grid g, L left, R ri
 // with this one's (beside 128 accumulators there are no registers for it).
 __device__ inline void one_row_at_a_time() { __builtin_amdgcn_sched_barrier(0); }
 
+// Four columns of a row, of which `count` are inside it, at any address (global
+// memory takes vectors wherever they begin; element by element the gradient of
+// 111968 x 318 of f16 from 123 rows took 96 us instead of 41).
 template <typename T>
-__device__ inline void store4(T *p, f32x4 v, int count, bool whole) {
-  if (whole && count >= 4) {
-    typedef T vec __attribute__((ext_vector_type(4)));
+__device__ inline void store4(T *p, f32x4 v, int count) {
+  if (count >= 4) {
+    typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
     *reinterpret_cast<vec *>(p) = vec{T(v[0]), T(v[1]), T(v[2]), T(v[3])};
   } else {
 #pragma unroll
@@ -455,10 +458,10 @@ __device__ inline void store4(T *p, f32x4 v, int count, bool whole) {
 }
 
 template <typename T>
-__device__ inline f32x4 load4(const T *p, int count, bool whole) {
+__device__ inline f32x4 load4(const T *p, int count) {
   f32x4 v = {0, 0, 0, 0};
-  if (whole && count >= 4) {
-    typedef T vec __attribute__((ext_vector_type(4)));
+  if (count >= 4) {
+    typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
     const vec w = *reinterpret_cast<const vec *>(p);
 #pragma unroll
     for (int r = 0; r < 4; ++r) v[r] = float(w[r]);
@@ -471,20 +474,19 @@ __device__ inline f32x4 load4(const T *p, int count, bool whole) {
 }
 
 // Stores the columns of C that a lane of group g holds, in a row that ends at
-// `cols`: with Runs and 16-bit types eight at a time.  `by` is how many
-// elements of the row can be stored at once: 8, 4 or 1.
+// `cols`: with Runs and 16-bit types eight at a time.
 template <bool Runs, typename T, int NI, typename Value>
-__device__ inline void store_row(T *row, int n0, int g, int cols, int by, Value value) {
+__device__ inline void store_row(T *row, int n0, int g, int cols, Value value) {
 #pragma unroll
   for (int j = 0; j < NI; j += 2) {
     const int c = n0 + Order<Runs>::col(j, g), d = n0 + Order<Runs>::col(j + 1, g);
     const f32x4 a = value(j), b = value(j + 1);
-    if (Runs && sizeof(T) == 2 && by == 8 && c + 8 <= cols) {
-      typedef T vec __attribute__((ext_vector_type(8)));
+    if (Runs && sizeof(T) == 2 && c + 8 <= cols) {
+      typedef T vec __attribute__((ext_vector_type(8), aligned(sizeof(T))));
       *reinterpret_cast<vec *>(row + c) = vec{T(a[0]), T(a[1]), T(a[2]), T(a[3]), T(b[0]), T(b[1]), T(b[2]), T(b[3])};
     } else {
-      if (c < cols) store4(row + c, a, cols - c, by >= 4);
-      if (d < cols) store4(row + d, b, cols - d, by >= 4);
+      if (c < cols) store4(row + c, a, cols - c);
+      if (d < cols) store4(row + d, b, cols - d);
     }
   }
 }
@@ -497,7 +499,6 @@ struct Target {
   int64_t ld;
   int rows;  // of p (and q)
   bool pair;
-  int by;               // columns that can be stored at once
   const float *factor;  // of the result, on the device: one for all (step 0) or one a row (step 1); NULL = 1
   int factor_step;
   __device__ float scale(int m) const { return factor ? factor[m * factor_step] : 1.0f; }
@@ -522,7 +523,7 @@ struct Store {
       T *row = out.row(m);
       if (!row) continue;
       const float f = out.scale(m);
-      store_row<kRuns, T, NI>(row, at.n0, at.lane >> 4, cols, out.by, [&](int j) { return c[i][j] * f; });
+      store_row<kRuns, T, NI>(row, at.n0, at.lane >> 4, cols, [&](int j) { return c[i][j] * f; });
     }
   }
 };
@@ -607,7 +608,6 @@ struct GatedForward {
   T *h;
   int64_t ld;
   int rows, hidden, act;
-  bool whole;
   template <int MI, int NI>
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
 #pragma unroll
@@ -626,7 +626,7 @@ struct GatedForward {
           gate<T>(act, c[i][j][r], p, dp);
           v[r] = p * c[i][j + 1][r];
         }
-        store4(h + m * ld + f, v, hidden - f, whole);
+        store4(h + m * ld + f, v, hidden - f);
       }
     }
   }
@@ -650,7 +650,6 @@ struct GatedBackward {
   const float *scale;  // of each row, with kScaledRows
   T *dab;              // [rows][pair_cols]
   int rows, hidden, pair_cols, act;
-  bool whole;
   template <int MI, int NI>
   __device__ void operator()(const Place &at, f32x4 (&c)[MI][NI]) const {
 #pragma unroll
@@ -664,7 +663,7 @@ struct GatedBackward {
 #pragma unroll
       for (int j = 0; j < NI; j += 2) {
         const int f = pair_row(at.n0 + Order<kRuns>::col(j, at.lane >> 4));
-        f32x4 dhv = load4(dh + m * ld + f, hidden - f, whole);
+        f32x4 dhv = load4(dh + m * ld + f, hidden - f);
         if constexpr (kScaledRows<T>) dhv *= s;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -674,7 +673,7 @@ struct GatedBackward {
           d[j + 1][r] = f + r < hidden ? dhv[r] * p : 0.0f;
         }
       }
-      store_row<kRuns, T, NI>(dab + int64_t(m) * pair_cols, at.n0, at.lane >> 4, pair_cols, 8, [&](int j) { return d[j]; });
+      store_row<kRuns, T, NI>(dab + int64_t(m) * pair_cols, at.n0, at.lane >> 4, pair_cols, [&](int j) { return d[j]; });
     }
   }
 };
@@ -857,10 +856,10 @@ struct SoftmaxGrad {
 #pragma unroll
       for (int j = 0; j < NI; ++j) sums[j] += z[j] * d;
       if (m < rows)
-        store_row<kRuns, T, NI>(grad + m * ldg, at.n0, at.lane >> 4, int(ldg), 8, [&](int j) { return z[j]; });
+        store_row<kRuns, T, NI>(grad + m * ldg, at.n0, at.lane >> 4, int(ldg), [&](int j) { return z[j]; });
       if constexpr (Teacher && sizeof(T) == 2 && BN < 256) {  // few rows have smaller tiles
         if (rest && m < rows)
-          store_row<kRuns, T, NI>(rest + m * ldg, at.n0, at.lane >> 4, int(ldg), 8, [&](int j) {
+          store_row<kRuns, T, NI>(rest + m * ldg, at.n0, at.lane >> 4, int(ldg), [&](int j) {
             f32x4 left;
 #pragma unroll
             for (int r = 0; r < 4; ++r) left[r] = z[j][r] - float(T(z[j][r]));
@@ -898,15 +897,19 @@ struct SoftmaxGrad {
 // reaches 4.8 TB/s; through tiles of 64 x 64 it took 83 us.
 constexpr int kFewRows = 16;
 
-// Chunk `c` of a row of `cols` elements, zero past its end; rows that do not
-// start at multiples of 16 bytes, or do not end at one, element by element.
+// Chunk `c` of a row of `cols` elements, zero past its end; a chunk that a row
+// ends inside of element by element.
 template <typename T, bool Aligned>
 __device__ inline u32x4 row_chunk(const T *row, int c, int cols) {
   if (Aligned) return c * kChunk<T> < cols ? *reinterpret_cast<const u32x4 *>(row + c * kChunk<T>) : u32x4{0, 0, 0, 0};
-  typedef T vec __attribute__((ext_vector_type(kChunk<T>)));
+  typedef T vec __attribute__((ext_vector_type(kChunk<T>), aligned(sizeof(T))));
   vec v;
+  if ((c + 1) * kChunk<T> <= cols) {
+    v = *reinterpret_cast<const vec *>(row + c * kChunk<T>);
+  } else {
 #pragma unroll
-  for (int e = 0; e < kChunk<T>; ++e) v[e] = c * kChunk<T> + e < cols ? row[c * kChunk<T> + e] : T(0.0f);
+    for (int e = 0; e < kChunk<T>; ++e) v[e] = c * kChunk<T> + e < cols ? row[c * kChunk<T> + e] : T(0.0f);
+  }
   return __builtin_bit_cast(u32x4, v);
 }
 
@@ -915,7 +918,7 @@ __device__ inline u32x4 row_chunk(const T *row, int c, int cols) {
 template <typename T, bool Aligned, int TILES>
 __device__ inline void few_products(const T *x, const T *const (&w)[TILES], int cols, int part, int parts, int lane,
                                     f32x4 (&c)[TILES]) {
-  constexpr int U = Aligned ? 8 / TILES : 2;  // groups in flight
+  constexpr int U = 8 / TILES;  // groups in flight
   const int groups = (cols + 4 * kChunk<T> - 1) / (4 * kChunk<T>);
 #pragma unroll
   for (int t = 0; t < TILES; ++t) c[t] = f32x4{0, 0, 0, 0};
@@ -1032,6 +1035,7 @@ __global__ __launch_bounds__(256) void k_lse_join(const float2 *part, int ntiles
   const int m = blockIdx.x * 16 + (threadIdx.x & 15), way = threadIdx.x >> 4;
   float2 a = make_float2(-INFINITY, 0.0f);
   if (m < rows)
+#pragma unroll 8
     for (int t = way; t < ntiles; t += 16) a = softmax_join(a, part[int64_t(t) * rows + m]);
   shared[way][threadIdx.x & 15] = a;
   __syncthreads();
@@ -1153,9 +1157,10 @@ __global__ __launch_bounds__(256) void k_join(const float *part, int splits, int
     T *row = out.row(m);
     if (!row || n >= cols) continue;
     f32x4 s = *reinterpret_cast<const f32x4 *>(part + at);
+#pragma unroll 8
     for (int z = 1; z < splits; ++z) s += *reinterpret_cast<const f32x4 *>(part + z * all + at);
     s *= out.scale(m);
-    store4(row + n, s, cols - n, out.by >= 4);
+    store4(row + n, s, cols - n);
   }
 }
 
@@ -1167,8 +1172,9 @@ __global__ __launch_bounds__(256) void k_zero(T *p, int64_t n) {
 // Copies of matrices for the products, up to four a launch (a launch takes
 // longer than the copy of a small matrix): rows at multiples of 16 bytes, zero
 // past their end; each row times its factor, a row of factor 0 zero whatever it
-// holds (factor NULL = 1).  A lane reads a chunk element by element and writes
-// it at once; divisions in 32 bits where the count of chunks allows it.
+// holds (factor NULL = 1).  A lane reads a chunk at once, from wherever it begins,
+// and the one that the row ends in element by element; divisions in 32 bits where
+// the count of chunks allows it.
 template <typename T>
 struct Copy {
   const T *src;
@@ -1191,20 +1197,22 @@ __global__ __launch_bounds__(256) void k_pack(const Copies<T> copies) {
     const int64_t r = all <= 0xffffffffll ? uint32_t(i) / uint32_t(c.chunks) : i / c.chunks;
     const int first = int(i - r * c.chunks) * kChunk<T>;
     const float f = c.factor ? c.factor[r] : 1.0f;
-    union {
-      T v[kChunk<T>];
-      uint4 all;
-    } u;
+    typedef T vec __attribute__((ext_vector_type(kChunk<T>), aligned(sizeof(T))));
+    const T *from = c.src + r * c.ld + first;
+    vec v = {};
+    if (f != 0.0f) {
+      if (first + kChunk<T> <= c.cols) {
+        v = *reinterpret_cast<const vec *>(from);
+      } else {
 #pragma unroll
-    for (int e = 0; e < kChunk<T>; ++e) {
-      T v = T(0.0f);
-      if (first + e < c.cols && f != 0.0f) {
-        v = c.src[r * c.ld + first + e];
-        if (c.factor) v = T(float(v) * f);
+        for (int e = 0; e < kChunk<T>; ++e)
+          if (first + e < c.cols) v[e] = from[e];
       }
-      u.v[e] = v;
+      if (c.factor)
+#pragma unroll
+        for (int e = 0; e < kChunk<T>; ++e) v[e] = T(float(v[e]) * f);
     }
-    reinterpret_cast<uint4 *>(c.dst)[i] = u.all;
+    reinterpret_cast<u32x4 *>(c.dst)[i] = __builtin_bit_cast(u32x4, v);
   }
 }
 
@@ -1500,14 +1508,6 @@ __global__ __launch_bounds__(256) void k_teacher_words(const int32_t *its_word, 
 }
 
 // ------------------------------------------------------------------- host ---
-// How many elements of a row can be moved at once: 8, 4 or 1.
-template <typename T>
-int at_once(const void *p, int64_t ld) {
-  for (int n : {8, 4})
-    if (reinterpret_cast<uintptr_t>(p) % (n * sizeof(T) < 16 ? n * sizeof(T) : 16) == 0 && ld % n == 0) return n;
-  return 1;
-}
-
 // Whether an operand can be read where it lies: its rows start at multiples of
 // 16 bytes and hold whole chunks.
 template <typename T>
@@ -1728,7 +1728,7 @@ hipError_t gated_forward_t(const lda_gated_args &a, Arena &ws, bool dry) {
   pair_operands<T>(a, false, ws, packs, gate, value);
   if (dry) return hipSuccess;
   OPS_TRY(packs.run(s));
-  const GatedForward<T> epi{static_cast<T *>(a.h), a.ldh, rows, a.hidden, a.act, at_once<T>(a.h, a.ldh) >= 4};
+  const GatedForward<T> epi{static_cast<T *>(a.h), a.ldh, rows, a.hidden, a.act};
   return with_shape<T>(tiles_of<T>(a.rows, pair_cols(a.hidden)), [&](auto shape) {
     return product<T, decltype(shape)>(a.rows, pair_cols(a.hidden), k, 1, Rows<T>{x.p, x.ld, rows, k},
                                        PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s);
@@ -1779,18 +1779,16 @@ hipError_t gated_backward_t(const lda_gated_args &a, Arena &ws, bool dry) {
   }
   if (!dry) {
     OPS_TRY(packs.run(s));
-    const GatedBackward<T> epi{static_cast<const T *>(a.dh), a.lddh, scale, dab, rows, a.hidden, pc, a.act,
-                               at_once<T>(a.dh, a.lddh) >= 4};
+    const GatedBackward<T> epi{static_cast<const T *>(a.dh), a.lddh, scale, dab, rows, a.hidden, pc, a.act};
     OPS_TRY(with_shape<T>(tiles_of<T>(a.rows, pc), [&](auto shape) {
       return product<T, decltype(shape)>(a.rows, pc, k, 1, Rows<T>{x.p, x.ld, rows, k},
                                          PairRows<T>{gate.p, value.p, gate.ld, value.ld, a.hidden, k}, epi, s);
     }));
   }
-  const Target<T> dx{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, at_once<T>(a.dx, a.lddx), dx_factor, 1};
+  const Target<T> dx{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, dx_factor, 1};
   OPS_TRY(product_into<T>(a.rows, a.width, pc, Rows<T>{dab, pc, rows, pc},
                           PairColumns<T>{gate.p, value.p, gate.ld, a.width, a.hidden}, dx, ws, dry, s));
-  const int by_g = at_once<T>(dwg, a.width), by_v = at_once<T>(dwv, a.width);
-  const Target<T> dw{dwg, dwv, a.width, a.hidden, true, by_g < by_v ? by_g : by_v, dw_factor, 0};
+  const Target<T> dw{dwg, dwv, a.width, a.hidden, true, dw_factor, 0};
   return product_into<T>(pc, a.width, a.rows, Columns<T>{dab, pc, pc, rows},
                          Columns<T>{x_scaled.p, x_scaled.ld, a.width, rows}, dw, ws, dry, s);
 }
@@ -1944,14 +1942,14 @@ hipError_t softmax_backward(const lda_xent_args &a, const Teaching &teaching, Ar
       }));
     }
     T *dwp = dw + int64_t(first) * a.width;
-    const Target<T> out{dwp, nullptr, a.width, words, false, at_once<T>(dwp, a.width), top, 0};
+    const Target<T> out{dwp, nullptr, a.width, words, false, top, 0};
     OPS_TRY(product_into<T>(words, a.width, all, Columns<T>{grad, words_k, words, all},
                             Columns<T>{x_scaled, k, a.width, all}, out, ws, dry, s));
     if (ws.used > most) most = ws.used;
   }
   ws.used = most;
   if (dry) return hipSuccess;
-  const Target<T> out{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, at_once<T>(a.dx, a.lddx), row_factor, 1};
+  const Target<T> out{static_cast<T *>(a.dx), nullptr, a.lddx, rows, false, row_factor, 1};
   k_join<T><<<strided(ceil_div(a.rows * cols4, 1024)), 256, 0, s>>>(dx_part, times * splits, rows, a.width, int(cols4), out);
   return hipGetLastError();
 }
