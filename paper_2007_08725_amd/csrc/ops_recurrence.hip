@@ -120,20 +120,35 @@ __device__ inline int column_of(int group, int lane, int cols) {
   return c < cols ? min(c, cols - N) : 0;
 }
 
+// A wave's lanes are P parts of 64 / P: narrow matrices leave lanes without columns
+// otherwise, and a row costs a wave the same whatever its width.  Each part has R
+// rows of its own, after those of the part before it.  Both passes over 262144 rows
+// x 20 of bf16 with 1 / 4 parts NARROW_20 us, x 64 with 1 / 2 NARROW_64.
+template <int P>
+__device__ inline int part_of(int lane) {
+  return P == 1 ? 0 : lane / (64 / P);
+}
+template <int P>
+__device__ inline int lane_of(int lane) {
+  return P == 1 ? lane : lane & (64 / P - 1);
+}
+
 // ------------------------------------------------------------- documents -----
 // What a row is: -1 of no document, else 4 times its document, + 1 if it is the
 // first of it, + 2 if the last.
 __device__ inline bool row_cuts(int info) { return info < 0 || (info & 1); }
 
-// The rows of a wave (lane r has what row r is, others -1) that are not inside a
-// document: one bit a row.
+// The rows of a part of a wave that are not inside a document: one bit a row.
+// Lane p R + r has what row r of part p is, other lanes -1.
 struct Special {
-  uint64_t outs, cuts, lasts;
-  __device__ Special(int info, int rows)
-      : outs(__ballot(info < 0)), cuts(__ballot(row_cuts(info))), lasts(__ballot(info >= 0 && (info & 2))) {
-    const uint64_t all = (uint64_t(1) << rows) - 1;
+  uint32_t outs, cuts, lasts;
+  __device__ Special(int info, int rows, int part)
+      : outs(uint32_t(__ballot(info < 0) >> part * rows)), cuts(uint32_t(__ballot(row_cuts(info)) >> part * rows)),
+        lasts(uint32_t(__ballot(info >= 0 && (info & 2)) >> part * rows)) {
+    const uint32_t all = uint32_t((uint64_t(1) << rows) - 1);
     outs &= all;
     cuts &= all;
+    lasts &= all;
   }
   __device__ bool out(int r) const { return outs >> r & 1; }    // of no document
   __device__ bool cut(int r) const { return cuts >> r & 1; }    // the chain is cut before it
@@ -287,10 +302,11 @@ struct Look {
 // (with all columns at each look 366 us instead of 306 for both passes over 65536
 // rows x 1024 of bf16; with the first look before the workgroup's maps are joined
 // 362).
-template <int N>
+template <int N, int P>
 __device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int order, bool needed, int group, bool in,
                                 const float (&map_a)[N], const float (&map_b)[N], bool cuts, float (&m)[N]) {
-  const int lane = threadIdx.x & 63, first = lane * N, part = group * 64 * N;
+  const int lane = threadIdx.x & 63, first = lane_of<P>(lane) * N, part = group * 64 * N;
+  const bool leaves = in && part_of<P>(lane) == 0;
   needed &= block > 0;  // the same in all waves
 #pragma unroll
   for (int e = 0; e < N; ++e) {
@@ -331,7 +347,7 @@ __device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int
     }
   }
   const bool known = cut || block == 0;  // the state after the workgroup, in its first wave
-  if (order == 0 && in) {
+  if (order == 0 && leaves) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       if (!known) chain.leave(block, 0, part, first + e, kMap, a[e]);
@@ -390,7 +406,7 @@ __device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int
       for (int e = 0; e < N; ++e) carry[e] = __builtin_fmaf(s.past_a[i][first + e], carry[e], s.past_b[i][first + e]);
   }
   if (order == 0) {
-    if (!known && in) {
+    if (!known && leaves) {
 #pragma unroll
       for (int e = 0; e < N; ++e) chain.leave(block, 1, part, first + e, kState, __builtin_fmaf(a[e], carry[e], b[e]));
     }
@@ -400,6 +416,62 @@ __device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int
 #pragma unroll
     for (int e = 0; e < N; ++e) m[e] = cut ? b[e] : __builtin_fmaf(a[e], carry[e], b[e]);
   }
+}
+
+// The maps of a wave's parts, (a, b) and whether one cuts the chain, joined from the
+// first part on (Back: from the last): (a, b) becomes the whole wave's, and before is
+// what comes to this part of the state that comes to the wave.
+template <int N, int P, bool Back>
+struct Parts {
+  float a[N], b[N];
+  bool cut;
+  __device__ Parts(float (&map_a)[N], float (&map_b)[N], bool &cuts) {
+    if constexpr (P == 1) return;
+    constexpr int L = 64 / P;
+    const int lane = threadIdx.x & 63, turn = Back ? P - 1 - part_of<P>(lane) : part_of<P>(lane);
+    auto from = [&](auto v, int by) { return Back ? __shfl_down(v, by) : __shfl_up(v, by); };
+#pragma unroll
+    for (int x = 1; x < P; x <<= 1) {
+      const bool joins = turn >= x, other = from(int(cuts), x * L);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float pa = from(map_a[e], x * L), pb = from(map_b[e], x * L);
+        if (joins && !cuts) {
+          map_b[e] = __builtin_fmaf(map_a[e], pb, map_b[e]);
+          map_a[e] *= pa;
+        }
+      }
+      cuts |= joins && other;
+    }
+    cut = from(int(cuts), L) && turn > 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      a[e] = from(map_a[e], L);
+      b[e] = from(map_b[e], L);
+      if (turn == 0) {
+        a[e] = 1.0f;
+        b[e] = 0.0f;
+      }
+    }
+    const int whole = (Back ? 0 : P - 1) * L + lane_of<P>(lane);
+    cuts = __shfl(int(cuts), whole);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      map_a[e] = __shfl(map_a[e], whole);
+      map_b[e] = __shfl(map_b[e], whole);
+    }
+  }
+  __device__ void apply(float (&m)[N]) const {
+    if constexpr (P > 1)
+#pragma unroll
+      for (int e = 0; e < N; ++e) m[e] = cut ? b[e] : __builtin_fmaf(a[e], m[e], b[e]);
+  }
+};
+
+// The document of row r of a part.
+template <int P>
+__device__ inline int64_t doc_of(int mine, const int *info, int row0, int r) {
+  return (P == 1 ? __builtin_amdgcn_readlane(mine, r) : info[row0 + r]) >> 2;
 }
 
 // The workgroup's place in the order: workgroups of a smaller ticket run.
@@ -431,18 +503,18 @@ struct Forward {
 // = 3.9 TB/s of x, gate and h (a copy reaches 4.8), 262144 x 1000 of f16 390 us =
 // 4.0; one document of 65537 rows x 257 in single precision, where every workgroup
 // waits for the state of those before it, 69 us = 2.9.
-template <typename T, int N, bool Past>
+template <typename T, int N, int P, bool Past>
 __global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
   constexpr int R = kRows<T, N, false>;
   __shared__ Shared<N> s;
   const int t = take_ticket(s, p.chain), block = t / p.groups;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool in = (t % p.groups * 64 + lane) * N < p.cols;
-  const int c = column_of<N>(t % p.groups, lane, p.cols);
-  const int row0 = block * R * kWaves + wave * R;
+  const bool in = (t % p.groups * 64 + lane_of<P>(lane)) * N < p.cols;
+  const int c = column_of<N>(t % p.groups, lane_of<P>(lane), p.cols);
+  const int wave_row = (block * kWaves + wave) * R * P, row0 = wave_row + part_of<P>(lane) * R;
   // rows past the end repeat the last one; what they are says that they are of no document
-  const int mine = lane < R && row0 + lane < p.rows ? p.info[row0 + lane] : -1;
-  const int begins = p.info[block * R * kWaves];
+  const int mine = lane < R * P && wave_row + lane < p.rows ? p.info[wave_row + lane] : -1;
+  const int begins = p.info[block * R * P * kWaves];
   Raw<T, N> x[R], g[R];
   const int last_row = p.rows - 1;
   const T *px = p.x + int64_t(min(row0, last_row)) * p.ldx, *pg = p.gate + int64_t(min(row0, last_row)) * p.ld_gate;
@@ -460,7 +532,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
     a[e] = 1.0f;
     sum[e] = 0.0f;
   }
-  const Special special(mine, R);
+  const Special special(mine, R, part_of<P>(lane));
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const bool cut = special.cut(r);
@@ -471,7 +543,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
       b[r][e] = keep * x[r][e];
     }
     if (special.first(r) && p.state) {
-      const float *state = p.state + int64_t(__builtin_amdgcn_readlane(mine, r) >> 2) * p.cols + c;
+      const float *state = p.state + doc_of<P>(mine, p.info, row0, r) * p.cols + c;
 #pragma unroll
       for (int e = 0; e < N; ++e) b[r][e] = __builtin_fmaf(f[r][e], state[e], b[r][e]);
     }
@@ -484,7 +556,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
     }
   }
   float m[N];
-  state_in<N>(s, p.chain, block, wave, !row_cuts(begins), t % p.groups, in, a, sum, special.cuts != 0, m);
+  bool cuts = special.cuts != 0;
+  const Parts<N, P, false> before(a, sum, cuts);
+  state_in<N, P>(s, p.chain, block, wave, !row_cuts(begins), t % p.groups, in, a, sum, cuts, m);
+  before.apply(m);
   if (!in || row0 >= p.rows) return;
   T *h = p.h + int64_t(row0) * p.ldh;
   float *kept = p.kept + int64_t(row0 / kKept) * p.cols;
@@ -497,7 +572,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
     store_raw<T, N, Past>(h + c, m);
     h += p.ldh;
     if (special.last(r)) {
-      float *last = p.last + int64_t(__builtin_amdgcn_readlane(mine, r) >> 2) * p.cols + c;
+      float *last = p.last + doc_of<P>(mine, p.info, row0, r) * p.cols + c;
 #pragma unroll
       for (int e = 0; e < N; ++e) last[e] = m[e];
     }
@@ -522,18 +597,18 @@ struct Backward {
 // where the chain is cut; m -> l (dh + m) is a row's map.  65536 rows x 1024 of
 // bf16: 168 us = 4.0 TB/s of x, gate, dh, dx and dgate; 65537 x 257 in single
 // precision 110 us = 3.1.
-template <typename T, int N, bool Past>
+template <typename T, int N, int P, bool Past>
 __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backward<T> p) {
   constexpr int R = kRows<T, N, true>;
   __shared__ Shared<N> s;
   const int t = take_ticket(s, p.chain), back = t / p.groups, block = p.blocks - 1 - back;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool in = (t % p.groups * 64 + lane) * N < p.cols;
-  int c = column_of<N>(t % p.groups, lane, p.cols);
-  const int row0 = block * R * kWaves + wave * R;
-  const int mine = lane < R && row0 + lane < p.rows ? p.info[row0 + lane] : -1;
+  const bool in = (t % p.groups * 64 + lane_of<P>(lane)) * N < p.cols;
+  int c = column_of<N>(t % p.groups, lane_of<P>(lane), p.cols);
+  const int wave_row = (block * kWaves + wave) * R * P, row0 = wave_row + part_of<P>(lane) * R;
+  const int mine = lane < R * P && wave_row + lane < p.rows ? p.info[wave_row + lane] : -1;
   // whether the row after the workgroup's last one passes anything on
-  const int after = (block + 1) * R * kWaves;
+  const int after = (block + 1) * R * P * kWaves;
   const int follows = after < p.rows ? p.info[after] : -1;
   Raw<T, N> x[R], g[R], d[R];
   const int last_row = p.rows - 1;
@@ -557,13 +632,13 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
     a[e] = 1.0f;
     sum[e] = 0.0f;
   }
-  const Special special(mine, R);
-  // only the first of the wave's last rows may lie before a cut
-  const int last = p.dlast && special.lasts ? __ffsll((unsigned long long)special.lasts) - 1 : -1;
+  const Special special(mine, R, part_of<P>(lane));
+  // only the first of the part's last rows may lie before a cut
+  const int last = p.dlast && special.lasts ? __ffs(int(special.lasts)) - 1 : -1;
   float more[N];
 #pragma unroll
   for (int e = 0; e < N; ++e)
-    more[e] = last < 0 ? 0.0f : p.dlast[int64_t(__builtin_amdgcn_readlane(mine, last) >> 2) * p.cols + c + e];
+    more[e] = last < 0 ? 0.0f : p.dlast[doc_of<P>(mine, p.info, row0, last) * p.cols + c + e];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     if (special.cut(r)) {
@@ -572,9 +647,9 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
       if (special.first(r) && p.state)
 #pragma unroll
         for (int e = 0; e < N; ++e)
-          h[e] = p.state[int64_t(__builtin_amdgcn_readlane(mine, r) >> 2) * p.cols + c + e];
+          h[e] = p.state[doc_of<P>(mine, p.info, row0, r) * p.cols + c + e];
     }
-    const bool cut = special.cuts << (63 - r);  // this row or one before it: its part goes to no row before them
+    const bool cut = special.cuts << (31 - r);  // this row or one before it: its part goes to no row before them
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       float f, k;
@@ -590,25 +665,27 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
   }
   const int order = kWaves - 1 - wave;
   float m[N];
-  state_in<N>(s, p.chain, back, order, !row_cuts(follows), t % p.groups, in, a, sum, special.cuts != 0, m);
+  bool cuts = special.cuts != 0;
+  const Parts<N, P, true> before(a, sum, cuts);
+  state_in<N, P>(s, p.chain, back, order, !row_cuts(follows), t % p.groups, in, a, sum, cuts, m);
+  before.apply(m);
   if (!in || row0 >= p.rows) return;
   // the column once more: kept in a register until here it would send others to memory
   int again = threadIdx.x & 63;
   anew(again);
-  c = column_of<N>(t % p.groups, again, p.cols);
+  c = column_of<N>(t % p.groups, lane_of<P>(again), p.cols);
   T *dx_row = p.dx + int64_t(row0 + R) * p.lddx, *dg_row = p.dgate + int64_t(row0 + R) * p.ld_dgate;
 #pragma unroll
   for (int r = R - 1; r >= 0; --r) {
     dx_row -= p.lddx;
     dg_row -= p.ld_dgate;
     if (row0 + r >= p.rows) continue;
-    const int64_t doc = __builtin_amdgcn_readlane(mine, r) >> 2;
     float dx[N], dg[N];
     anew(d[r]);
     // nothing comes to a last row from the next one
     if (special.last(r) && p.dlast)
 #pragma unroll
-      for (int e = 0; e < N; ++e) m[e] = p.dlast[doc * p.cols + c + e];
+      for (int e = 0; e < N; ++e) m[e] = p.dlast[doc_of<P>(mine, p.info, row0, r) * p.cols + c + e];
     const bool out = special.out(r);
 #pragma unroll
     for (int e = 0; e < N; ++e) {
@@ -624,7 +701,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backwar
     store_raw<T, N, Past>(dg_row + c, dg);
     if (special.first(r) && p.dstate)
 #pragma unroll
-      for (int e = 0; e < N; ++e) p.dstate[doc * p.cols + c + e] = m[e];
+      for (int e = 0; e < N; ++e) p.dstate[doc_of<P>(mine, p.info, row0, r) * p.cols + c + e] = m[e];
 #pragma unroll
     for (int e = 0; e < N; ++e) m[e] = special.cut(r) ? 0.0f : m[e];
   }
@@ -697,23 +774,23 @@ bool past_cache(const lda_recur_args &a, size_t bytes) {
   return a.rows * a.cols * int64_t(bytes) >= int64_t(256) << 20;
 }
 
-template <typename T, int N>
+template <typename T, int N, int P>
 hipError_t forward_n(const lda_recur_args &a, Arena &ws, bool dry) {
-  const Scan scan(a, N, kRows<T, N, false> * kWaves, ws);
+  const Scan scan(a, N, kRows<T, N, false> * P * kWaves, ws);
   if (dry) return hipSuccess;
   OPS_TRY(scan.documents(a, a.state, a.last));
   if (a.rows == 0) return hipSuccess;
   const Forward<T> p{static_cast<const T *>(a.x), static_cast<const T *>(a.gate), a.ldx, a.ld_gate, scan.info, a.state,
                      static_cast<T *>(a.h), a.ldh, a.last, a.kept, int(a.rows), a.cols, scan.groups, scan.chain};
-  auto kernel = past_cache(a, sizeof(T)) ? k_recur<T, N, true> : k_recur<T, N, false>;
+  auto kernel = P == 1 && past_cache(a, sizeof(T)) ? k_recur<T, N, P, P == 1> : k_recur<T, N, P, false>;
   kernel<<<unsigned(scan.blocks) * unsigned(scan.groups), 64 * kWaves, 0, static_cast<hipStream_t>(a.stream)>>>(
       p);
   return hipGetLastError();
 }
 
-template <typename T, int N>
+template <typename T, int N, int P>
 hipError_t backward_n(const lda_recur_args &a, Arena &ws, bool dry) {
-  const Scan scan(a, N, kRows<T, N, true> * kWaves, ws);
+  const Scan scan(a, N, kRows<T, N, true> * P * kWaves, ws);
   if (dry) return hipSuccess;
   OPS_TRY(scan.documents(a, a.dlast, a.dstate));
   if (a.rows == 0) return hipSuccess;
@@ -721,26 +798,45 @@ hipError_t backward_n(const lda_recur_args &a, Arena &ws, bool dry) {
                       a.ld_gate, a.lddh, scan.info, a.state, a.kept, a.dlast, static_cast<T *>(a.dx),
                       static_cast<T *>(a.dgate), a.lddx, a.ld_dgate, a.dstate, int(a.rows), a.cols, scan.groups, scan.blocks,
                       scan.chain};
-  auto kernel = past_cache(a, 2 * sizeof(T)) ? k_recur_backward<T, N, true> : k_recur_backward<T, N, false>;
+  auto kernel = P == 1 && past_cache(a, 2 * sizeof(T)) ? k_recur_backward<T, N, P, P == 1>
+                                                        : k_recur_backward<T, N, P, false>;
   kernel<<<unsigned(scan.blocks) * unsigned(scan.groups), 64 * kWaves, 0, static_cast<hipStream_t>(a.stream)>>>(p);
   return hipGetLastError();
 }
 
-// 16-bit columns in pairs, 32 bits a lane as in single precision.
+// Calls fn with the columns of a lane (16-bit ones in pairs, 32 bits as in single
+// precision) and the parts of a wave: as many as a row leaves room for and as the
+// wave has lanes to hold what their rows are.
+template <typename T, bool Back, typename Fn>
+hipError_t with_lanes(int cols, Fn fn) {
+  auto parts = [&](auto n) {
+    constexpr int N = decltype(n)::value, R = kRows<T, N, Back>;
+    if constexpr (R * 4 <= 64) {
+      if (cols <= 16 * N) return fn(n, std::integral_constant<int, 4>());
+    }
+    if constexpr (R * 2 <= 64) {
+      if (cols <= 32 * N) return fn(n, std::integral_constant<int, 2>());
+    }
+    return fn(n, std::integral_constant<int, 1>());
+  };
+  if constexpr (sizeof(T) == 2) {
+    if (cols > 1) return parts(std::integral_constant<int, 2>());
+  }
+  return parts(std::integral_constant<int, 1>());
+}
+
 template <typename T>
 hipError_t forward_t(const lda_recur_args &a, Arena &ws, bool dry) {
-  if constexpr (sizeof(T) == 2) {
-    if (a.cols > 1) return forward_n<T, 2>(a, ws, dry);
-  }
-  return forward_n<T, 1>(a, ws, dry);
+  return with_lanes<T, false>(a.cols, [&](auto n, auto p) {
+    return forward_n<T, decltype(n)::value, decltype(p)::value>(a, ws, dry);
+  });
 }
 
 template <typename T>
 hipError_t backward_t(const lda_recur_args &a, Arena &ws, bool dry) {
-  if constexpr (sizeof(T) == 2) {
-    if (a.cols > 1) return backward_n<T, 2>(a, ws, dry);
-  }
-  return backward_n<T, 1>(a, ws, dry);
+  return with_lanes<T, true>(a.cols, [&](auto n, auto p) {
+    return backward_n<T, decltype(n)::value, decltype(p)::value>(a, ws, dry);
+  });
 }
 
 template <typename T>

@@ -304,20 +304,22 @@ def test_recurrence_bad_documents_between_sound_ones(ops, dtype, bad):  # noqa: 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("cols", [129, 257, 385])
 def test_recurrence_columns_of_two_workgroups(ops, dtype, cols):  # noqa: F811
-    """A row's last column alone in a part of 128, so that its pair has a column of the part before: as by themselves."""
+    """A row's last column alone in a part of 128, so that its pair has a column of the part before: the bits that it
+    has with a column after it, which makes the pair whole."""
     rows = 30000
     off = offsets_of([rows - 900, 900])
-    x, gate, state, dh, dlast = inputs(dtype, rows, cols, 2, True, level=4.0)
+    x, gate, state, dh, dlast = inputs(dtype, rows, cols + 1, 2, True, level=4.0)
 
-    def everything(at):
-        h, last, kept = ops.recurrence(x[:, at], gate[:, at], off, state[:, at].contiguous())
-        return [h, last, kept, *ops.recurrence_backward(dh[:, at], x[:, at], gate[:, at], off, kept,
-                                                        state[:, at].contiguous(), dlast[:, at].contiguous())]
+    def everything(n):
+        first = state[:, :n].contiguous()
+        h, last, kept = ops.recurrence(x[:, :n], gate[:, :n], off, first)
+        return [h, last, kept, *ops.recurrence_backward(dh[:, :n], x[:, :n], gate[:, :n], off, kept, first,
+                                                        dlast[:, :n].contiguous())]
 
-    want = everything(slice(cols - 2, cols))
+    want = everything(cols + 1)
     for _ in range(5):
-        for a, b in zip(everything(slice(0, cols)), want):
-            assert torch.equal(a[:, -2:], b)
+        for a, b in zip(everything(cols), want):
+            assert torch.equal(a, b[:, :cols])
 
 
 def test_recurrence_same_bits_and_streams(ops):  # noqa: F811
