@@ -504,7 +504,7 @@ struct Forward {
 // 4.0; one document of 65537 rows x 257 in single precision, where every workgroup
 // waits for the state of those before it, 69 us = 2.9.
 template <typename T, int N, int P, bool Past>
-__global__ __launch_bounds__(64 * kWaves, 4) void k_recur(const Forward<T> p) {
+__global__ __launch_bounds__(64 * kWaves, P == 1 ? 4 : 2) void k_recur(const Forward<T> p) {
   constexpr int R = kRows<T, N, false>;
   __shared__ Shared<N> s;
   const int t = take_ticket(s, p.chain), block = t / p.groups;
@@ -598,7 +598,7 @@ struct Backward {
 // bf16: 168 us = 4.0 TB/s of x, gate, dh, dx and dgate; 65537 x 257 in single
 // precision 110 us = 3.1.
 template <typename T, int N, int P, bool Past>
-__global__ __launch_bounds__(64 * kWaves, 4) void k_recur_backward(const Backward<T> p) {
+__global__ __launch_bounds__(64 * kWaves, P == 1 ? 4 : 2) void k_recur_backward(const Backward<T> p) {
   constexpr int R = kRows<T, N, true>;
   __shared__ Shared<N> s;
   const int t = take_ticket(s, p.chain), back = t / p.groups, block = p.blocks - 1 - back;
