@@ -122,8 +122,13 @@ __device__ inline int column_of(int group, int lane, int cols) {
 
 // A wave's lanes are P parts of 64 / P: narrow matrices leave lanes without columns
 // otherwise, and a row costs a wave the same whatever its width.  Each part has R
-// rows of its own, after those of the part before it.  Both passes over 262144 rows
-// x 20 of bf16 with 1 / 4 parts NARROW_20 us, x 64 with 1 / 2 NARROW_64.
+// rows of its own, after those of the part before it.  Both passes over 262144
+// rows x 20 of bf16 with 1 / 4 parts 128 / 63 us, x 64 with 1 / 2 134 / 112; one
+// document x 64, forward, 190 / 101.  Addresses and what rows are then differ by
+// lane and take registers, so that one workgroup fits a CU (two, with 19 registers
+// in memory: x 64 124 us).
+template <int P>
+constexpr int kWavesPerSimd = P == 1 ? 4 : 2;
 template <int P>
 __device__ inline int part_of(int lane) {
   return P == 1 ? 0 : lane / (64 / P);
@@ -239,15 +244,15 @@ __global__ __launch_bounds__(256) void k_documents(const Docs d) {
 // of its lanes' columns: its map's A and B, and in the place of B, as soon as it
 // has it, the state after its last row.  A word holds its value and beside it what
 // it is, so that a reader needs no order between the words.  They are numbered by
-// the lanes, not by the columns: a column that two parts of a row have (column_of)
-// has words of each, or the map of one could take the place of the other's state.
+// the lanes, not by the columns: a column that two workgroups have (column_of) has
+// words of each, or the map of one could take the place of the other's state.
 enum : uint32_t { kNothing = 0, kMap = 1, kState = 2 };
 constexpr int kWords = 2;
 struct Chain {
   uint64_t *words;   // [blocks][kWords][slots]
   uint32_t *ticket;  // the workgroups' order
-  int slots;         // N for each lane of a row's parts
-  // `part` begins the workgroup's slots, `slot` is a lane's in them
+  int slots;         // N for each lane of the workgroups of a row
+  // the workgroup's slots begin at `part`, `slot` is a lane's among them
   __device__ uint64_t *at(int block, int word, int part, int slot) const {
     return words + ((int64_t(block) * kWords + word) * slots + part) + slot;
   }
@@ -504,7 +509,7 @@ struct Forward {
 // 4.0; one document of 65537 rows x 257 in single precision, where every workgroup
 // waits for the state of those before it, 69 us = 2.9.
 template <typename T, int N, int P, bool Past>
-__global__ __launch_bounds__(64 * kWaves, P == 1 ? 4 : 2) void k_recur(const Forward<T> p) {
+__global__ __launch_bounds__(64 * kWaves, kWavesPerSimd<P>) void k_recur(const Forward<T> p) {
   constexpr int R = kRows<T, N, false>;
   __shared__ Shared<N> s;
   const int t = take_ticket(s, p.chain), block = t / p.groups;
@@ -598,7 +603,7 @@ struct Backward {
 // bf16: 168 us = 4.0 TB/s of x, gate, dh, dx and dgate; 65537 x 257 in single
 // precision 110 us = 3.1.
 template <typename T, int N, int P, bool Past>
-__global__ __launch_bounds__(64 * kWaves, P == 1 ? 4 : 2) void k_recur_backward(const Backward<T> p) {
+__global__ __launch_bounds__(64 * kWaves, kWavesPerSimd<P>) void k_recur_backward(const Backward<T> p) {
   constexpr int R = kRows<T, N, true>;
   __shared__ Shared<N> s;
   const int t = take_ticket(s, p.chain), back = t / p.groups, block = p.blocks - 1 - back;
