@@ -23,6 +23,19 @@ inline unsigned strided(int64_t workgroups) { return unsigned(workgroups < 65536
     if (e_ != hipSuccess) return e_;       \
   } while (0)
 
+// Launches fn(first row, rows) for all rows, `groups` of them to a workgroup of
+// `threads`: in more than one launch where one would have 2^32 threads.
+template <typename Fn>
+hipError_t by_rows(int64_t rows, int64_t threads, int64_t groups, Fn fn) {
+  const int64_t most = 0xffffffffll / threads * groups;
+  for (int64_t first = 0; first < rows; first += most) {
+    fn(first, rows - first < most ? rows - first : most);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 // Scratch of one call, cut from the caller's workspace in 256-byte steps.
 // With a null base it only counts: the *_workspace calls and the launches
 // walk through the same code.

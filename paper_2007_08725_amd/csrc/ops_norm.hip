@@ -400,19 +400,6 @@ bool aligned16(const void *p, int64_t ld) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % kChunk<T> == 0;
 }
 
-// Launches fn(first row, rows) for all rows, `groups` of them to a workgroup of
-// `threads`: in more than one launch where one would have 2^32 threads.
-template <typename Fn>
-hipError_t by_rows(int64_t rows, int64_t threads, int64_t groups, Fn fn) {
-  const int64_t most = 0xffffffffll / threads * groups;
-  for (int64_t first = 0; first < rows; first += most) {
-    fn(first, rows - first < most ? rows - first : most);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
-}
-
 template <typename T>
 hipError_t norm_forward_t(const lda_norm_args &a) {
   if (a.rows == 0) return hipSuccess;

@@ -1988,10 +1988,13 @@ hipError_t distill_forward_t(const lda_distill_args &a, Arena &ws, bool dry) {
   const float unit = 1.0f / a.temperature;
   OPS_TRY((softmax_forward<T, true>(student(a), unit, ws, dry)));
   if (dry || a.rows == 0) return hipSuccess;
-  k_distill_loss<T><<<unsigned(a.rows), 256, 0, static_cast<hipStream_t>(a.stream)>>>(
-      static_cast<const T *>(a.x), a.ldx, static_cast<const T *>(a.weight), a.ld_weight, a.bias, a.words, a.ld_words,
-      a.scores, a.ld_scores, a.width, a.vocab, a.top, unit, a.lse, a.logits, a.loss);
-  return hipGetLastError();
+  const T *x = static_cast<const T *>(a.x);
+  return by_rows(a.rows, 256, 1, [&](int64_t m, int64_t rows) {
+    k_distill_loss<T><<<unsigned(rows), 256, 0, static_cast<hipStream_t>(a.stream)>>>(
+        x + m * a.ldx, a.ldx, static_cast<const T *>(a.weight), a.ld_weight, a.bias, a.words + m * a.ld_words,
+        a.ld_words, a.scores + m * a.ld_scores, a.ld_scores, a.width, a.vocab, a.top, unit, a.lse + m,
+        a.logits + m * a.top, a.loss + m);
+  });
 }
 
 template <typename T>
