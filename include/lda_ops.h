@@ -20,7 +20,7 @@
  *     rows start at multiples of 16 bytes and hold a multiple of 16 bytes are
  *     read where they lie; others are slower (the products copy them into the
  *     workspace first).
- *   - Sums, softmax statistics and row statistics are kept in 32 bits; an
+ *   - Sums, softmax statistics and row statistics are kept in 32 bits or more; an
  *     output is rounded once to its type.  Every sum has one order: results
  *     are the same bits on every run.
  *   - `workspace` is device scratch of at least the size that the operator's
@@ -200,8 +200,9 @@ lda_status lda_softmax_xent_backward(const lda_xent_args *a);
  *   dweight_v = scale * sum of dy_i over the rows with word_i = v
  * (0 for a word that no row has; rows outside the vocabulary have no part in
  * it, whatever their dy holds).  The rows are sorted by word and a word's are
- * summed in 32 bits in their order, in pieces of a fixed length.  scale must be
- * finite.
+ * summed in their order, in pieces of a fixed length: in 32 bits for 16-bit types,
+ * in 64 bits for single precision, so that dweight is off by its own rounding
+ * alone however many rows a word has.  scale must be finite.
  */
 typedef struct {
   int32_t dtype; /* of weight, y, dy, dweight */

@@ -8,6 +8,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "ops_internal.h"
 
 #pragma clang fp contract(fast)
@@ -398,13 +400,23 @@ __global__ __launch_bounds__(256) void k_sort_place(const SortPass p, const Fill
 // piece goes to its row of the gradient; what it has in a piece that it shares
 // with the piece before (slot 0) or after it (slot 1, where it begins in this
 // piece) goes to `part` [pieces][2][width], which k_join_words sums.
+//
+// Sums are kept in 32 bits for 16-bit types, whose own rounding is 2^13 or 2^16
+// times theirs, and in 64 for single precision: added there in 32 bits, one after
+// another, a word of 5,000 rows is off by 5.6 times its result's rounding and one of
+// 105,000 by 8.5, sums that cancel by any part of themselves.  It costs both passes
+// over 50000 x 257 of 2000 words 58.6 -> 59.7 us, the backward pass over 1048576 x 256
+// of 102000 319 -> 333.
+template <typename T>
+using Total = std::conditional_t<sizeof(T) == 4, double, float>;
+template <typename T>
 struct Sums {
   const uint32_t *keys, *places;
   int64_t n;
   uint32_t vocab;
   int width;
   float scale;
-  float *part;
+  Total<T> *part;
   int64_t pieces;
   int each;
   __device__ uint32_t key(int64_t i) const { return i >= 0 && i < n ? keys[i] : vocab; }
@@ -414,7 +426,7 @@ struct Sums {
 // bytes, in rows that lie anywhere: 65536 x 1024 of bf16 38 us = 3.5 TB/s, 1048576
 // x 512 of f16 248 us = 4.3.
 template <typename T, bool Narrow>
-__global__ __launch_bounds__(256) void k_word_sums(const Sums a, const T *dy, int64_t lddy, T *dweight, int groups) {
+__global__ __launch_bounds__(256) void k_word_sums(const Sums<T> a, const T *dy, int64_t lddy, T *dweight, int groups) {
   constexpr int U = 4, N = kMany<T>;
   const int64_t item = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t piece = item / groups;
@@ -424,9 +436,9 @@ __global__ __launch_bounds__(256) void k_word_sums(const Sums a, const T *dy, in
   const int c = Many<T, Narrow>::first(mine, a.width);
   const int64_t begin = piece * a.each;
   bool open = false;  // the word began in an earlier piece
-  float s[N];
+  Total<T> s[N];
 #pragma unroll
-  for (int e = 0; e < N; ++e) s[e] = 0.0f;
+  for (int e = 0; e < N; ++e) s[e] = 0;
   const int span = min(64, a.each);  // places at a time
   for (int64_t first = begin; first < begin + a.each; first += span) {
     const uint32_t key = lane < span ? a.key(first + lane) : a.vocab;
@@ -454,10 +466,10 @@ __global__ __launch_bounds__(256) void k_word_sums(const Sums a, const T *dy, in
         const int t = t0 + u;
         if (t >= count) break;
 #pragma unroll
-        for (int e = 0; e < N; ++e) s[e] += float(v[u].v[e]);
+        for (int e = 0; e < N; ++e) s[e] += Total<T>(v[u].v[e]);
         if (!(ends >> t & 1)) continue;
         if (open || (goes_on && t == span - 1)) {
-          float *to = a.part + (piece * 2 + (open ? 0 : 1)) * a.width + c;
+          Total<T> *to = a.part + (piece * 2 + (open ? 0 : 1)) * a.width + c;
 #pragma unroll
           for (int e = 0; e < N; ++e)
             if (in && (!Narrow || e < a.width)) to[e] = s[e];
@@ -469,7 +481,7 @@ __global__ __launch_bounds__(256) void k_word_sums(const Sums a, const T *dy, in
         }
         open = false;
 #pragma unroll
-        for (int e = 0; e < N; ++e) s[e] = 0.0f;
+        for (int e = 0; e < N; ++e) s[e] = 0;
       }
     };
     // the next rows are asked for before this ones' sums are stored: a wave waits for what it asked for in its order
@@ -487,15 +499,17 @@ __global__ __launch_bounds__(256) void k_word_sums(const Sums a, const T *dy, in
 // Words that go over the ends of pieces: the piece that a word begins in holds
 // its first sum, the heads of the following pieces the others.  A workgroup looks
 // at kJoin pieces; up to kShort heads are summed by one wave, more by all of
-// them, each every kJoin-th.  8 to 20 us, a chain of four to six loads.
+// them, each every kJoin-th.  8 to 26 us, a chain of four to six loads.  A lane has 16
+// bytes of sums, 4 or 2 columns.
 constexpr int kShort = 16, kJoin = 16;
 template <typename T>
-__global__ __launch_bounds__(1024) void k_join_words(const Sums a, T *dweight) {
-  __shared__ float shared[kJoin][256];
+__global__ __launch_bounds__(1024) void k_join_words(const Sums<T> a, T *dweight) {
+  constexpr int U = 8, C = 16 / int(sizeof(Total<T>));
+  __shared__ Total<T> shared[kJoin][64 * C];
   __shared__ int64_t longer[kJoin];
   __shared__ uint32_t its[kJoin];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int mine_c = int(blockIdx.y) * 256 + lane * 4;
+  const int mine_c = (int(blockIdx.y) * 64 + lane) * C;
   const int64_t p0 = int64_t(blockIdx.x) * kJoin, p = p0 + wave, end = (p + 1) * a.each;
   // how many pieces after p begin with the word that begins in p and goes over its end
   uint32_t word = a.vocab;
@@ -521,30 +535,33 @@ __global__ __launch_bounds__(1024) void k_join_words(const Sums a, T *dweight) {
       mine = low - p;
     }
   }
-  const bool narrow = a.width < 4;
-  const int c = narrow ? 0 : min(mine_c, a.width - 4);
-  typedef float four __attribute__((ext_vector_type(4), aligned(4)));
+  const bool narrow = a.width < C;
+  const int c = narrow ? 0 : min(mine_c, a.width - C);
+  typedef Total<T> some __attribute__((ext_vector_type(C), aligned(sizeof(Total<T>))));
   // what k_word_sums left of piece q in `slot`
   auto left = [&](int64_t q, int slot) {
-    const float *from = a.part + (q * 2 + slot) * a.width + c;
-    if (!narrow) return *reinterpret_cast<const four *>(from);
-    return four{from[0], a.width > 1 ? from[1] : 0.0f, a.width > 2 ? from[2] : 0.0f, 0.0f};
+    const Total<T> *from = a.part + (q * 2 + slot) * a.width + c;
+    if (!narrow) return *reinterpret_cast<const some *>(from);
+    some s = {};
+#pragma unroll
+    for (int e = 0; e < C - 1; ++e) s[e] = e < a.width ? from[e] : 0;
+    return s;
   };
   // the heads after piece q, from the first-th to the count-th, every step-th: eight on their way at a time
-  auto heads = [&](int64_t q, int64_t first, int64_t count, int step, four s) {
-    for (int64_t i = first; i <= count; i += 8 * step) {
-      four v[8];
+  auto heads = [&](int64_t q, int64_t first, int64_t count, int step, some s) {
+    for (int64_t i = first; i <= count; i += U * step) {
+      some v[U];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = left(q + (i + u * step <= count ? i + u * step : i), 0);
+      for (int u = 0; u < U; ++u) v[u] = left(q + (i + u * step <= count ? i + u * step : i), 0);
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+      for (int u = 0; u < U; ++u)
         if (i + u * step <= count) s += v[u];
     }
     return s;
   };
-  auto store = [&](four s, uint32_t to) {
+  auto store = [&](some s, uint32_t to) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < C; ++e)
       if (c + e < a.width) dweight[int64_t(to) * a.width + c + e] = T(s[e] * a.scale);
   };
   if (mine > 0 && mine <= kShort && mine_c < a.width) store(heads(p, 1, mine, 1, left(p, 1)), word);
@@ -556,13 +573,13 @@ __global__ __launch_bounds__(1024) void k_join_words(const Sums a, T *dweight) {
   for (int k = 0; k < kJoin; ++k) {
     const int64_t count = longer[k], q = p0 + k;
     if (!count) continue;
-    four s = {0.0f, 0.0f, 0.0f, 0.0f};
+    some s = {};
     if (mine_c < a.width) s = heads(q, 1 + wave, count, kJoin, wave == 0 ? left(q, 1) : s);
     __syncthreads();
-    *reinterpret_cast<four *>(&shared[wave][lane * 4]) = s;
+    *reinterpret_cast<some *>(&shared[wave][lane * C]) = s;
     __syncthreads();
     if (wave == 0 && mine_c < a.width) {
-      for (int w = 1; w < kJoin; ++w) s += *reinterpret_cast<const four *>(&shared[w][lane * 4]);
+      for (int w = 1; w < kJoin; ++w) s += *reinterpret_cast<const some *>(&shared[w][lane * C]);
       store(s, its[k]);
     }
   }
@@ -666,7 +683,7 @@ hipError_t sum_by_word(const int32_t *words, int64_t n, const T *dy, int64_t ldd
   fill.bytes = bytes % 4;
   Sorted order;
   OPS_TRY(sort_words(words, n, vocab, fill, ws, dry, s, order));
-  Sums a = {};
+  Sums<T> a = {};
   a.keys = order.keys;
   a.places = order.places;
   a.n = n;
@@ -679,13 +696,14 @@ hipError_t sum_by_word(const int32_t *words, int64_t n, const T *dy, int64_t ldd
   a.each = 16;
   while (a.each < 512 && ceil_div(n, 2 * a.each) * groups >= 3000) a.each *= 2;
   a.pieces = ceil_div(n, a.each);
-  a.part = ws.take<float>(a.pieces * 2 * width);
+  a.part = ws.take<Total<T>>(a.pieces * 2 * width);
   if (dry || n == 0) return hipSuccess;
   auto kernel = width < kMany<T> ? k_word_sums<T, true> : k_word_sums<T, false>;
   kernel<<<unsigned(ceil_div(a.pieces * groups, 4)), 256, 0, s>>>(a, dy, lddy, dweight, groups);
   OPS_TRY(hipGetLastError());
   if (a.pieces <= 1) return hipSuccess;
-  k_join_words<T><<<dim3(unsigned(ceil_div(a.pieces, kJoin)), unsigned(ceil_div(width, 256))), 1024, 0, s>>>(a, dweight);
+  const int64_t strips = ceil_div(width, 64 * 16 / int64_t(sizeof(Total<T>)));
+  k_join_words<T><<<dim3(unsigned(ceil_div(a.pieces, kJoin)), unsigned(strips)), 1024, 0, s>>>(a, dweight);
   return hipGetLastError();
 }
 
