@@ -112,12 +112,11 @@ __device__ inline void anew(Raw<T, N> &x) {
 }
 
 // A lane's first column.  The last lane of an odd row has the last N, one of which
-// its neighbour has too: both compute and store the same.  Lanes past the end have
-// the first ones, and store nothing.
+// its neighbour has too, and lanes past the end have them as well: all compute the
+// same.
 template <int N>
 __device__ inline int column_of(int group, int lane, int cols) {
-  const int c = (group * 64 + lane) * N;
-  return c < cols ? min(c, cols - N) : 0;
+  return min((group * 64 + lane) * N, cols - N);
 }
 
 // A wave's lanes are P parts of 64 / P: narrow matrices leave lanes without columns
@@ -136,6 +135,13 @@ __device__ inline int part_of(int lane) {
 template <int P>
 __device__ inline int lane_of(int lane) {
   return P == 1 ? lane : lane & (64 / P - 1);
+}
+// Whether a lane goes on to what is stored.  A whole wave reads what its rows are from
+// the registers of other lanes (doc_of), so all of its lanes have to be there to the
+// end: those past the end of a row leave, look for and store what the last one does.
+template <int N, int P>
+__device__ inline bool lane_in(int group, int lane, int cols) {
+  return P == 1 || (group * 64 + lane_of<P>(lane)) * N < cols;
 }
 
 // ------------------------------------------------------------- documents -----
@@ -514,7 +520,7 @@ __global__ __launch_bounds__(64 * kWaves, kWavesPerSimd<P>) void k_recur(const F
   __shared__ Shared<N> s;
   const int t = take_ticket(s, p.chain), block = t / p.groups;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool in = (t % p.groups * 64 + lane_of<P>(lane)) * N < p.cols;
+  const bool in = lane_in<N, P>(t % p.groups, lane, p.cols);
   const int c = column_of<N>(t % p.groups, lane_of<P>(lane), p.cols);
   const int wave_row = (block * kWaves + wave) * R * P, row0 = wave_row + part_of<P>(lane) * R;
   // rows past the end repeat the last one; what they are says that they are of no document
@@ -608,7 +614,7 @@ __global__ __launch_bounds__(64 * kWaves, kWavesPerSimd<P>) void k_recur_backwar
   __shared__ Shared<N> s;
   const int t = take_ticket(s, p.chain), back = t / p.groups, block = p.blocks - 1 - back;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool in = (t % p.groups * 64 + lane_of<P>(lane)) * N < p.cols;
+  const bool in = lane_in<N, P>(t % p.groups, lane, p.cols);
   int c = column_of<N>(t % p.groups, lane_of<P>(lane), p.cols);
   const int wave_row = (block * kWaves + wave) * R * P, row0 = wave_row + part_of<P>(lane) * R;
   const int mine = lane < R * P && wave_row + lane < p.rows ? p.info[wave_row + lane] : -1;
