@@ -1866,8 +1866,8 @@ struct Teaching {
 // both products take the two and the error is the results' rounding alone.
 // Training, us of G once / twice: 8, 32, 128 x 1024 x 141000 of bf16 344 / 378,
 // 415 / 477, 473 / 557; 128 x 257 x 9001 of f16 83 / 88.  For 8192 rows twice
-// would double two thirds of the operations.  Tiles of 256 x 256 never have the
-// least time at so few rows, and their epilogue is without it.
+// would double two thirds of the operations.  Tiles of 256 x 256, which never have the
+// least time at so few rows, have no epilogue for it: G is kept once with them.
 constexpr int kTwiceRows = 128;
 
 template <typename T, bool Teacher>
@@ -1880,8 +1880,11 @@ hipError_t softmax_backward(const lda_xent_args &a, const Teaching &teaching, Ar
     return a.dbias ? zero(a.dbias, a.vocab, s) : hipSuccess;
   }
   const int rows = int(a.rows), piece = piece_words<T>(a.rows, a.vocab), k = int(round_up(a.width, kChunk<T>));
-  const int mtiles = int(ceil_div(a.rows, tiles_of<T>(a.rows, piece).m));
-  const int times = Teacher && sizeof(T) == 2 && rows <= kTwiceRows ? 2 : 1, all = times * rows;  // of G
+  const Tiles tiles = tiles_of<T>(a.rows, piece);
+  const int mtiles = int(ceil_div(a.rows, tiles.m));
+  // what the rounding of G left is read only where the epilogue of the tiles writes it
+  const bool twice = Teacher && sizeof(T) == 2 && rows <= kTwiceRows && tiles.n < 256;
+  const int times = twice ? 2 : 1, all = times * rows;  // of G
   Packs<T> packs;
   const Matrix<T> x = operand<T>(a.x, a.ldx, a.rows, a.width, ws, packs);
   const Matrix<T> w = operand<T>(a.weight, a.ld_weight, a.vocab, a.width, ws, packs);
@@ -1913,7 +1916,7 @@ hipError_t softmax_backward(const lda_xent_args &a, const Teaching &teaching, Ar
     T *rest = times > 1 ? grad + a.rows * words_k : nullptr;
     ws.used = mark;
     if (!dry) {
-      OPS_TRY(with_shape<T>(tiles_of<T>(a.rows, piece), [&](auto shape) {
+      OPS_TRY(with_shape<T>(tiles, [&](auto shape) {
         typedef decltype(shape) S;
         const SoftmaxGrad<T, S::BN, S::WM, Teacher> epi{a.bias,   a.labels, a.lse, row_factor, grad,  words_k,
                                                         col_part, rows,     a.vocab, first,    words, teaching.unit, rest};
