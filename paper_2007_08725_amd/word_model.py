@@ -14,6 +14,8 @@ stand side by side.  Scoring new words of a document needs no sampling.
 With ``--reader`` a second model is trained, that needs no topics of a document
 but reads its words in order (``word_reader.py``), from the words alone or, with
 ``--distil``, from the fitted topics' most likely words for each document too.
+Like the others it is scored on the documents that it was trained on, whose words
+it may know by heart: that says nothing of new ones.
 
     python -m paper_2007_08725_amd.word_model --workload c1 --iters 50 --steps 300 --reader --distil 0.5
 """
@@ -156,6 +158,24 @@ def train(model, proportions, word, doc, steps: int, batch: int = 4096, lr: floa
     return [float(x) for x in losses]
 
 
+def _check(ap, args):
+    """Refuses what the reader cannot be trained with, before anything is fitted, and fills in what was not given."""
+    if not 0.0 <= args.distil <= 1.0:
+        ap.error("--distil must be 0 to 1")
+    if args.distil > 0 and not args.reader:
+        ap.error("--distil needs --reader")
+    for name, default in (("top", 32), ("temperature", 1.0)):
+        if getattr(args, name) is None:
+            setattr(args, name, default)
+        elif not args.distil > 0:
+            ap.error("--%s needs --distil" % name)
+    if not 1 <= args.top <= ops.MAX_TOP:
+        ap.error("--top must be 1 to %d" % ops.MAX_TOP)
+    most = float(np.finfo(np.float32).max)  # the operator takes it in single precision
+    if not 1.0 / most < args.temperature < most:
+        ap.error("--temperature and its reciprocal must be finite and positive")
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--workload", default="c1", choices=["c1", "c2"])
@@ -165,12 +185,14 @@ def main(argv=None):
     ap.add_argument("--batch", type=int, default=4096)
     ap.add_argument("--hidden", type=int, default=256)
     ap.add_argument("--lr", type=float, default=1e-2)
-    ap.add_argument("--reader", action="store_true", help="train a reader of the words in order too")
+    ap.add_argument("--reader", action="store_true",
+                    help="train a reader of the words in order too (scored on the documents that it was trained on)")
     ap.add_argument("--distil", type=float, default=0.0, help="the fitted topics' part of the reader's loss, 0 to 1")
-    ap.add_argument("--top", type=int, default=32, help="words that the fitted topics list for a document")
-    ap.add_argument("--temperature", type=float, default=1.0)
+    ap.add_argument("--top", type=int, help="words that the fitted topics list for a document (32)")
+    ap.add_argument("--temperature", type=float, help="of the fitted topics' and the reader's probabilities (1)")
     ap.add_argument("--eval-tokens", type=int, default=1 << 20, help="tokens scored at the end, from the corpus' start")
     args = ap.parse_args(argv)
+    _check(ap, args)
 
     import lda_synth
 
