@@ -78,7 +78,8 @@ class WordReader(Trained):
         dh, dweight, dbias = ops.softmax_xent_backward(dloss, lse, h, p["weight"], words, p["bias"])
         if taught is not None:
             more = ops.softmax_distill_backward(dapart, *taught)
-            dh, dweight, dbias = dh + more[0], dweight + more[1], dbias + more[2]
+            # the weight's in 32 bits, as the step takes it: no third rounding to the products' type
+            dh, dweight, dbias = dh + more[0], dweight.float() + more[1], dbias + more[2]
         dx, dw_gate, dw_value = ops.gated_backward(dh, x, p["w_gate"], p["w_value"], self.act)
         ds, dnorm_weight, dnorm_bias = ops.layer_norm_backward(dx, s, p["norm_weight"], mean, rstd)
         de, dg, _ = ops.recurrence_backward(ds, e, g, offsets, kept)
@@ -120,7 +121,10 @@ class WordReader(Trained):
                 torch.zeros(docs, self.width, device=device))
 
     def read(self, state, words):
-        """Scores the next word of each document and reads it: ``(loss, state)``, as ``loss`` has them for the whole."""
+        """Scores the next word of each document and reads it: ``(loss, state)``, as ``loss`` has them for the whole.
+
+        A document that has ended among others has the word -1: its loss is 0, and what its state is then says nothing.
+        """
         p, s, exact = state
         _, _, _, h = self._hidden(p, s)
         loss, _ = ops.softmax_xent(h, p["weight"], words, p["bias"])
