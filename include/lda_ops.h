@@ -55,6 +55,10 @@ typedef enum { LDA_SILU = 0, LDA_GELU = 1, LDA_SIGMOID = 2 } lda_act;
 /* Most tiles of 128 x 128 of a product's result (logits, gated layer, weight
  * gradient): a call on more rows is made in parts. */
 #define LDA_OPS_MAX_TILES 8388608
+/* Most bytes of an embedding's gradient, and most parts of 512 rows by 1,024 bytes
+ * that it is summed from. */
+#define LDA_OPS_MAX_EMBED_BYTES 273804165120
+#define LDA_OPS_MAX_EMBED_PARTS 67108860
 /* Most words that a teacher lists for a row, and most of all rows of a call
  * (rows times top). */
 #define LDA_OPS_MAX_TOP 256

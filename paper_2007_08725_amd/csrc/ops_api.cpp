@@ -140,6 +140,11 @@ lda_status check_embed(const lda_embed_args *a, bool backward) {
   REQUIRE(a->words || a->rows == 0, LDA_E_ARG, "words is NULL");
   if (backward) {
     REQUIRE(a->dweight, LDA_E_ARG, "dweight is NULL");
+    const int64_t size = a->dtype == LDA_F32 ? 4 : 2;
+    REQUIRE(int64_t(a->vocab) * a->width * size <= LDA_OPS_MAX_EMBED_BYTES, LDA_E_RANGE,
+            "an embedding's gradient of more than LDA_OPS_MAX_EMBED_BYTES");
+    REQUIRE(ceil_div(a->rows, 512) * ceil_div(a->width, 1024 / size) <= LDA_OPS_MAX_EMBED_PARTS, LDA_E_RANGE,
+            "an embedding's gradient from more than LDA_OPS_MAX_EMBED_PARTS parts of 512 rows by 1,024 bytes");
     return check_in(a->dy, a->lddy, a->rows, "dy is NULL");
   }
   LDA_TRY(check_in(a->weight, a->ld_weight, a->rows, "weight is NULL"));
