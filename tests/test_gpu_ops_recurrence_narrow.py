@@ -97,6 +97,31 @@ def test_same_bits_and_streams(ops, dtype, cols):  # noqa: F811
         assert all(torch.equal(one[n], want[n]) for n in NAMES)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [1, 5, 20, 40])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_bad_documents_between_sound_ones(ops, dtype, cols, bad):  # noqa: F811
+    """Documents of nothing but infinities or NaN, which begin and end inside the rows of a part, a wave and a workgroup,
+    and padding that holds the same, leave every other document's bits as they are."""
+    lengths = [3, 5, 40, 20, 3, 1, 700, 300, 9000, 1, 90, 2, 5000, 77]
+    off, rows = offsets_of(lengths, 11), sum(lengths) + 30
+    x, gate, state, dh, dlast = inputs(dtype, rows, cols, len(lengths), True)
+    want = everything(ops, x, gate, off, state, dh, dlast)
+    sound = torch.ones(rows, dtype=torch.bool, device="cuda")
+    for s in range(1, len(lengths), 2):
+        part = slice(int(off[s]), int(off[s + 1]))
+        sound[part] = False
+        for t in (x, gate, dh):
+            t[part] = bad
+        state[s], dlast[s] = bad, bad
+    for t in (x, gate, dh):
+        t[:11], t[int(off[-1]):] = bad, bad
+    got = everything(ops, x, gate, off, state, dh, dlast)
+    for name in NAMES:
+        at = slice(0, None, 2) if name in ("last", "dstate") else sound
+        assert torch.equal(got[name][at], want[name][at]), name
+
+
 @pytest.mark.parametrize("dtype,cols", [(torch.float32, 20), (torch.float32, 12), (torch.bfloat16, 20),
                                         (torch.float16, 48), (torch.bfloat16, 1)])
 def test_in_a_graph(ops, dtype, cols):  # noqa: F811
