@@ -311,9 +311,9 @@ lda_status lda_recurrence_step(const lda_recur_args *a);
  * without words).  As for the softmax cross entropy the logits are recomputed in
  * pieces of the vocabulary, one piece of G is kept, without the power of two in
  * dloss / temperature and in 16-bit types rounded to them (up to 128 rows with what
- * the rounding left beside it), and rows of weight must be finite; in half precision a row's part of dweight loses bits as there.  dbias
- * is NULL if and only if bias is.  temperature and its reciprocal must be finite
- * and positive.
+ * the rounding left beside it), and rows of weight must be finite; in half precision
+ * a row's part of dweight loses bits as there.  dbias is NULL if and only if bias is.
+ * temperature and its reciprocal must be finite and positive.
  */
 typedef struct {
   int32_t dtype;

@@ -68,13 +68,15 @@ struct Many {
 // 2^shift lanes a row (a workgroup has 256 >> shift rows at a time), four rows
 // of each lane in flight.
 //
-// Bound by its bytes: 65536 words x 1024 of bf16 from a table of 141000 rows 38 us
-// = 4.3 TB/s of y and the rows that are named, 1048576 x 512 of f16 279 us = 4.0.
+// Bound by its bytes: 65536 words x 1024 of bf16 from a table of 141000 rows 37 us
+// = 4.4 TB/s of y and the rows that are named, 1048576 x 512 of f16 281 us = 4.0.
+// Rows that do not lie on a grid of 16 bytes take longer: 50000 x 256 from 2000 rows in
+// single precision 11.0 us a call, x 257 15.2.
 //
 // Results that are larger than the last cache (256 MB) are stored past it, so
 // that it keeps the table and dy: both passes over 1048576 words x 512 of f16
-// 673 -> 636 us.  Smaller ones are left in it for who reads them (50000 x 257 in
-// single precision 63 us, past it 77).
+// 673 -> 636 us.  Smaller ones are left in it for who reads them (both passes
+// over 50000 x 257 in single precision, when they took 63 us: past it 77).
 template <typename T, bool Narrow, bool Past>
 __global__ __launch_bounds__(256) void k_embed(const int32_t *words, int64_t rows, const T *weight, int64_t ldw,
                                                int width, int vocab, float scale, int shift, T *y, int64_t ldy) {
@@ -424,7 +426,7 @@ struct Sums {
 
 // A wave a piece and 64 kMany columns, eight rows of dy in flight.  Bound by dy's
 // bytes, in rows that lie anywhere: 65536 x 1024 of bf16 38 us = 3.5 TB/s, 1048576
-// x 512 of f16 248 us = 4.3.
+// x 512 of f16 247 us = 4.3.
 template <typename T, bool Narrow>
 __global__ __launch_bounds__(256) void k_word_sums(const Sums<T> a, const T *dy, int64_t lddy, T *dweight, int groups) {
   constexpr int U = 4, N = kMany<T>;

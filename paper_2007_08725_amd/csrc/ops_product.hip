@@ -1864,9 +1864,9 @@ struct Teaching {
 // products are bound by the weights and not by G, it is kept in twice its bits: as
 // G and what its rounding left, which stands below it as further rows, so that
 // both products take the two and the error is the results' rounding alone.
-// Training, us of G once / twice: 8, 32, 128 x 1024 x 141000 of bf16 344 / 378,
-// 415 / 477, 473 / 557; 128 x 257 x 9001 of f16 83 / 88.  For 8192 rows twice
-// would double two thirds of the operations.  Tiles of 256 x 256, which never have the
+// Training, us of G once / twice: 8, 32, 128 x 1024 x 141000 of bf16 300 / 309,
+// 342 / 381, 408 / 467; 128 x 257 x 9001 of f16 80 / 84.  More rows pay more, 129
+// 436 / 562, 256 522 / 668; for 8192 twice would double two thirds of the operations.  Tiles of 256 x 256, which never have the
 // least time at so few rows, have no epilogue for it: G is kept once with them.
 constexpr int kTwiceRows = 128;
 
@@ -1984,8 +1984,8 @@ lda_xent_args student(const lda_distill_args &a) {
 }
 
 // 8192 x 1024 x 141000 of bf16, 32 words listed: forward 2.2 ms, as the cross
-// entropy's and 68 us for the listed words; backward 6.7 ms, of which the teacher's
-// part, its words' sort for dbias included, is 0.16.
+// entropy's and 69 us for the listed words; backward 6.7 ms, of which the teacher's
+// part, its words' sort and sums for dbias included, is 0.13.
 template <typename T>
 hipError_t distill_forward_t(const lda_distill_args &a, Arena &ws, bool dry) {
   const float unit = 1.0f / a.temperature;

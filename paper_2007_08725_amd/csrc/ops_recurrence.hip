@@ -10,7 +10,9 @@
 // every input is read once and every output written once, and the results are
 // those of one fixed order of the operations whichever workgroup was faster.
 // A document's first row cuts the chain: a map with a first row in it does not
-// depend on the state that comes in.
+// depend on the state that comes in.  Scans in one pass that look back in this way
+// were published by D. Merrill and M. Garland (Single-pass Parallel Prefix Scan with
+// Decoupled Look-back, 2016).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -34,8 +36,8 @@ constexpr int kWaves = 8;
 // Rows of a wave, which has N columns a lane: as many as leave room in the
 // registers for two workgroups a CU (128 a lane), so that one loads while the
 // other waits or computes.  Both passes over 65536 rows x 1024 of bf16: 8 waves of
-// 16 rows 277 us, 4 waves 309, 16 waves 312, 8 waves of 32 rows (one workgroup a
-// CU) 625.  In single precision the backward pass' three matrices fill twice as
+// 16 rows 278 us, 4 waves 316, 16 waves 288, 8 waves of 32 rows (one workgroup a
+// CU) 318.  In single precision the backward pass' three matrices fill twice as
 // many registers.
 template <typename T, int N, bool Back>
 constexpr int kRows = Back && sizeof(T) == 4 ? 16 : 32 / N;
@@ -310,9 +312,8 @@ struct Look {
 // them has (the first at once).  A look at memory takes 1.5 us in a
 // full machine, as long as a sixth of a workgroup's life, and 2 KiB of all
 // columns' words: a wave looks at one word until it knows that it needs the others
-// (with all columns at each look 366 us instead of 306 for both passes over 65536
-// rows x 1024 of bf16; with the first look before the workgroup's maps are joined
-// 362).
+// (when both passes over 65536 rows x 1024 of bf16 took 306 us, all columns at each
+// look took 366, and a first look before the workgroup's maps are joined 362).
 template <int N, int P>
 __device__ inline void state_in(Shared<N> &s, const Chain &chain, int block, int order, bool needed, int group, bool in,
                                 const float (&map_a)[N], const float (&map_b)[N], bool cuts, float (&m)[N]) {
@@ -510,10 +511,10 @@ struct Forward {
 };
 
 // Bound by its bytes, x and gate in and h out, with an eighth of h more in the kept
-// states and a tenth of the time in looking back: 65536 rows x 1024 of bf16 103 us
-// = 3.9 TB/s of x, gate and h (a copy reaches 4.8), 262144 x 1000 of f16 390 us =
+// states and a tenth of the time in looking back: 65536 rows x 1024 of bf16 99 us
+// = 4.1 TB/s of x, gate and h (a copy reaches 4.8), 262144 x 1000 of f16 389 us =
 // 4.0; one document of 65537 rows x 257 in single precision, where every workgroup
-// waits for the state of those before it, 69 us = 2.9.
+// waits for the state of those before it, 67 us = 3.0.
 template <typename T, int N, int P, bool Past>
 __global__ __launch_bounds__(64 * kWaves, kWavesPerSimd<P>) void k_recur(const Forward<T> p) {
   constexpr int R = kRows<T, N, false>;
@@ -606,8 +607,8 @@ struct Backward {
 // The states are computed again from the kept ones, and the gradients run the
 // other way: row t passes l_t g_t on to row t - 1, where l_t is f_t, or nothing
 // where the chain is cut; m -> l (dh + m) is a row's map.  65536 rows x 1024 of
-// bf16: 168 us = 4.0 TB/s of x, gate, dh, dx and dgate; 65537 x 257 in single
-// precision 110 us = 3.1.
+// bf16: 165 us = 4.1 TB/s of x, gate, dh, dx and dgate; 65537 x 257 in single
+// precision 104 us = 3.2.
 template <typename T, int N, int P, bool Past>
 __global__ __launch_bounds__(64 * kWaves, kWavesPerSimd<P>) void k_recur_backward(const Backward<T> p) {
   constexpr int R = kRows<T, N, true>;
