@@ -169,5 +169,6 @@ def fit(corpus, args, word_counts, teacher=None):
     losses = train(model, words, offsets, args.steps, args.batch, args.lr, teacher, args.distil, args.temperature)
     elapsed = time.perf_counter() - t0
     return dict(llpt_reader_before=before, llpt_reader=model.llpt(words, offsets[:some + 1]),
+                llpt_reader_of="documents that it was trained on",
                 reader_first_loss=losses[0] if losses else None, reader_last_loss=losses[-1] if losses else None,
                 reader_ms_per_step=elapsed * 1e3 / max(1, args.steps))

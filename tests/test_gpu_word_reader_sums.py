@@ -23,3 +23,12 @@ def test_weight_gradients_are_added_in_single_precision(corpus, dtype):  # noqa:
     one = ops.softmax_xent_backward(dloss, lse, h, p["weight"], words, p["bias"])[1]
     two = ops.softmax_distill_backward(dapart, *taught)[1]
     assert got.dtype == torch.float32 and torch.equal(got, one.float() + two.float())
+
+
+def test_the_command_says_what_the_reader_is_scored_on(capsys):
+    import json
+    from paper_2007_08725_amd import word_model
+    assert word_model.main(["--docs", "60", "--iters", "2", "--steps", "2", "--batch", "256", "--hidden", "16",
+                            "--reader", "--distil", "0.3", "--top", "4", "--temperature", "2"]) == 0
+    said = json.loads(capsys.readouterr().out.strip().splitlines()[-1])
+    assert said["llpt_reader"] < 0 and "trained on" in said["llpt_reader_of"]
